@@ -51,6 +51,7 @@ extern "C" {
 #define LRC_FP64 0
 #define LRC_FP32 1
 #define LRC_FP16 2
+#define LRC_BF16 3          /* output-head calls only (lrc_q4_*, lrc_sample, lrc_distill*) */
 
 /* return codes */
 #define LRC_OK 0
@@ -411,6 +412,144 @@ int lrc_rsvd(const double* A, int64_t m, int64_t n, const double* omega, int64_t
  * Synchronizes.  Errors as lrc_rsvd (LRC_ENUMERIC names the step). */
 int lrc_tt_rsvd(const double* T, const int64_t* dims, const int64_t* ranks, int d, const double* const* omegas,
                 const int64_t* samples, int power_iters, double* const* cores, double* sigma);
+
+/* ---- Compressed output head: 4-bit weights with rank compensation, the
+ * draw from the logits they give, and the loss that fits the compensation
+ * to an uncompressed teacher.  Matrices of these calls may have a row pitch
+ * (ld*, in elements, at least the row's length); elements within a row are
+ * contiguous.  Calls of zero rows return LRC_OK and launch nothing. */
+
+/*
+ * 4-bit weights.  W (m x n) is stored as
+ *   codes   m rows of lrc_q4_row_bytes(n) = 16 ceil(n / 32) bytes; column j of
+ *           a row is bits 4 (j & 1) .. of byte j / 2, an E2M1 code (bit 3 the
+ *           sign; magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6 for bits 0..2 = 0..7),
+ *           the columns from n on are 0; 16-byte aligned
+ *   scales  m x ceil(n / group) in `sprec` (LRC_FP32, LRC_FP16 or LRC_BF16),
+ *           group one of 32, 64, 128, 256, 512
+ * and stands for w_ij = code_ij scale_i,(j / group).
+ */
+int64_t lrc_q4_row_bytes(int64_t n);
+/* Stored bytes of codes and scales; LRC_EINVAL / LRC_EOVERFLOW as elsewhere. */
+int64_t lrc_q4_storage_bytes(int64_t m, int64_t n, int64_t group, int sprec);
+
+/*
+ * lrc_q4_quantize -- 4-bit weights from dense ones
+ *   W       device, m x n of pitch ldw, in `prec` (any of the four)
+ *   codes, scales  device, written whole (layout above)
+ *   values  device, m x n (no pitch), in `prec`, or NULL: the values the codes
+ *           stand for, rounded once; W - values is what a compensation fits
+ *   n_nonfinite  host, or NULL.  When given, the call waits for the result and
+ *           stores the number of groups that hold a NaN or an infinity or whose
+ *           scale overflows `sprec`; such a group gets the scale NaN.
+ * scale = max |w| of the group times 1/6 (each rounded to binary32, binary64 for
+ * LRC_FP64), rounded to binary32 and then to sprec; a code is the E2M1 value nearest to the quotient w / scale (rounded to binary32;
+ * binary64 for LRC_FP64), ties to the even code, magnitudes above 6 become 6.
+ * A group whose scale is 0 gets codes 0.  Enqueued on the calling thread's
+ * stream; without n_nonfinite it returns without synchronizing.
+ * Errors: LRC_EINVAL for NULL pointers, m or n < 1, ldw < n, another group,
+ * unknown precisions, misaligned codes or an output that overlaps W or another
+ * output; LRC_EOVERFLOW, LRC_ENOMEM, LRC_EHIP, LRC_ENODEV as elsewhere.
+ */
+int lrc_q4_quantize(const void* W, int64_t ldw, int64_t m, int64_t n, int64_t group, int prec, void* codes,
+                    void* scales, int sprec, void* values, int64_t* n_nonfinite);
+
+/*
+ * lrc_q4_apply -- Y = X W^T + [(X V) diag(s)] U^T for 4-bit weights W
+ *   codes, scales, sprec, group   the weights (m x n), layout above
+ *   U, s, V, k, fprec   rank-k compensation as lrc_matrix_apply stores it
+ *           (U m x k, s k, V n x k, row-major without pitch), in fprec
+ *           (LRC_FP32, LRC_FP16 or LRC_BF16); k = 0: none, the pointers may be
+ *           NULL
+ *   X       device, batch rows of n values, pitch ldx, in `prec` (LRC_FP32,
+ *           LRC_FP16 or LRC_BF16); one row per token
+ *   Y       device, batch rows of m values, pitch ldy, in `yprec` (the same
+ *           three), rounded once
+ * Products of codes and activations are exact and summed in binary32 (a
+ * binary32 activation as the exact sum of three bfloat16 values; below 2^-110
+ * its last bits may be lost), the scale of a group enters in binary32, and so
+ * does the compensation, whose (X V) diag(s) is not rounded further.  Sums are
+ * split in a fixed order: bitwise reproducible.  Infinities and NaN in X reach
+ * the outputs of their row as in the sums above (a zero weight times an
+ * infinity is NaN).
+ * Errors: LRC_EINVAL for NULL pointers, m or n < 1, batch or k < 0, k >
+ * min(m, n), ldx < n, ldy < m, another group, unknown precisions, misaligned
+ * codes or Y overlapping an input; LRC_EOVERFLOW, LRC_ENOMEM, LRC_EHIP,
+ * LRC_ENODEV as elsewhere.
+ */
+int lrc_q4_apply(const void* codes, const void* scales, int sprec, int64_t group, const void* U, const void* s,
+                 const void* V, int64_t k, int fprec, const void* X, int64_t ldx, void* Y, int64_t ldy, int64_t m,
+                 int64_t n, int64_t batch, int prec, int yprec);
+
+/*
+ * lrc_sample -- one token per row of logits
+ *   logits  device, rows x vocab of pitch ld, in `prec` (LRC_FP32, LRC_FP16 or
+ *           LRC_BF16); NaN counts as -infinity
+ *   u       device, rows uniform numbers in [0, 1) (others are moved to the
+ *           nearer end, NaN to 0)
+ *   temperature, top_k, top_p, min_p   device, one value per row, or NULL: 1
+ *           and three filters that are off
+ *   tokens  device, rows indices; -1 for a row whose logits are all -infinity
+ * With M the row's largest logit and z = (l - M) c, c = log2(e) / T: a token
+ * weighs w = 2^z, held as the whole number floor(2^31 w).  Kept are
+ *   the top_k first tokens by logit, ties by index (top_k < 1: all),
+ *   of those the tokens before which less than top_p of their mass lies (the
+ *     first always; off unless top_p < 1),
+ *   of those the tokens with w >= min_p (off unless min_p > 0; above 1 as 1),
+ * and the token is the first index at which the running sum of the kept
+ * weights exceeds u times their total.  A temperature that is not above 0
+ * takes the largest logit of lowest index.  The sums are of whole numbers: the
+ * result does not depend on how the work is split.
+ * Errors: LRC_EINVAL for NULL logits, u or tokens, rows < 0, vocab < 1 or >=
+ * 2^31, ld < vocab, an unknown precision or tokens overlapping an input;
+ * LRC_EOVERFLOW, LRC_ENOMEM, LRC_EHIP, LRC_ENODEV as elsewhere.
+ */
+int lrc_sample(const void* logits, int64_t ld, int64_t rows, int64_t vocab, int prec, const float* u,
+               const float* temperature, const int64_t* top_k, const float* top_p, const float* min_p,
+               int64_t* tokens);
+
+/*
+ * lrc_distill -- distillation loss from a teacher's top logits, and its
+ * gradient by the student's logits
+ *   logits  device, rows x vocab of pitch ld, in `prec` (LRC_FP32, LRC_FP16 or
+ *           LRC_BF16): the student's z
+ *   ids, top   device, rows x K token indices and the teacher's logits t of
+ *           them, in `tprec` (the same three); an id outside [0, vocab) is an
+ *           unused slot; an id named twice counts with both
+ *   teacher_lse   device, rows values log sum_j exp(t_j / T) over the teacher's
+ *           whole vocabulary, or NULL: the teacher is renormalized over the
+ *           named tokens
+ *   weight  device, rows, or NULL (1); a row of weight 0 is not read and gives
+ *           zeros
+ *   temperature   T > 0
+ *   loss    device, rows:  w T^2 [ sum_k p_k (log p_k - log q_k)
+ *                                  + r (log r - log Q) ],
+ *           q = softmax(z / T), p_k = exp(t_k / T - lse), r = 1 - sum_k p_k (0
+ *           without teacher_lse), Q the student's mass outside the named tokens
+ *   stats   device, rows x 4, or NULL: what lrc_distill_backward needs
+ *   grad    device, rows x vocab of pitch ldg, in `prec`, or NULL: d (sum of
+ *           the losses) / d logits; may be `logits` itself (ldg = ld)
+ * A row whose teacher names nothing gives 0 without teacher_lse.  Terms of
+ * p_k = 0 are 0; a named token that the student gives -infinity makes the loss
+ * infinite; a row that holds a NaN or nothing but -infinity gives NaN.  Sums are split in a
+ * fixed order: bitwise reproducible.
+ * Errors: LRC_EINVAL for NULL logits, ids, top or loss, rows < 0, vocab < 1 or
+ * >= 2^31, K outside [1, LRC_DISTILL_MAX_TOP], pitches below vocab, T not a
+ * positive finite number, unknown precisions or an output that overlaps an
+ * input (other than grad = logits) or another output; LRC_EOVERFLOW, LRC_EHIP,
+ * LRC_ENODEV as elsewhere.
+ */
+#define LRC_DISTILL_MAX_TOP 1024
+int lrc_distill(const void* logits, int64_t ld, int64_t rows, int64_t vocab, int prec, const int64_t* ids,
+                const void* top, int64_t K, int tprec, const float* teacher_lse, const float* weight,
+                double temperature, float* loss, float* stats, void* grad, int64_t ldg);
+
+/* The gradient alone: grad = dloss_i d loss_i / d logits, from the same inputs
+ * as lrc_distill and the stats that it wrote; dloss device, rows, or NULL (1).
+ * Errors as lrc_distill, with stats and grad required. */
+int lrc_distill_backward(const void* logits, int64_t ld, int64_t rows, int64_t vocab, int prec, const int64_t* ids,
+                         const void* top, int64_t K, int tprec, const float* teacher_lse, const float* weight,
+                         double temperature, const float* stats, const float* dloss, void* grad, int64_t ldg);
 
 /* Stored bytes of rank-k factors in `prec`: (b/8) k (m+n+1)  (Sec. 4.2).
  * Returns LRC_EINVAL for bad arguments or LRC_EOVERFLOW on overflow. */

@@ -16,7 +16,7 @@ CSRC = os.path.join(HERE, "csrc")
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "liblrc.so")
 SOURCES = ["apply.hip", "tt.hip", "reduce.hip", "quant.hip", "gauge.hip", "quality.hip", "factor.hip", "ceiling.hip",
-           "lrc_api.cpp"]
+           "q4.hip", "sample.hip", "distill.hip", "lrc_api.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 

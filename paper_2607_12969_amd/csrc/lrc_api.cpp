@@ -11,6 +11,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <initializer_list>
 #include <map>
 #include <mutex>
 #include <string>
@@ -827,6 +828,264 @@ int lrc_certify(const lrc_cert_args* args, lrc_cert_result* res) {
     if (args->kind == LRC_CERT_TT) return certify_tt(args, res);
     return fail(LRC_EINVAL, "unknown certificate kind %d", args->kind);
 }
+
+// ------------------------------------------------------------ output head --
+namespace {
+
+// The entry points below let no exception out (allocation of host memory).
+#define LRC_NO_EXCEPTION \
+    catch (...) {        \
+        return LRC_ENOMEM; \
+    }
+
+bool head_prec(int p) { return p == LRC_FP32 || p == LRC_FP16 || p == LRC_BF16; }
+
+// Bytes from the first to past the last element of `rows` rows of `cols`
+// elements at a pitch; false on overflow.
+bool span_bytes(int64_t rows, int64_t ld, int64_t cols, int64_t e, size_t* out) {
+    int64_t t;
+    if (!mul_ok(rows, ld, &t) || !mul_ok(t, e, &t) || !mul_ok(cols, e, &t)) return false;
+    *out = rows < 1 ? 0 : (size_t)(((rows - 1) * ld + cols) * e);
+    return true;
+}
+
+struct Span {
+    const void* p;
+    size_t bytes;
+    const char* name;
+};
+
+// LRC_EINVAL when `out` overlaps one of the given arrays (NULL ones do not count).
+int check_out(const Span& out, std::initializer_list<Span> others) {
+    for (const Span& o : others)
+        if (out.p && o.p && out.bytes && o.bytes && overlaps(out.p, out.bytes, o.p, o.bytes))
+            return fail(LRC_EINVAL, "output %s overlaps %s", out.name, o.name);
+    return LRC_OK;
+}
+
+bool q4_group(int64_t g) { return g == 32 || g == 64 || g == 128 || g == 256 || g == 512; }
+
+// Sizes of the stored weights.
+int check_q4(int64_t m, int64_t n, int64_t group, int sprec, size_t* code_bytes, size_t* scale_bytes) {
+    if (m < 1 || n < 1) return fail(LRC_EINVAL, "sizes must be >= 1 (m=%lld n=%lld)", (long long)m, (long long)n);
+    if (!q4_group(group)) return fail(LRC_EINVAL, "group = %lld is not 32, 64, 128, 256 or 512", (long long)group);
+    if (!head_prec(sprec)) return fail(LRC_EINVAL, "unknown precision code %d of the scales", sprec);
+    int64_t c, s;
+    if (n > INT64_MAX - 512 || !mul_ok(m, q4_row_bytes(n), &c) || !mul_ok(m, (n + group - 1) / group, &s) ||
+        !mul_ok(s, elem_bytes(sprec), &s) || c > INT64_MAX - s || !mul_ok(m, (n + 511) / 512, &c))
+        return fail(LRC_EOVERFLOW, "array sizes overflow int64");
+    *code_bytes = (size_t)m * q4_row_bytes(n);
+    *scale_bytes = (size_t)s;
+    return LRC_OK;
+}
+
+int check_logits(const void* logits, int64_t ld, int64_t rows, int64_t vocab, int prec) {
+    if (rows < 0) return fail(LRC_EINVAL, "rows = %lld < 0", (long long)rows);
+    if (vocab < 1 || vocab > INT32_MAX) return fail(LRC_EINVAL, "vocab = %lld outside [1, 2^31)", (long long)vocab);
+    if (rows > INT32_MAX) return fail(LRC_EOVERFLOW, "rows = %lld above 2^31 - 1", (long long)rows);
+    if (ld < vocab) return fail(LRC_EINVAL, "pitch %lld below vocab = %lld", (long long)ld, (long long)vocab);
+    if (!head_prec(prec)) return fail(LRC_EINVAL, "unknown precision code %d", prec);
+    if (rows > 0 && !logits) return fail(LRC_EINVAL, "NULL array argument");
+    size_t t;
+    if (!span_bytes(rows, ld, vocab, elem_bytes(prec), &t)) return fail(LRC_EOVERFLOW, "array sizes overflow int64");
+    return LRC_OK;
+}
+
+}  // namespace
+
+int64_t lrc_q4_row_bytes(int64_t n) {
+    if (n < 1) return fail(LRC_EINVAL, "n = %lld < 1", (long long)n);
+    if (n > INT64_MAX - 512) return fail(LRC_EOVERFLOW, "n overflows");
+    return q4_row_bytes(n);
+}
+
+int64_t lrc_q4_storage_bytes(int64_t m, int64_t n, int64_t group, int sprec) {
+    size_t c, s;
+    const int rc = check_q4(m, n, group, sprec, &c, &s);
+    return rc ? rc : (int64_t)(c + s);
+}
+
+int lrc_q4_quantize(const void* W, int64_t ldw, int64_t m, int64_t n, int64_t group, int prec, void* codes,
+                    void* scales, int sprec, void* values, int64_t* n_nonfinite) try {
+    if (!W || !codes || !scales) return fail(LRC_EINVAL, "NULL array argument");
+    if (!valid_prec(prec) && prec != LRC_BF16) return fail(LRC_EINVAL, "unknown precision code %d", prec);
+    size_t cb, sb, wb, vb;
+    int rc = check_q4(m, n, group, sprec, &cb, &sb);
+    if (rc) return rc;
+    if (ldw < n) return fail(LRC_EINVAL, "pitch %lld below n = %lld", (long long)ldw, (long long)n);
+    if (!span_bytes(m, ldw, n, elem_bytes(prec), &wb) || !span_bytes(m, n, n, elem_bytes(prec), &vb))
+        return fail(LRC_EOVERFLOW, "array sizes overflow int64");
+    if ((m * ((n + 511) / 512) + 3) / 4 > INT32_MAX) return fail(LRC_EOVERFLOW, "more than 2^31 - 1 workgroups");
+    if (reinterpret_cast<uintptr_t>(codes) % 16) return fail(LRC_EINVAL, "codes must be 16-byte aligned");
+    const Span w{W, wb, "W"}, c{codes, cb, "codes"}, s{scales, sb, "scales"}, v{values, vb, "values"};
+    if ((rc = check_out(c, {w, s, v})) || (rc = check_out(s, {w, v})) || (rc = check_out(v, {w}))) return rc;
+    int dev;
+    rc = current_device(&dev, nullptr);
+    if (rc) return rc;
+    hipStream_t st = g_stream;
+    unsigned long long* bad = nullptr;
+    if (n_nonfinite) {
+        Workspace& ws = workspace_for(dev, st);
+        ws.reset();
+        hipError_t e = ws.reserve(256, st);
+        if (e != hipSuccess) return fail_hip(e, "workspace");
+        bad = static_cast<unsigned long long*>(ws.take(8));
+    }
+    hipError_t e = launch_q4_quantize(W, ldw, prec, m, n, group, codes, scales, sprec, values, bad, st);
+    if (e != hipSuccess) return fail_hip(e, "4-bit quantization launch");
+    if (n_nonfinite) {
+        unsigned long long count = 0;
+        e = hipMemcpyAsync(&count, bad, 8, hipMemcpyDeviceToHost, st);
+        if (e == hipSuccess) e = hipStreamSynchronize(st);
+        if (e != hipSuccess) return fail_hip(e, "non-finite count");
+        *n_nonfinite = (int64_t)count;
+    }
+    return LRC_OK;
+} LRC_NO_EXCEPTION
+
+int lrc_q4_apply(const void* codes, const void* scales, int sprec, int64_t group, const void* U, const void* s,
+                 const void* V, int64_t k, int fprec, const void* X, int64_t ldx, void* Y, int64_t ldy, int64_t m,
+                 int64_t n, int64_t batch, int prec, int yprec) try {
+    size_t cb, sb, xb, yb;
+    int rc = check_q4(m, n, group, sprec, &cb, &sb);
+    if (rc) return rc;
+    if (!head_prec(prec) || !head_prec(yprec))
+        return fail(LRC_EINVAL, "unknown precision code %d", head_prec(prec) ? yprec : prec);
+    if (batch < 0 || k < 0) return fail(LRC_EINVAL, "batch = %lld or k = %lld < 0", (long long)batch, (long long)k);
+    if (k > std::min(m, n)) return fail(LRC_EINVAL, "k = %lld exceeds min(m, n)", (long long)k);
+    if (k > 0 && !head_prec(fprec)) return fail(LRC_EINVAL, "unknown precision code %d of the factors", fprec);
+    if (ldx < n || ldy < m) return fail(LRC_EINVAL, "pitches %lld, %lld below n = %lld, m = %lld", (long long)ldx,
+                                        (long long)ldy, (long long)n, (long long)m);
+    if (!codes || !scales || (k > 0 && (!U || !s || !V)) || (batch > 0 && (!X || !Y)))
+        return fail(LRC_EINVAL, "NULL array argument");
+    if (reinterpret_cast<uintptr_t>(codes) % 16) return fail(LRC_EINVAL, "codes must be 16-byte aligned");
+    int64_t t, fe = k > 0 ? elem_bytes(fprec) : 0, need;
+    if (!span_bytes(batch, ldx, n, elem_bytes(prec), &xb) || !span_bytes(batch, ldy, m, elem_bytes(yprec), &yb) ||
+        !mul_ok(m, k, &t) || !mul_ok(t, fe, &t) || !mul_ok(n, k, &t) || !mul_ok(t, fe, &t) ||
+        !mul_ok(std::max<int64_t>(batch, 1), n, &need) || !mul_ok(need, 64, &need) ||
+        !mul_ok(std::max<int64_t>(batch, 1), std::max<int64_t>(k, 1), &need) || !mul_ok(need, 8192, &need))
+        return fail(LRC_EOVERFLOW, "array sizes overflow int64");
+    if ((rc = check_out({Y, yb, "Y"}, {{codes, cb, "codes"}, {scales, sb, "scales"}, {X, xb, "X"},
+                                       {k ? U : nullptr, (size_t)(m * k * fe), "U"}, {k ? s : nullptr, (size_t)(k * fe), "s"},
+                                       {k ? V : nullptr, (size_t)(n * k * fe), "V"}})))
+        return rc;
+    if (batch == 0) return LRC_OK;
+    int dev;
+    rc = current_device(&dev, nullptr);
+    if (rc) return rc;
+    hipStream_t st = g_stream;
+    const Q4Weights w{codes, scales, m, n, group, sprec, U, s, V, k, fprec};
+    Workspace& ws = workspace_for(dev, st);
+    ws.reset();
+    const size_t bytes = q4_apply_workspace_bytes(w, batch, prec);
+    hipError_t e = bytes ? ws.reserve(bytes, st) : hipSuccess;
+    if (e != hipSuccess) return fail_hip(e, "workspace");
+    e = launch_q4_apply(w, X, ldx, Y, ldy, batch, prec, yprec, ws, st);
+    return e == hipSuccess ? LRC_OK : fail_hip(e, "4-bit apply launch");
+} LRC_NO_EXCEPTION
+
+int lrc_sample(const void* logits, int64_t ld, int64_t rows, int64_t vocab, int prec, const float* u,
+               const float* temperature, const int64_t* top_k, const float* top_p, const float* min_p,
+               int64_t* tokens) try {
+    int rc = check_logits(logits, ld, rows, vocab, prec);
+    if (rc) return rc;
+    if (rows > 0 && (!u || !tokens)) return fail(LRC_EINVAL, "NULL array argument");
+    size_t lb;
+    span_bytes(rows, ld, vocab, elem_bytes(prec), &lb);
+    const size_t fb = (size_t)rows * 4;
+    if ((rc = check_out({tokens, (size_t)rows * 8, "tokens"},
+                        {{logits, lb, "logits"}, {u, fb, "u"}, {temperature, fb, "temperature"}, {top_k, 2 * fb, "top_k"},
+                         {top_p, fb, "top_p"}, {min_p, fb, "min_p"}})))
+        return rc;
+    if (rows == 0) return LRC_OK;
+    int dev;
+    rc = current_device(&dev, nullptr);
+    if (rc) return rc;
+    hipStream_t st = g_stream;
+    const SampleArgs a{logits, rows, vocab, ld, prec, u, temperature, top_p, min_p, top_k, tokens};
+    Workspace& ws = workspace_for(dev, st);
+    ws.reset();
+    const size_t bytes = sample_workspace_bytes(a);
+    hipError_t e = bytes ? ws.reserve(bytes, st) : hipSuccess;
+    if (e != hipSuccess) return fail_hip(e, "workspace");
+    e = launch_sample(a, ws, st);
+    return e == hipSuccess ? LRC_OK : fail_hip(e, "sampling launch");
+} LRC_NO_EXCEPTION
+
+static int check_distill(const void* logits, int64_t ld, int64_t rows, int64_t vocab, int prec, const int64_t* ids,
+                         const void* top, int64_t K, int tprec, double temperature, const void* grad, int64_t ldg) {
+    int rc = check_logits(logits, ld, rows, vocab, prec);
+    if (rc) return rc;
+    if (rows > 0 && (!ids || !top)) return fail(LRC_EINVAL, "NULL array argument");
+    if (K < 1 || K > LRC_DISTILL_MAX_TOP)
+        return fail(LRC_EINVAL, "K = %lld outside [1, %d]", (long long)K, LRC_DISTILL_MAX_TOP);
+    if (!head_prec(tprec)) return fail(LRC_EINVAL, "unknown precision code %d of the teacher's logits", tprec);
+    const float T = (float)temperature;
+    if (!(T >= 1.17549435e-38f && T <= 3.4028234663852886e38f))
+        return fail(LRC_EINVAL, "temperature %g is not a positive finite number", temperature);
+    size_t t;
+    if (grad && ldg < vocab) return fail(LRC_EINVAL, "pitch %lld below vocab = %lld", (long long)ldg, (long long)vocab);
+    if (grad && !span_bytes(rows, ldg, vocab, elem_bytes(prec), &t))
+        return fail(LRC_EOVERFLOW, "array sizes overflow int64");
+    return LRC_OK;
+}
+
+// The gradient may be the logits themselves, and overlaps nothing else.
+static int check_distill_out(const Span& out, bool alias, const void* logits, int64_t ld, int64_t rows, int64_t vocab,
+                             int prec, const int64_t* ids, const void* top, int64_t K, int tprec,
+                             const float* teacher_lse, const float* weight) {
+    size_t lb;
+    span_bytes(rows, ld, vocab, elem_bytes(prec), &lb);
+    const size_t slots = (size_t)rows * K;
+    return check_out(out, {{alias ? nullptr : logits, lb, "logits"}, {ids, slots * 8, "ids"},
+                           {top, slots * elem_bytes(tprec), "top"}, {teacher_lse, (size_t)rows * 4, "teacher_lse"},
+                           {weight, (size_t)rows * 4, "weight"}});
+}
+
+int lrc_distill(const void* logits, int64_t ld, int64_t rows, int64_t vocab, int prec, const int64_t* ids,
+                const void* top, int64_t K, int tprec, const float* teacher_lse, const float* weight,
+                double temperature, float* loss, float* stats, void* grad, int64_t ldg) try {
+    int rc = check_distill(logits, ld, rows, vocab, prec, ids, top, K, tprec, temperature, grad, ldg);
+    if (rc) return rc;
+    if (rows > 0 && !loss) return fail(LRC_EINVAL, "NULL array argument");
+    size_t gb = 0;
+    if (grad) span_bytes(rows, ldg, vocab, elem_bytes(prec), &gb);
+    const Span outs[3] = {{loss, (size_t)rows * 4, "loss"}, {stats, (size_t)rows * 16, "stats"}, {grad, gb, "grad"}};
+    for (const Span& o : outs)
+        if ((rc = check_distill_out(o, o.p == grad && grad == logits && ldg == ld, logits, ld, rows, vocab, prec, ids, top,
+                                    K, tprec, teacher_lse, weight)))
+            return rc;
+    if ((rc = check_out(outs[0], {outs[1], outs[2]})) || (rc = check_out(outs[1], {outs[2]}))) return rc;
+    if (rows == 0) return LRC_OK;
+    int dev;
+    rc = current_device(&dev, nullptr);
+    if (rc) return rc;
+    const DistillArgs a{logits, rows, vocab, ld, prec, ids, top, K, tprec, teacher_lse, weight, (float)temperature};
+    hipError_t e = launch_distill(a, loss, stats, grad, ldg, g_stream);
+    return e == hipSuccess ? LRC_OK : fail_hip(e, "distillation launch");
+} LRC_NO_EXCEPTION
+
+int lrc_distill_backward(const void* logits, int64_t ld, int64_t rows, int64_t vocab, int prec, const int64_t* ids,
+                         const void* top, int64_t K, int tprec, const float* teacher_lse, const float* weight,
+                         double temperature, const float* stats, const float* dloss, void* grad, int64_t ldg) try {
+    if (rows > 0 && (!stats || !grad)) return fail(LRC_EINVAL, "NULL array argument");
+    int rc = check_distill(logits, ld, rows, vocab, prec, ids, top, K, tprec, temperature, grad, ldg);
+    if (rc) return rc;
+    size_t gb = 0;
+    if (grad) span_bytes(rows, ldg, vocab, elem_bytes(prec), &gb);
+    const Span g{grad, gb, "grad"};
+    if ((rc = check_distill_out(g, grad == logits && ldg == ld, logits, ld, rows, vocab, prec, ids, top, K, tprec,
+                                teacher_lse, weight)) ||
+        (rc = check_out(g, {{stats, (size_t)rows * 16, "stats"}, {dloss, (size_t)rows * 4, "dloss"}})))
+        return rc;
+    if (rows == 0) return LRC_OK;
+    int dev;
+    rc = current_device(&dev, nullptr);
+    if (rc) return rc;
+    const DistillArgs a{logits, rows, vocab, ld, prec, ids, top, K, tprec, teacher_lse, weight, (float)temperature};
+    hipError_t e = launch_distill_backward(a, stats, dloss, grad, ldg, g_stream);
+    return e == hipSuccess ? LRC_OK : fail_hip(e, "distillation gradient launch");
+} LRC_NO_EXCEPTION
 
 }  // extern "C"
 

@@ -10,7 +10,7 @@
 
 namespace lrc {
 
-enum Prec { P64 = 0, P32 = 1, P16 = 2 };
+enum Prec { P64 = 0, P32 = 1, P16 = 2, PB16 = 3 };
 
 inline int elem_bytes(int prec) { return prec == P64 ? 8 : (prec == P32 ? 4 : 2); }
 inline int mfma_kb(int prec) { return prec == P16 ? 32 : 4; }
@@ -204,6 +204,55 @@ hipError_t launch_sumsq5(const double* T, const double* a, const double* b, cons
 // nsums x count, row-major) into out[nsums] (device).
 hipError_t launch_reduce_rows(const double* part, int64_t count, int nsums, double* out,
                               hipStream_t stream);
+
+// ------------------------------------------------------------ output head
+// 4-bit weights: rows of E2M1 codes, two a byte, padded to whole 16 bytes, and
+// one scale per `group` (a power of two, 32 to 512) weights of a row.
+inline int64_t q4_row_bytes(int64_t n) { return (n + 31) / 32 * 16; }
+struct Q4Weights {
+    const void* codes;
+    const void* scales;
+    int64_t m, n, group;
+    int sprec;
+    const void *U, *s, *V;   // rank-k compensation in fprec, or k = 0
+    int64_t k;
+    int fprec;
+};
+// values (prec, m x n with pitch n) and nbad (zeroed first) may be null
+hipError_t launch_q4_quantize(const void* W, int64_t ldw, int prec, int64_t m, int64_t n, int64_t group, void* codes,
+                              void* scales, int sprec, void* values, unsigned long long* nbad, hipStream_t stream);
+size_t q4_apply_workspace_bytes(const Q4Weights& w, int64_t batch, int prec);
+hipError_t launch_q4_apply(const Q4Weights& w, const void* X, int64_t ldx, void* Y, int64_t ldy, int64_t batch,
+                           int prec, int yprec, Workspace& ws, hipStream_t stream);
+
+// Sampling: per-row parameters on the device, each may be null (off).
+struct SampleArgs {
+    const void* logits;
+    int64_t rows, vocab, ld;
+    int prec;
+    const float *u, *temperature, *top_p, *min_p;
+    const int64_t* top_k;
+    int64_t* tokens;
+};
+size_t sample_workspace_bytes(const SampleArgs& a);
+hipError_t launch_sample(const SampleArgs& a, Workspace& ws, hipStream_t stream);
+
+// Distillation: loss (rows), stats (rows x 4) and grad may be null.
+struct DistillArgs {
+    const void* logits;
+    int64_t rows, vocab, ld;
+    int prec;
+    const int64_t* ids;
+    const void* top;
+    int64_t K;
+    int tprec;
+    const float *teacher_lse, *weight;
+    float temperature;
+};
+hipError_t launch_distill(const DistillArgs& a, float* loss, float* stats, void* grad, int64_t ldg,
+                          hipStream_t stream);
+hipError_t launch_distill_backward(const DistillArgs& a, const float* stats, const float* dloss, void* grad,
+                                   int64_t ldg, hipStream_t stream);
 
 // ------------------------------------------------------------------- TT ---
 constexpr int kMaxD = 16;

@@ -7,7 +7,7 @@ HIP kernels.  There is no CPU fallback: if the library is missing this
 module raises on first use.
 
 Precision follows the tensors' dtype: float64 -> FP64, float32 -> FP32,
-float16 -> FP16 (FP32 accumulation).
+float16 -> FP16 (FP32 accumulation); the output-head calls also take bfloat16.
 """
 from __future__ import annotations
 
@@ -21,7 +21,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("LRC_LIBRARY") or os.path.join(HERE, "liblrc.so")
 HEADER = os.path.join(os.path.dirname(HERE), "include", "lrc.h")
 
-FP64, FP32, FP16 = 0, 1, 2
+FP64, FP32, FP16, BF16 = 0, 1, 2, 3
 PATH_AUTO, PATH_STREAM, PATH_MFMA = 0, 1, 2
 CERT_MATRIX, CERT_TT = 0, 1
 ERRORS = {-1: "EINVAL", -2: "EOVERFLOW", -3: "EHIP", -4: "ENOMEM", -5: "ENODEV", -6: "ENUMERIC"}
@@ -114,6 +114,23 @@ def lib():
     L.lrc_tt_rsvd.argtypes = [_vp, ctypes.POINTER(_i64), ctypes.POINTER(_i64), ctypes.c_int, ctypes.POINTER(_vp),
                               ctypes.POINTER(_i64), ctypes.c_int, ctypes.POINTER(_vp), _vp]
     L.lrc_tt_rsvd.restype = ctypes.c_int
+    L.lrc_q4_row_bytes.argtypes = [_i64]
+    L.lrc_q4_row_bytes.restype = _i64
+    L.lrc_q4_storage_bytes.argtypes = [_i64, _i64, _i64, ctypes.c_int]
+    L.lrc_q4_storage_bytes.restype = _i64
+    L.lrc_q4_quantize.argtypes = [_vp, _i64, _i64, _i64, _i64, ctypes.c_int, _vp, _vp, ctypes.c_int, _vp,
+                                  ctypes.POINTER(_i64)]
+    L.lrc_q4_quantize.restype = ctypes.c_int
+    L.lrc_q4_apply.argtypes = [_vp, _vp, ctypes.c_int, _i64, _vp, _vp, _vp, _i64, ctypes.c_int, _vp, _i64, _vp, _i64,
+                               _i64, _i64, _i64, ctypes.c_int, ctypes.c_int]
+    L.lrc_q4_apply.restype = ctypes.c_int
+    L.lrc_sample.argtypes = [_vp, _i64, _i64, _i64, ctypes.c_int, _vp, _vp, _vp, _vp, _vp, _vp]
+    L.lrc_sample.restype = ctypes.c_int
+    distill = [_vp, _i64, _i64, _i64, ctypes.c_int, _vp, _vp, _i64, ctypes.c_int, _vp, _vp, ctypes.c_double]
+    L.lrc_distill.argtypes = distill + [_vp, _vp, _vp, _i64]
+    L.lrc_distill.restype = ctypes.c_int
+    L.lrc_distill_backward.argtypes = distill + [_vp, _vp, _vp, _i64]
+    L.lrc_distill_backward.restype = ctypes.c_int
     L.lrc_storage_bytes.argtypes = [_i64, _i64, _i64, ctypes.c_int]
     L.lrc_storage_bytes.restype = _i64
     L.lrc_tt_storage_bytes.argtypes = [ctypes.POINTER(_i64), ctypes.POINTER(_i64), ctypes.c_int, ctypes.c_int]
@@ -480,6 +497,258 @@ def tt_rsvd(T, ranks, omegas, power_iters: int = 0):
         sigmas.append(sig[o:o + r])
         o += r
     return cores, sigmas
+
+
+# ---- compressed output head ----
+
+_head_dtypes = None
+
+
+def _head_prec(dtype) -> int:
+    """FP32, FP16 or BF16 of an activation, logit, scale or factor dtype."""
+    global _head_dtypes
+    if _head_dtypes is None:
+        import torch
+        _head_dtypes = {torch.float32: FP32, torch.float16: FP16, torch.bfloat16: BF16}
+    p = _head_dtypes.get(dtype)
+    if p is None:
+        raise TypeError(f"unsupported dtype {dtype}")
+    return p
+
+
+def _rows(t, name):
+    """Pitch of a matrix whose rows are contiguous."""
+    shape, (ld, step) = t.shape, t.stride()
+    if step != 1 and shape[1] > 1:
+        raise ValueError(f"the rows of {name} must be contiguous")
+    return ld if shape[0] > 1 else max(ld, shape[1])
+
+
+def _on(dev, **ts):
+    """Every given tensor lives on the device `dev`, a GPU."""
+    if dev.type != "cuda":
+        raise ValueError("tensors must be on the GPU")
+    for name, t in ts.items():
+        if t is not None and t.device != dev:
+            raise ValueError(f"{name} is on {t.device}, the others on {dev}")
+
+
+def q4_row_bytes(n: int) -> int:
+    return _check(lib().lrc_q4_row_bytes(n))
+
+
+def q4_storage_bytes(m: int, n: int, group: int, scale_prec) -> int:
+    p = {"fp32": FP32, "fp16": FP16, "bf16": BF16}.get(scale_prec, scale_prec)
+    return _check(lib().lrc_q4_storage_bytes(m, n, group, p))
+
+
+def q4_quantize(W, group: int = 128, scale_dtype=None, values: bool = False, count_nonfinite: bool = False):
+    """4-bit weights of the matrix W (m x n, float64, float32, float16 or
+    bfloat16, contiguous rows): E2M1 codes (uint8, m x q4_row_bytes(n), two a
+    byte) and scales (m x ceil(n / group), float16 unless scale_dtype says
+    otherwise).  With values=True also the values they stand for, in W's
+    dtype; with count_nonfinite=True also the number of groups that hold a
+    NaN or an infinity or whose scale overflows (this waits for the result)."""
+    import torch
+    _need(W.dim() == 2, "W must be a matrix")
+    prec = FP64 if W.dtype == torch.float64 else _head_prec(W.dtype)
+    scale_dtype = scale_dtype or torch.float16
+    sprec = _head_prec(scale_dtype)
+    _need(group in (32, 64, 128, 256, 512), "group must be 32, 64, 128, 256 or 512")
+    m, n = W.shape
+    ld = _rows(W, "W")
+    dev = W.device
+    _on(dev)
+    codes = torch.empty((m, (n + 31) // 32 * 16), dtype=torch.uint8, device=dev)
+    scales = torch.empty((m, -(-n // group)), dtype=scale_dtype, device=dev)
+    val = torch.empty((m, n), dtype=W.dtype, device=dev) if values else None
+    bad = _i64(0)
+    _bind_stream(dev)
+    _check(lib().lrc_q4_quantize(W.data_ptr(), ld, m, n, group, prec, codes.data_ptr(), scales.data_ptr(), sprec,
+                                 val.data_ptr() if values else None,
+                                 ctypes.byref(bad) if count_nonfinite else None))
+    out = (codes, scales) + ((val,) if values else ()) + ((int(bad.value),) if count_nonfinite else ())
+    return out
+
+
+def q4_apply(codes, scales, X, group: int = 128, factors=None, out_dtype=None, Y=None):
+    """Y = X W^T + [(X V) diag(s)] U^T: X (batch x n, float32, float16 or
+    bfloat16, contiguous rows), W the m x n weights of `codes` and `scales`
+    (q4_quantize), factors = (U, s, V) a rank-k compensation (U m x k, s k,
+    V n x k, one dtype) or None.  Y (batch x m) is in out_dtype (X's unless
+    given); a caller-supplied Y sets it."""
+    _need(X.dim() == 2 and codes.dim() == 2 and scales.dim() == 2, "X, codes and scales must be matrices")
+    b, n = X.shape
+    m = codes.shape[0]
+    if codes.dtype != _uint8():
+        raise TypeError(f"codes have dtype {codes.dtype}, want uint8")
+    if codes.shape[1] != (n + 31) // 32 * 16 or scales.shape != (m, -(-n // group)):
+        raise ValueError(f"shape mismatch: codes {tuple(codes.shape)} (want {(m, (n + 31) // 32 * 16)}), "
+                         f"scales {tuple(scales.shape)} (want {(m, -(-n // group))})")
+    prec, sprec = _head_prec(X.dtype), _head_prec(scales.dtype)
+    ldx = _rows(X, "X")
+    k, fprec, ptrs = 0, 0, (None, None, None)
+    dev = X.device
+    if factors is not None:
+        U, s, V = factors
+        k = s.shape[0]
+        if U.shape != (m, k) or V.shape != (n, k) or s.dim() != 1:
+            raise ValueError(f"shape mismatch: U {tuple(U.shape)}, s {tuple(s.shape)}, V {tuple(V.shape)}")
+        fprec = _head_prec(s.dtype)
+        if U.dtype != s.dtype or V.dtype != s.dtype:
+            raise TypeError("U, s and V must share one dtype")
+        _dev(U, s, V)
+        _on(dev, U=U, s=s, V=V)
+        ptrs = (U.data_ptr(), s.data_ptr(), V.data_ptr())
+    if Y is not None:
+        _need(tuple(Y.shape) == (b, m), f"Y has shape {tuple(Y.shape)}, want {(b, m)}")
+        _need(out_dtype is None or Y.dtype == out_dtype, f"Y has dtype {Y.dtype}, want {out_dtype}")
+        ldy = _rows(Y, "Y")
+        yprec = _head_prec(Y.dtype)
+    else:
+        yprec = prec if out_dtype is None else _head_prec(out_dtype)
+    _dev(codes, scales)
+    _on(dev, codes=codes, scales=scales, Y=Y)
+    if Y is None:
+        Y, ldy = _empty((b, m), out_dtype or X.dtype, dev), m
+    _bind_stream(dev)
+    rc = lib().lrc_q4_apply(codes.data_ptr(), scales.data_ptr(), sprec, group, *ptrs, k, fprec, X.data_ptr(), ldx,
+                            Y.data_ptr(), ldy, m, n, b, prec, yprec)
+    if rc < 0:
+        _check(rc)
+    return Y
+
+
+def _empty(shape, dtype, device):
+    import torch
+    return torch.empty(shape, dtype=dtype, device=device)
+
+
+_whole = None
+
+
+def _uint8():
+    return _whole_dtypes()[0]
+
+
+def _whole_dtypes():
+    """(uint8, int64, float32), looked up once."""
+    global _whole
+    if _whole is None:
+        import torch
+        _whole = (torch.uint8, torch.int64, torch.float32)
+    return _whole
+
+
+def _row_values(t, name, rows, dtype):
+    """Pointer of one value per row, or None."""
+    if t is None:
+        return None
+    if t.dtype != dtype:
+        raise TypeError(f"{name} has dtype {t.dtype}, want {dtype}")
+    if t.shape != (rows,) or not t.is_contiguous():
+        raise ValueError(f"{name} must hold one contiguous value per row ({rows})")
+    return t.data_ptr()
+
+
+def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, out=None):
+    """One token index (int64) per row of logits (rows x vocab, float32,
+    float16 or bfloat16, contiguous rows) from the uniform numbers u (float32,
+    one per row).  temperature, top_p, min_p (float32) and top_k (int64) hold
+    one value per row, or None: 1 and filters that are off.  A temperature
+    that is not above 0 takes the largest logit; a row whose logits are all
+    -infinity gives -1."""
+    _need(logits.dim() == 2, "logits must be a matrix")
+    rows, vocab = logits.shape
+    prec = _head_prec(logits.dtype)
+    ld = _rows(logits, "logits")
+    _, i64, f32 = _whole_dtypes()
+    pu = _row_values(u, "u", rows, f32)
+    pt = _row_values(temperature, "temperature", rows, f32)
+    pk = _row_values(top_k, "top_k", rows, i64)
+    pp = _row_values(top_p, "top_p", rows, f32)
+    pm = _row_values(min_p, "min_p", rows, f32)
+    dev = logits.device
+    _on(dev, u=u, temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p, out=out)
+    if out is None:
+        out = _empty((rows,), i64, dev)
+    po = _row_values(out, "out", rows, i64)
+    _bind_stream(dev)
+    rc = lib().lrc_sample(logits.data_ptr(), ld, rows, vocab, prec, pu, pt, pk, pp, pm, po)
+    if rc < 0:
+        _check(rc)
+    return out
+
+
+def _distill_args(logits, ids, top_logits, temperature, teacher_lse, weight):
+    _need(logits.dim() == 2 and ids.dim() == 2, "logits, ids and top_logits must be matrices")
+    rows, vocab = logits.shape
+    _, i64, f32 = _whole_dtypes()
+    if ids.dtype != i64:
+        raise TypeError(f"ids have dtype {ids.dtype}, want {i64}")
+    if ids.shape[0] != rows or top_logits.shape != ids.shape:
+        raise ValueError(f"shape mismatch: ids {tuple(ids.shape)}, top_logits {tuple(top_logits.shape)}, {rows} rows")
+    prec, tprec = _head_prec(logits.dtype), _head_prec(top_logits.dtype)
+    lse = _row_values(teacher_lse, "teacher_lse", rows, f32)
+    w = _row_values(weight, "weight", rows, f32)
+    ld = _rows(logits, "logits")
+    _dev(ids, top_logits)
+    _on(logits.device, ids=ids, top_logits=top_logits, teacher_lse=teacher_lse, weight=weight)
+    return (logits.data_ptr(), ld, rows, vocab, prec, ids.data_ptr(), top_logits.data_ptr(), ids.shape[1], tprec, lse, w,
+            float(temperature))
+
+
+def _grad_like(logits, grad):
+    if grad is None:
+        return _empty(tuple(logits.shape), logits.dtype, logits.device)
+    _need(grad.shape == logits.shape and grad.dtype == logits.dtype, "grad must have the logits' shape and dtype")
+    _on(logits.device, grad=grad)
+    return grad
+
+
+def distill(logits, ids, top_logits, temperature: float = 1.0, teacher_lse=None, weight=None, grad=None):
+    """Distillation loss of every row (float32) and the gradient of their sum
+    by the student's logits, in one pass: logits rows x vocab (float32,
+    float16 or bfloat16, contiguous rows), ids (int64) and top_logits rows x K
+    the teacher's named tokens (an id outside the vocabulary is an unused
+    slot).  Without teacher_lse the teacher is renormalized over them; with it
+    (float32, log-sum-exp of the teacher's logits / temperature) the rest of
+    both distributions is one more class.  weight (float32) scales each row's
+    loss; rows of weight 0 are not read.  grad may be the logits themselves."""
+    args = _distill_args(logits, ids, top_logits, temperature, teacher_lse, weight)
+    g = _grad_like(logits, grad)
+    loss = _empty((args[2],), _whole_dtypes()[2], logits.device)
+    _bind_stream(logits.device)
+    _check(lib().lrc_distill(*args, loss.data_ptr(), None, g.data_ptr(), _rows(g, "grad")))
+    return loss, g
+
+
+def distill_forward(logits, ids, top_logits, temperature: float = 1.0, teacher_lse=None, weight=None):
+    """The loss of distill alone, and the statistics (rows x 4, float32) that
+    distill_backward takes."""
+    args = _distill_args(logits, ids, top_logits, temperature, teacher_lse, weight)
+    f32 = _whole_dtypes()[2]
+    loss, stats = _empty((args[2],), f32, logits.device), _empty((args[2], 4), f32, logits.device)
+    _bind_stream(logits.device)
+    _check(lib().lrc_distill(*args, loss.data_ptr(), stats.data_ptr(), None, 0))
+    return loss, stats
+
+
+def distill_backward(logits, ids, top_logits, stats, dloss=None, temperature: float = 1.0, teacher_lse=None, weight=None,
+                     grad=None):
+    """Gradient of sum_i dloss_i loss_i by the logits, from the same inputs as
+    distill_forward and the statistics that it gave (dloss float32, one per
+    row, or None: 1).  grad may be the logits themselves."""
+    args = _distill_args(logits, ids, top_logits, temperature, teacher_lse, weight)
+    f32 = _whole_dtypes()[2]
+    _need(stats.shape == (args[2], 4) and stats.dtype == f32, "stats must be float32, rows x 4")
+    up = _row_values(dloss, "dloss", args[2], f32)
+    _dev(stats)
+    _on(logits.device, stats=stats, dloss=dloss)
+    g = _grad_like(logits, grad)
+    _bind_stream(logits.device)
+    _check(lib().lrc_distill_backward(*args, stats.data_ptr(), up, g.data_ptr(), _rows(g, "grad")))
+    return g
 
 
 def _result(res: CertResult) -> dict:
