@@ -977,7 +977,7 @@ int lrc_q4_apply(const void* codes, const void* scales, int sprec, int64_t group
     const Q4Weights w{codes, scales, m, n, group, sprec, U, s, V, k, fprec};
     Workspace& ws = workspace_for(dev, st);
     ws.reset();
-    const size_t bytes = q4_apply_workspace_bytes(w, batch, prec);
+    const size_t bytes = q4_apply_workspace_bytes(w, X, ldx, batch, prec);
     hipError_t e = bytes ? ws.reserve(bytes, st) : hipSuccess;
     if (e != hipSuccess) return fail_hip(e, "workspace");
     e = launch_q4_apply(w, X, ldx, Y, ldy, batch, prec, yprec, ws, st);

@@ -221,7 +221,7 @@ struct Q4Weights {
 // values (prec, m x n with pitch n) and nbad (zeroed first) may be null
 hipError_t launch_q4_quantize(const void* W, int64_t ldw, int prec, int64_t m, int64_t n, int64_t group, void* codes,
                               void* scales, int sprec, void* values, unsigned long long* nbad, hipStream_t stream);
-size_t q4_apply_workspace_bytes(const Q4Weights& w, int64_t batch, int prec);
+size_t q4_apply_workspace_bytes(const Q4Weights& w, const void* X, int64_t ldx, int64_t batch, int prec);
 hipError_t launch_q4_apply(const Q4Weights& w, const void* X, int64_t ldx, void* Y, int64_t ldy, int64_t batch,
                            int prec, int yprec, Workspace& ws, hipStream_t stream);
 

@@ -164,21 +164,26 @@ struct Q4Args {
     int64_t rb, G;
     int sprec, gshift;
     const void* U;
-    const float* Tm;     // T' [batch][k]
+    const float* Tm;      // T' [batch][k], or its `tsplits` partial sums without the factor s
+    int tsplits;
+    const void* s;
     int64_t k;
     int fprec;
     const void* X;
-    int64_t ldx;
+    int64_t ldx, plane;   // k_q4_tile: 16-bit planes, `plane` elements apart
     void* Y;
     int64_t ldy;
     int yprec;
     int64_t m, n, b;
+    float* part;          // k_q4_tile: partial sums [split][batch][m], or null
+    int splits;
 };
 
 // Activations as MFMA operands: P planes of 8 values.
 template <typename T> struct ActTraits;
 template <> struct ActTraits<half_t> {
     static constexpr int P = 1;
+    using plane_t = half_t;
     using frag = half8_t;
     static __device__ __forceinline__ float4_t mfma(frag a, frag b, float4_t c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
@@ -193,6 +198,7 @@ template <> struct ActTraits<half_t> {
 };
 template <> struct ActTraits<bhalf_t> {
     static constexpr int P = 1;
+    using plane_t = bhalf_t;
     using frag = bhalf8_t;
     static __device__ __forceinline__ float4_t mfma(frag a, frag b, float4_t c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
@@ -209,50 +215,56 @@ template <> struct ActTraits<float> : ActTraits<bhalf_t> {
     static constexpr int P = 3;
 };
 
-// x = h + m + l exactly, each with 8 significant bits; an infinity keeps its
-// sign in h alone, NaN stays NaN.
-__device__ __forceinline__ void split3(float x, unsigned short (&p)[3]) {
+// x = h + m + l exactly, each with 8 significant bits, as bits of bfloat16; an
+// infinity keeps its sign in h alone, NaN stays NaN.
+__device__ __forceinline__ void split3(float x, unsigned (&p)[3]) {
     const unsigned ux = __float_as_uint(x);
-    unsigned hi = ux & 0xFFFF0000u;
-    float r = x - __uint_as_float(hi);
-    if ((ux & 0x7FFFFFFFu) == 0x7F800000u) r = 0.0f;
-    if (x != x) hi = 0x7FC00000u;
+    const bool special = (ux & 0x7F800000u) == 0x7F800000u;
+    const float r = special ? 0.0f : x - __uint_as_float(ux & 0xFFFF0000u);
     const unsigned um = __float_as_uint(r);
-    const float l = (r != r) ? 0.0f : r - __uint_as_float(um & 0xFFFF0000u);
-    p[0] = (unsigned short)(hi >> 16);
-    p[1] = (unsigned short)((r != r) ? 0u : um >> 16);
-    p[2] = (unsigned short)(__float_as_uint(l) >> 16);
+    p[0] = x != x ? 0x7FC0u : ux >> 16;
+    p[1] = um >> 16;
+    p[2] = __float_as_uint(r - __uint_as_float(um & 0xFFFF0000u)) >> 16;
 }
 
 // The 8 values x[j .. j + 8) of one row of n as MFMA operands; zero past n.
-template <typename T, bool VEC>
-__device__ __forceinline__ void load_act(const T* x, int64_t j, int64_t n, typename ActTraits<T>::frag (&f)[ActTraits<T>::P]) {
-    T v[8];
-    if (VEC && j + 8 <= n) {
-        typedef T vec_t __attribute__((ext_vector_type(16 / sizeof(T))));
+template <typename T>
+__device__ __forceinline__ void load_act(const T* x, int64_t j, int64_t n,
+                                         typename ActTraits<T>::frag (&f)[ActTraits<T>::P]) {
+    uint4v_t v[sizeof(T) / 2];
+    if (j + 8 <= n) {
 #pragma unroll
-        for (int h = 0; h < (int)(8 * sizeof(T) / 16); ++h) {
-            const vec_t w = reinterpret_cast<const vec_t*>(x + j)[h];
-#pragma unroll
-            for (int q = 0; q < (int)(16 / sizeof(T)); ++q) v[h * (16 / sizeof(T)) + q] = w[q];
-        }
+        for (int h = 0; h < (int)sizeof(T) / 2; ++h) v[h] = load16(x + j + h * kVec<T>);
     } else {
 #pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] = j + q < n ? x[j + q] : (T)0.0f;
+        for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
+            v[h] = uint4v_t{0, 0, 0, 0};
+#pragma unroll
+            for (int e = 0; e < kVec<T>; ++e) {
+                const int64_t q = j + h * kVec<T> + e;
+                if (q < n) {
+                    unsigned b;
+                    if constexpr (sizeof(T) == 4) b = __builtin_bit_cast(unsigned, x[q]);
+                    else b = __builtin_bit_cast(unsigned short, x[q]);
+                    set_bits<T>(v[h], e, b);
+                }
+            }
+        }
     }
     if constexpr (sizeof(T) == 4) {
-        unsigned short s[3][8];
+        uint4v_t o[3];
 #pragma unroll
-        for (int q = 0; q < 8; ++q) {
-            unsigned short p[3];
-            split3(v[q], p);
+        for (int q = 0; q < 4; ++q) {
+            unsigned lo[3], hi[3];
+            split3(elem<float>(v[q >> 1], 2 * (q & 1)), lo);
+            split3(elem<float>(v[q >> 1], 2 * (q & 1) + 1), hi);
 #pragma unroll
-            for (int t = 0; t < 3; ++t) s[t][q] = p[t];
+            for (int t = 0; t < 3; ++t) o[t][q] = lo[t] | hi[t] << 16;
         }
 #pragma unroll
-        for (int t = 0; t < 3; ++t) f[t] = __builtin_bit_cast(bhalf8_t, s[t]);
+        for (int t = 0; t < 3; ++t) f[t] = __builtin_bit_cast(bhalf8_t, o[t]);
     } else {
-        f[0] = __builtin_bit_cast(typename ActTraits<T>::frag, v);
+        f[0] = __builtin_bit_cast(typename ActTraits<T>::frag, v[0]);
     }
 }
 
@@ -269,75 +281,123 @@ __device__ __forceinline__ void transpose4(unsigned (&w)[4]) {
     w[3] = d[1];
 }
 
-// One workgroup of 4 waves: 16 RT rows of W for 16 NB rows of X; the waves
-// split the columns in steps of 128 and add up through LDS in a fixed order.
-template <typename T, int NB, int RT, bool VEC>
-__global__ __launch_bounds__(256) void k_q4_rows(Q4Args a) {
+// Adds T' U^T, 16 ranks at a time from rank q0 in steps of `step`, to FA x FB
+// result blocks: tok[a] are the batch rows, row[b] the rows of U of this lane's
+// operand in each block.
+template <int FA, int FB, typename F>
+__device__ __forceinline__ void add_ranks(const Q4Args& a, const int64_t (&tok)[FA], const int64_t (&row)[FB],
+                                          int64_t q0, int64_t step, F&& tm, float4_t (&acc)[FB][FA]) {
+    const int lg = (threadIdx.x & 63) >> 4;
+    for (int64_t q = q0; q < a.k; q += step) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const int64_t c = q + lg * 4 + t;
+            float tv[FA], uv[FB];
+#pragma unroll
+            for (int f = 0; f < FA; ++f) tv[f] = c < a.k ? tm(tok[f], c) : 0.0f;
+#pragma unroll
+            for (int r = 0; r < FB; ++r) uv[r] = c < a.k ? load_as_f32(a.U, row[r] * a.k + c, a.fprec) : 0.0f;
+#pragma unroll
+            for (int r = 0; r < FB; ++r)
+#pragma unroll
+                for (int f = 0; f < FA; ++f) acc[r][f] = mfma(tv[f], uv[r], acc[r][f]);
+        }
+    }
+}
+
+// ---- few rows: the weights' bytes bound it --------------------------------
+// One workgroup of NW waves: 16 RT rows of W for 16 NB rows of X.  The waves
+// take steps of 128 columns in turn (so a workgroup streams whole rows) and add
+// up through LDS in a fixed order; codes, scales and activations of the next
+// step are on their way during this one.  FL: MFMAs (32 columns) per scale group,
+// 4 for groups of 128 and more, whose words then need no transpose.
+template <typename T, int NB, int RT, int FL>
+struct RowStep {
     using Tr = ActTraits<T>;
-    __shared__ float red[4][16 * NB][16 * RT + 1];
+    uint4v_t w[RT];
+    float sc[RT][4 / FL];
+    typename Tr::frag x[NB][4][Tr::P];
+};
+
+template <typename T, int NB, int RT, int FL, int NW>
+__global__ __launch_bounds__(64 * NW) void k_q4_rows(Q4Args a) {
+    using Tr = ActTraits<T>;
+    __shared__ float red[NW][16 * NB][16 * RT + 1];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int lr = lane & 15, lg = lane >> 4;
     const int64_t i0 = (int64_t)blockIdx.x * 16 * RT, b0 = (int64_t)blockIdx.y * 16 * NB;
-    int64_t row[RT];
+    int64_t row[RT], tok[NB];
 #pragma unroll
     for (int r = 0; r < RT; ++r) row[r] = std::min(i0 + 16 * r + lr, a.m - 1);
-    const T* x[NB];
 #pragma unroll
-    for (int f = 0; f < NB; ++f) x[f] = static_cast<const T*>(a.X) + std::min(b0 + 16 * f + lr, a.b - 1) * a.ldx;
+    for (int f = 0; f < NB; ++f) tok[f] = std::min(b0 + 16 * f + lr, a.b - 1);
     float4_t acc[RT][NB];
 #pragma unroll
     for (int r = 0; r < RT; ++r)
 #pragma unroll
         for (int f = 0; f < NB; ++f) acc[r][f] = zero_accv<float4_t>();
+
     const int64_t blocks = (a.n + 127) / 128;
-    for (int64_t kb = wave; kb < blocks; kb += 4) {
-        unsigned w[RT][4];
+    auto load = [&](RowStep<T, NB, RT, FL>& st, int64_t kb) {
         const int64_t off = kb * 64 + lg * 16;
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
-            uint4v_t c = {0, 0, 0, 0};
-            if (off < a.rb) c = *reinterpret_cast<const uint4v_t*>(a.codes + row[r] * a.rb + off);
+            st.w[r] = uint4v_t{0, 0, 0, 0};
+            if (off < a.rb) st.w[r] = __builtin_nontemporal_load(reinterpret_cast<const uint4v_t*>(a.codes + row[r] * a.rb + off));
 #pragma unroll
-            for (int t = 0; t < 4; ++t) w[r][t] = c[t];
-            transpose4(w[r]);
+            for (int q = 0; q < 4 / FL; ++q) {
+                const int64_t j = std::min(kb * 128 + q * 32 * FL, a.n - 1);
+                st.sc[r][q] = load_as_f32(a.scales, row[r] * a.G + (j >> a.gshift), a.sprec);
+            }
         }
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const int64_t j = kb * 128 + t * 32;
-            if (j >= a.n) break;
-            typename Tr::frag xa[NB][Tr::P];
+        for (int f = 0; f < NB; ++f)
 #pragma unroll
-            for (int f = 0; f < NB; ++f) load_act<T, VEC>(x[f], j + lg * 8, a.n, xa[f]);
+            for (int t = 0; t < 4; ++t)
+                load_act<T>(static_cast<const T*>(a.X) + tok[f] * a.ldx, kb * 128 + (FL == 4 ? lg * 32 + t * 8 : t * 32 + lg * 8),
+                            a.n, st.x[f][t]);
+    };
+    auto multiply = [&](RowStep<T, NB, RT, FL>& st) {
 #pragma unroll
-            for (int r = 0; r < RT; ++r) {
-                const float sc = load_as_f32(a.scales, row[r] * a.G + (j >> a.gshift), a.sprec);
-                const typename Tr::frag wf = Tr::widen(w[r][t]);
+        for (int r = 0; r < RT; ++r) {
+            unsigned w[4] = {st.w[r][0], st.w[r][1], st.w[r][2], st.w[r][3]};
+            if (FL != 4) transpose4(w);
+            float4_t d[NB];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                const typename Tr::frag wf = Tr::widen(w[t]);
 #pragma unroll
                 for (int f = 0; f < NB; ++f) {
-                    float4_t d = zero_accv<float4_t>();
+                    if (t % FL == 0) d[f] = zero_accv<float4_t>();
 #pragma unroll
-                    for (int p = Tr::P - 1; p >= 0; --p) d = Tr::mfma(xa[f][p], wf, d);
+                    for (int p = Tr::P - 1; p >= 0; --p) d[f] = Tr::mfma(st.x[f][t][p], wf, d[f]);
+                    if (t % FL == FL - 1) {
 #pragma unroll
-                    for (int v = 0; v < 4; ++v) acc[r][f][v] += sc * d[v];
+                        for (int v = 0; v < 4; ++v) acc[r][f][v] += st.sc[r][t / FL] * d[f][v];
+                    }
                 }
             }
         }
-    }
-    // compensation: T' (rows of the batch) against U (rows of W), 16 ranks a step
-    for (int64_t q = wave * 16; q < a.k; q += 64) {
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const int64_t c = q + lg * 4 + t;
-            float tv[NB], uv[RT];
-#pragma unroll
-            for (int f = 0; f < NB; ++f) tv[f] = c < a.k ? a.Tm[std::min(b0 + 16 * f + lr, a.b - 1) * a.k + c] : 0.0f;
-#pragma unroll
-            for (int r = 0; r < RT; ++r) uv[r] = c < a.k ? load_as_f32(a.U, row[r] * a.k + c, a.fprec) : 0.0f;
-#pragma unroll
-            for (int r = 0; r < RT; ++r)
-#pragma unroll
-                for (int f = 0; f < NB; ++f) acc[r][f] = mfma(tv[f], uv[r], acc[r][f]);
+    };
+    RowStep<T, NB, RT, FL> s0, s1;
+    int64_t kb = wave;
+    if (kb < blocks) load(s0, kb);
+    for (; kb < blocks; kb += 2 * NW) {
+        if (kb + NW < blocks) load(s1, kb + NW);
+        multiply(s0);
+        if (kb + NW < blocks) {
+            if (kb + 2 * NW < blocks) load(s0, kb + 2 * NW);
+            multiply(s1);
         }
+    }
+    if (a.k) {
+        auto tm = [&](int64_t t, int64_t c) {
+            if (!a.tsplits) return a.Tm[t * a.k + c];
+            float x = 0.0f;
+            for (int q = 0; q < a.tsplits; ++q) x += a.Tm[(q * a.b + t) * a.k + c];
+            return x * load_as_f32(a.s, c, a.fprec);
+        };
+        add_ranks(a, tok, row, 16 * wave, 16 * NW, tm, acc);
     }
 #pragma unroll
     for (int r = 0; r < RT; ++r)
@@ -346,54 +406,275 @@ __global__ __launch_bounds__(256) void k_q4_rows(Q4Args a) {
 #pragma unroll
             for (int v = 0; v < 4; ++v) red[wave][16 * f + 4 * lg + v][16 * r + lr] = acc[r][f][v];
     __syncthreads();
-    for (int e = threadIdx.x; e < 256 * NB * RT; e += 256) {
+    for (int e = threadIdx.x; e < 256 * NB * RT; e += 64 * NW) {
         const int i = e % (16 * RT), f = e / (16 * RT);
         if (i0 + i < a.m && b0 + f < a.b) {
             float y = red[0][f][i];
-            y += red[1][f][i];
-            y += red[2][f][i];
-            y += red[3][f][i];
+#pragma unroll
+            for (int w = 1; w < NW; ++w) y += red[w][f][i];
             store_from_f32(a.Y, (b0 + f) * a.ldy + i0 + i, a.yprec, y);
         }
     }
 }
 
-// Partial sums of V^T x: part[split][batch][k], one wave per 16 ranks x 16
-// batch rows x split of the columns.
-template <typename T, bool VEC>
-__global__ __launch_bounds__(64) void k_q4_mid(const T* __restrict__ X, int64_t ldx, const void* __restrict__ V,
-                                               int fprec, int64_t n, int64_t k, int64_t b, int64_t chunk,
-                                               float* __restrict__ part) {
-    const int lane = threadIdx.x, lr = lane & 15, lg = lane >> 4;
-    const int64_t r0 = (int64_t)blockIdx.x * 16, b0 = (int64_t)blockIdx.y * 16, s = blockIdx.z;
-    const int64_t j0 = s * chunk, j1 = std::min(n, j0 + chunk);
-    const T* x = X + std::min(b0 + lr, b - 1) * ldx;
-    const int64_t r = std::min(r0 + lr, k - 1);
-    float4_t acc = zero_accv<float4_t>();
-    for (int64_t j = j0 + lg * 8; j - lg * 8 < j1; j += 32) {
-        float xv[8];
-        if (VEC && j + 8 <= j1) {
-            typedef T vec_t __attribute__((ext_vector_type(16 / sizeof(T))));
+// ---- many rows: bound by the matrix cores ----------------------------------
+// One workgroup of 4 waves: 128 rows of W for 16 NX WX rows of X, WX waves along
+// X and 4 / WX along W, a wave 16 NR x 16 NX results.  Steps of 128 columns: the
+// activations move straight into one of two LDS buffers (the other is being
+// multiplied), rows of 256 bytes with their 16-byte chunks XOR-swizzled by the
+// row on the global side; the codes go to registers and are widened there, once
+// for NX MFMAs.  X: 16-bit planes, 16-byte aligned rows, zero from n on to the
+// next multiple of 128.
+template <typename T, int WX, int NX, int FL>
+__global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) void k_q4_tile(Q4Args a, int tiles_m, int tiles_b) {
+    using Tr = ActTraits<T>;
+    using P16 = typename Tr::plane_t;
+    constexpr int P = Tr::P, NR = 2 * WX, BT = 16 * NX * WX;       // rows of X in a tile
+    constexpr int PLANE = BT * 128, BUF = P * PLANE;
+    __shared__ alignas(16) P16 S[2 * BUF];
+    const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wx = wave % WX, wr = wave / WX;
+    // an XCD's consecutive workgroups take 8 row tiles for one tile of X after another
+    const int64_t lt = xcd_tile((int64_t)tiles_m * tiles_b * a.splits);
+    if (lt >= (int64_t)tiles_m * tiles_b * a.splits) return;
+    const int64_t split = lt / ((int64_t)tiles_m * tiles_b), q = lt % ((int64_t)tiles_m * tiles_b);
+    const int64_t g = q / (8 * tiles_b), gs = std::min<int64_t>(8, tiles_m - 8 * g), in = q - g * 8 * tiles_b;
+    const int64_t i0 = (8 * g + in % gs) * 128, b0 = in / gs * BT;
+
+    int64_t row[NR], tok[NX];
 #pragma unroll
-            for (int h = 0; h < (int)(8 * sizeof(T) / 16); ++h) {
-                const vec_t w = reinterpret_cast<const vec_t*>(x + j)[h];
+    for (int r = 0; r < NR; ++r) row[r] = std::min(i0 + wr * 16 * NR + 16 * r + lr, a.m - 1);
 #pragma unroll
-                for (int q = 0; q < (int)(16 / sizeof(T)); ++q) xv[h * (16 / sizeof(T)) + q] = (float)w[q];
+    for (int f = 0; f < NX; ++f) tok[f] = std::min(b0 + wx * 16 * NX + 16 * f + lr, a.b - 1);
+    float4_t acc[NR][NX];
+#pragma unroll
+    for (int r = 0; r < NR; ++r)
+#pragma unroll
+        for (int f = 0; f < NX; ++f) acc[r][f] = zero_accv<float4_t>();
+
+    const int64_t blocks = (a.n + 127) / 128;
+    const int64_t k0 = blocks * split / a.splits, k1 = blocks * (split + 1) / a.splits;
+    // wave w moves rows [w BT / 4, (w + 1) BT / 4) of every plane, 4 rows a load
+    const P16* xs[BT / 16];
+#pragma unroll
+    for (int h = 0; h < BT / 16; ++h) {
+        const int r = wave * (BT / 4) + 4 * h + lg;
+        xs[h] = static_cast<const P16*>(a.X) + std::min(b0 + r, a.b - 1) * a.ldx + ((lr ^ (r & 15)) * 8);
+    }
+    auto move = [&](int64_t kb, int buf) {
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int h = 0; h < BT / 16; ++h)
+                __builtin_amdgcn_global_load_lds(
+                    (const __attribute__((address_space(1))) void*)(xs[h] + p * a.plane + kb * 128),
+                    (__attribute__((address_space(3))) void*)(S + buf * BUF + p * PLANE + (wave * (BT / 4) + 4 * h) * 128), 16, 0,
+                    0);
+    };
+    uint4v_t w[NR], wn[NR];
+    float sc[NR][4 / FL], sn[NR][4 / FL];
+    auto fetch = [&](int64_t kb) {
+        const int64_t off = kb * 64 + lg * 16;
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+            wn[r] = uint4v_t{0, 0, 0, 0};
+            if (off < a.rb) wn[r] = *reinterpret_cast<const uint4v_t*>(a.codes + row[r] * a.rb + off);
+#pragma unroll
+            for (int t = 0; t < 4 / FL; ++t) {
+                const int64_t j = std::min(kb * 128 + t * 32 * FL, a.n - 1);
+                sn[r][t] = load_as_f32(a.scales, row[r] * a.G + (j >> a.gshift), a.sprec);
             }
-        } else {
-#pragma unroll
-            for (int q = 0; q < 8; ++q) xv[q] = j + q < j1 ? (float)x[j + q] : 0.0f;
         }
+    };
+    if (k0 < k1) {
+        move(k0, 0);
+        fetch(k0);
+    }
+    for (int64_t kb = k0; kb < k1; ++kb) {
+        const int buf = (int)(kb - k0) & 1;
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
 #pragma unroll
-        for (int q = 0; q < 8; ++q) {
-            const float v = j + q < j1 ? load_as_f32(V, (j + q) * k + r, fprec) : 0.0f;
-            acc = mfma(xv[q], v, acc);
+        for (int r = 0; r < NR; ++r) {
+            w[r] = wn[r];
+#pragma unroll
+            for (int t = 0; t < 4 / FL; ++t) sc[r][t] = sn[r][t];
+        }
+        if (kb + 1 < k1) {
+            move(kb + 1, buf ^ 1);
+            fetch(kb + 1);
+        }
+        unsigned ww[NR][4];
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t) ww[r][t] = w[r][t];
+            if (FL != 4) transpose4(ww[r]);
+        }
+        float4_t d[NR][NX];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            typename Tr::frag x[NX][P];
+#pragma unroll
+            for (int f = 0; f < NX; ++f) {
+                const int r = wx * 16 * NX + 16 * f + lr, ch = (FL == 4 ? lg * 4 + t : t * 4 + lg) ^ (r & 15);
+#pragma unroll
+                for (int p = 0; p < P; ++p)
+                    x[f][p] = *reinterpret_cast<const typename Tr::frag*>(S + buf * BUF + p * PLANE + r * 128 + ch * 8);
+            }
+#pragma unroll
+            for (int r = 0; r < NR; ++r) {
+                const typename Tr::frag wf = Tr::widen(ww[r][t]);
+#pragma unroll
+                for (int f = 0; f < NX; ++f) {
+                    if (t % FL == 0) d[r][f] = zero_accv<float4_t>();
+#pragma unroll
+                    for (int p = P - 1; p >= 0; --p) d[r][f] = Tr::mfma(x[f][p], wf, d[r][f]);
+                    if (t % FL == FL - 1) {
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) acc[r][f][v] += sc[r][t / FL] * d[r][f][v];
+                    }
+                }
+            }
         }
     }
+    if (split == 0) add_ranks(a, tok, row, 0, 16, [&](int64_t t, int64_t c) { return a.Tm[t * a.k + c]; }, acc);
 #pragma unroll
-    for (int v = 0; v < 4; ++v) {
-        const int64_t bb = b0 + 4 * lg + v;
-        if (bb < b && r0 + lr < k) part[(s * b + bb) * k + r0 + lr] = acc[v];
+    for (int r = 0; r < NR; ++r)
+#pragma unroll
+        for (int f = 0; f < NX; ++f)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const int64_t i = i0 + wr * 16 * NR + 16 * r + lr, b = b0 + wx * 16 * NX + 16 * f + 4 * lg + v;
+                if (i < a.m && b < a.b) {
+                    if (a.part) a.part[(split * a.b + b) * a.m + i] = acc[r][f][v];
+                    else store_from_f32(a.Y, b * a.ldy + i, a.yprec, acc[r][f][v]);
+                }
+            }
+}
+
+// Y = the sum of the splits, in their order.
+__global__ __launch_bounds__(256) void k_q4_join(const float* __restrict__ part, int splits, int64_t m, int64_t b,
+                                                 void* __restrict__ Y, int64_t ldy, int yprec) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, t = blockIdx.y;
+    if (i >= m) return;
+    float y = 0.0f;
+    for (int q = 0; q < splits; ++q) y += part[(q * b + t) * m + i];
+    store_from_f32(Y, t * ldy + i, yprec, y);
+}
+
+// Activations as 16-bit planes of padded rows (pitch ldp, zero from n on).
+template <typename T>
+__global__ __launch_bounds__(256) void k_q4_pack(const T* __restrict__ X, int64_t ldx, int64_t n, int64_t b,
+                                                 unsigned short* __restrict__ out, int64_t ldp) {
+    const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x, per = ldp / 8;
+    if (c >= b * per) return;
+    typename ActTraits<T>::frag f[ActTraits<T>::P];
+    load_act<T>(X + c / per * ldx, c % per * 8, n, f);
+#pragma unroll
+    for (int p = 0; p < ActTraits<T>::P; ++p)
+        *reinterpret_cast<typename ActTraits<T>::frag*>(out + p * b * ldp + c * 8) = f[p];
+}
+
+// ---- T' = diag(s) V^T x -----------------------------------------------------
+// Partial sums of V^T x over a range of columns: part[split][batch][k].  A
+// workgroup of 4 waves takes 16 TW batch rows and up to 16 F ranks; steps of 128
+// rows of V go through LDS in binary32 (as they lie in memory when the tile holds
+// all ranks: no index arithmetic per value).  TW = 4: a wave per 16 batch rows;
+// TW = 1: the waves share the columns and add up in order.
+template <typename T, int F, int TW>
+__global__ __launch_bounds__(256) void k_q4_mid(const T* __restrict__ X, int64_t ldx, const void* __restrict__ V,
+                                                int fprec, int64_t n, int64_t k, int64_t b, int64_t chunk,
+                                                float* __restrict__ part) {
+    extern __shared__ float lv[];
+    const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4, wave = tid >> 6;
+    const int64_t r0 = (int64_t)blockIdx.x * 16 * F, s = blockIdx.y, b0 = (int64_t)blockIdx.z * 16 * TW;
+    const int w = (int)std::min<int64_t>(k - r0, 16 * F);
+    const int64_t j0 = s * chunk, j1 = std::min(n, j0 + chunk);
+    const T* x = X + std::min(b0 + (TW == 4 ? 16 * wave : 0) + lr, b - 1) * ldx;
+    float4_t acc[F];
+#pragma unroll
+    for (int f = 0; f < F; ++f) acc[f] = zero_accv<float4_t>();
+    for (int64_t j = j0; j < j1; j += 128) {
+        const int rows = (int)std::min<int64_t>(128, j1 - j);
+        __syncthreads();
+        if (w == k) {
+            const int64_t at = j * k;
+            const int count = rows * w;
+            if (fprec == P32) {
+                for (int e = tid; e < 128 * w; e += 256) lv[e] = e < count ? static_cast<const float*>(V)[at + e] : 0.0f;
+            } else {
+                const unsigned short* src = static_cast<const unsigned short*>(V) + at;
+                for (int e = tid * 8; e < 128 * w; e += 2048) {
+                    if (e + 8 <= count) {
+                        const uint4v_t v = load16(src + e);
+#pragma unroll
+                        for (int h = 0; h < 8; ++h) lv[e + h] = fprec == P16 ? elem<half_t>(v, h) : elem<bhalf_t>(v, h);
+                    } else {
+#pragma unroll
+                        for (int h = 0; h < 8; ++h)
+                            if (e + h < 128 * w) lv[e + h] = e + h < count ? load_as_f32(V, at + e + h, fprec) : 0.0f;
+                    }
+                }
+            }
+        } else {
+            for (int e = tid; e < 128 * 16 * F; e += 256) {
+                const int c = e % (16 * F), r = e / (16 * F);
+                if (c < w) lv[r * w + c] = r < rows ? load_as_f32(V, (j + r) * k + r0 + c, fprec) : 0.0f;
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            const int hh = TW == 4 ? h : wave;
+            if (TW == 4 || h == 0) {
+                const int64_t c = j + hh * 32 + lg * 8;
+                float xv[8];
+                if (c + 8 <= j1) {
+#pragma unroll
+                    for (int q = 0; q < (int)sizeof(T) / 2; ++q) {
+                        const uint4v_t v = load16(x + c + q * kVec<T>);
+#pragma unroll
+                        for (int e = 0; e < kVec<T>; ++e) xv[q * kVec<T> + e] = elem<T>(v, e);
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) xv[e] = c + e < j1 ? (float)x[c + e] : 0.0f;
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+#pragma unroll
+                    for (int f = 0; f < F; ++f) {
+                        const int r = 16 * f + lr;
+                        acc[f] = mfma(xv[e], r < w ? lv[(hh * 32 + lg * 8 + e) * w + r] : 0.0f, acc[f]);
+                    }
+            }
+        }
+    }
+    if (TW == 4) {
+#pragma unroll
+        for (int f = 0; f < F; ++f)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const int64_t bb = b0 + 16 * wave + 4 * lg + v, r = 16 * f + lr;
+                if (bb < b && r < w) part[(s * b + bb) * k + r0 + r] = acc[f][v];
+            }
+    } else {
+        __syncthreads();
+#pragma unroll
+        for (int f = 0; f < F; ++f)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) lv[(wave * 16 + 4 * lg + v) * 16 * F + 16 * f + lr] = acc[f][v];
+        __syncthreads();
+        for (int e = tid; e < 256 * F; e += 256) {
+            const int r = e % (16 * F), t = e / (16 * F);
+            float y = lv[t * 16 * F + r];
+#pragma unroll
+            for (int q = 1; q < 4; ++q) y += lv[(q * 16 + t) * 16 * F + r];
+            if (b0 + t < b && r < w) part[(s * b + b0 + t) * k + r0 + r] = y;
+        }
     }
 }
 
@@ -404,88 +685,190 @@ __global__ __launch_bounds__(256) void k_q4_mid_finish(const float* __restrict__
     const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (e >= count) return;
     float t = 0.0f;
+#pragma unroll 8
     for (int q = 0; q < splits; ++q) t += part[q * count + e];
     Tm[e] = t * load_as_f32(s, e % k, fprec);
 }
 
+// ------------------------------------------------------------------ plan --
 namespace {
-struct MidPlan {
-    int splits;
-    int64_t chunk;
+
+struct Q4Plan {
+    bool tile;            // k_q4_tile, else k_q4_rows
+    int wx, nx;           // tile: waves along X, 16-row blocks of X per wave
+    int splits;           // tile: parts of the columns
+    bool pack;            // tile: activations copied to padded planes
+    int64_t ldp;
+    int mid_splits, mid_tw;
+    int64_t mid_chunk;
+    bool mid_finish;      // T' finished by a kernel of its own
+    size_t tm, mid_part, planes, part;
 };
-// About four waves per compute unit, each at least 64 columns deep.
-MidPlan plan_mid(int64_t n, int64_t k, int64_t b) {
-    const int64_t tiles = (k + 15) / 16 * ((b + 15) / 16);
-    int64_t s = std::max<int64_t>(1, std::min<int64_t>(1024 / std::max<int64_t>(tiles, 1), (n + 63) / 64));
-    const int64_t chunk = round_up((n + s - 1) / s, 32);
-    s = (n + chunk - 1) / chunk;
-    return {(int)s, chunk};
-}
-}  // namespace
 
-size_t q4_apply_workspace_bytes(const Q4Weights& w, int64_t batch, int) {
-    if (!w.k) return 0;
-    const size_t t = (size_t)batch * w.k * 4;
-    return (size_t)round_up((int64_t)t, 256) + (size_t)round_up((int64_t)(t * plan_mid(w.n, w.k, batch).splits), 256);
+Q4Plan plan_q4(const Q4Weights& w, const void* X, int64_t ldx, int64_t b, int prec) {
+    Q4Plan p{};
+    const int64_t blocks = (w.n + 127) / 128;
+    p.tile = b > (prec == P32 ? 16 : 32);
+    if (p.tile) {
+        p.wx = prec == P32 || b <= 64 ? 1 : 2;
+        p.nx = 4;
+        const int64_t tiles = (w.m + 127) / 128 * ((b + 64 * p.wx - 1) / (64 * p.wx));
+        p.splits = (int)std::min<int64_t>(std::max<int64_t>(1, 512 / tiles), std::max<int64_t>(1, blocks / 4));
+        const int e = elem_bytes(prec);
+        p.ldp = blocks * 128;
+        p.pack = prec == P32 || w.n % 128 || reinterpret_cast<uintptr_t>(X) % 16 || ldx * e % 16;
+        if (p.pack) p.planes = (size_t)(prec == P32 ? 3 : 1) * b * p.ldp * 2;
+        if (p.splits > 1) p.part = (size_t)p.splits * b * w.m * 4;
+    }
+    if (w.k) {
+        p.mid_tw = b <= 16 ? 1 : 4;
+        const int64_t groups = (w.k + 127) / 128 * ((b + 16 * p.mid_tw - 1) / (16 * p.mid_tw));
+        // enough workgroups for the chip, few partials for their readers
+        int64_t s = std::min<int64_t>(blocks, std::max<int64_t>(1, 512 / groups));
+        s = std::min<int64_t>(s, b <= 2 ? 32 : b <= 16 ? 32 : 64);
+        p.mid_chunk = (blocks + s - 1) / s * 128;
+        p.mid_splits = (int)((w.n + p.mid_chunk - 1) / p.mid_chunk);
+        p.mid_finish = p.tile || b * p.mid_splits > 64;
+        p.mid_part = (size_t)p.mid_splits * b * w.k * 4;
+        if (p.mid_finish) p.tm = (size_t)b * w.k * 4;
+    }
+    return p;
 }
 
-template <typename T, int NB, int RT>
-static void launch_rows(const Q4Args& a, bool vec, hipStream_t st) {
+size_t plan_bytes(const Q4Plan& p) {
+    auto r = [](size_t x) { return (size_t)round_up((int64_t)x, 256); };
+    return r(p.tm) + r(p.mid_part) + r(p.planes) + r(p.part);
+}
+
+template <typename T, int NB, int RT, int FL, int NW>
+void launch_rows(const Q4Args& a, hipStream_t st) {
     KernelTimer t("q4_rows", st);
-    auto* kern = vec ? k_q4_rows<T, NB, RT, true> : k_q4_rows<T, NB, RT, false>;
-    hipLaunchKernelGGL(kern, dim3((unsigned)((a.m + 16 * RT - 1) / (16 * RT)), (unsigned)((a.b + 16 * NB - 1) / (16 * NB))),
-                       dim3(256), 0, st, a);
+    hipLaunchKernelGGL((k_q4_rows<T, NB, RT, FL, NW>), dim3((unsigned)((a.m + 16 * RT - 1) / (16 * RT))), dim3(64 * NW), 0,
+                       st, a);
+}
+template <typename T, int FL>
+void rows_t(const Q4Args& a, hipStream_t st) {
+    if constexpr (sizeof(T) == 2) {
+        if (a.b > 16) return launch_rows<T, 2, 1, FL, 8>(a, st);
+    }
+    launch_rows<T, 1, 1, FL, 8>(a, st);
+}
+
+template <typename T, int WX, int FL>
+void launch_tile(const Q4Args& a, hipStream_t st) {
+    const int tm = (int)((a.m + 127) / 128), tb = (int)((a.b + 64 * WX - 1) / (64 * WX));
+    KernelTimer t("q4_tile", st);
+    hipLaunchKernelGGL((k_q4_tile<T, WX, 4, FL>), dim3(xcd_grid((int64_t)tm * tb * a.splits)), dim3(256), 0, st, a, tm, tb);
+}
+template <typename T, int FL>
+void tile_t(const Q4Plan& p, const Q4Args& a, hipStream_t st) {
+    if constexpr (sizeof(T) == 2) {
+        if (p.wx == 2) return launch_tile<T, 2, FL>(a, st);
+    }
+    launch_tile<T, 1, FL>(a, st);
+}
+
+template <typename T, int F>
+void mid_f(const Q4Plan& p, const Q4Weights& w, const Q4Args& a, float* part, hipStream_t st) {
+    KernelTimer t("q4_mid", st);
+    const dim3 grid((unsigned)((w.k + 16 * F - 1) / (16 * F)), p.mid_splits,
+                    (unsigned)((a.b + 16 * p.mid_tw - 1) / (16 * p.mid_tw)));
+    const int64_t wide = std::min<int64_t>(w.k, 16 * F);
+    const size_t lds = std::max<size_t>((size_t)128 * wide, (size_t)4 * 16 * 16 * F) * 4;
+    auto* kern = p.mid_tw == 4 ? k_q4_mid<T, F, 4> : k_q4_mid<T, F, 1>;
+    hipLaunchKernelGGL(kern, grid, dim3(256), lds, st, static_cast<const T*>(a.X), a.ldx, w.V, w.fprec, w.n, w.k, a.b,
+                       p.mid_chunk, part);
 }
 
 template <typename T>
-static hipError_t apply_t(const Q4Weights& w, Q4Args& a, Workspace& ws, hipStream_t st) {
-    const bool vec = reinterpret_cast<uintptr_t>(a.X) % 16 == 0 && a.ldx * sizeof(T) % 16 == 0;
+hipError_t apply_t(const Q4Weights& w, Q4Args& a, int prec, Workspace& ws, hipStream_t st) {
+    const Q4Plan p = plan_q4(w, a.X, a.ldx, a.b, prec);
+    float* Tm = static_cast<float*>(ws.take(p.tm));
+    float* mid = static_cast<float*>(ws.take(p.mid_part));
+    unsigned short* planes = static_cast<unsigned short*>(ws.take(p.planes));
+    a.part = static_cast<float*>(ws.take(p.part));
+    if (ws.overrun) return hipErrorOutOfMemory;
     if (w.k) {
-        const MidPlan p = plan_mid(w.n, w.k, a.b);
-        float* Tm = static_cast<float*>(ws.take((size_t)a.b * w.k * 4));
-        float* part = static_cast<float*>(ws.take((size_t)p.splits * a.b * w.k * 4));
-        if (ws.overrun) return hipErrorOutOfMemory;
-        {
-            KernelTimer t("q4_mid", st);
-            auto* kern = vec ? k_q4_mid<T, true> : k_q4_mid<T, false>;
-            hipLaunchKernelGGL(kern, dim3((unsigned)((w.k + 15) / 16), (unsigned)((a.b + 15) / 16), p.splits), dim3(64),
-                               0, st, (const T*)a.X, a.ldx, w.V, w.fprec, w.n, w.k, a.b, p.chunk, part);
+        if (w.k <= 32) mid_f<T, 2>(p, w, a, mid, st);
+        else if (w.k <= 80) mid_f<T, 5>(p, w, a, mid, st);
+        else mid_f<T, 8>(p, w, a, mid, st);
+        if (p.mid_finish) {
+            KernelTimer t("q4_mid_finish", st);
+            const int64_t count = a.b * w.k;
+            hipLaunchKernelGGL(k_q4_mid_finish, dim3((unsigned)((count + 255) / 256)), dim3(256), 0, st, mid, p.mid_splits,
+                               w.s, w.fprec, w.k, count, Tm);
+            a.Tm = Tm;
+        } else {
+            a.Tm = mid;
+            a.tsplits = p.mid_splits;
         }
-        KernelTimer t("q4_mid_finish", st);
-        const int64_t count = a.b * w.k;
-        hipLaunchKernelGGL(k_q4_mid_finish, dim3((unsigned)((count + 255) / 256)), dim3(256), 0, st, part, p.splits,
-                           w.s, w.fprec, w.k, count, Tm);
-        a.Tm = Tm;
     }
-    if (a.b <= 16) launch_rows<T, 1, 1>(a, vec, st);
-    else if (a.b <= 32) launch_rows<T, 2, 2>(a, vec, st);
-    else launch_rows<T, 4, 2>(a, vec, st);
+    if (!p.tile) {
+        if (a.gshift == 5) rows_t<T, 1>(a, st);
+        else if (a.gshift == 6) rows_t<T, 2>(a, st);
+        else rows_t<T, 4>(a, st);
+        return hipGetLastError();
+    }
+    a.splits = p.splits;
+    if (p.pack) {
+        KernelTimer t("q4_pack", st);
+        hipLaunchKernelGGL(k_q4_pack<T>, dim3((unsigned)((a.b * (p.ldp / 8) + 255) / 256)), dim3(256), 0, st,
+                           static_cast<const T*>(a.X), a.ldx, w.n, a.b, planes, p.ldp);
+        a.X = planes;
+        a.ldx = p.ldp;
+        a.plane = a.b * p.ldp;
+    }
+    if (a.gshift == 5) tile_t<T, 1>(p, a, st);
+    else if (a.gshift == 6) tile_t<T, 2>(p, a, st);
+    else tile_t<T, 4>(p, a, st);
+    if (p.splits > 1) {
+        KernelTimer t("q4_join", st);
+        hipLaunchKernelGGL(k_q4_join, dim3((unsigned)((w.m + 255) / 256), (unsigned)a.b), dim3(256), 0, st, a.part, p.splits,
+                           w.m, a.b, a.Y, a.ldy, a.yprec);
+    }
     return hipGetLastError();
+}
+
+}  // namespace
+
+// Larger batches run in panels (the grids' third dimension ends at 2^16).
+constexpr int64_t kQ4Panel = 1 << 20;
+
+size_t q4_apply_workspace_bytes(const Q4Weights& w, const void* X, int64_t ldx, int64_t batch, int prec) {
+    size_t bytes = plan_bytes(plan_q4(w, X, ldx, std::min(batch, kQ4Panel), prec));
+    if (batch > kQ4Panel) bytes = std::max(bytes, plan_bytes(plan_q4(w, X, ldx, batch % kQ4Panel, prec)));
+    return bytes;
 }
 
 hipError_t launch_q4_apply(const Q4Weights& w, const void* X, int64_t ldx, void* Y, int64_t ldy, int64_t batch,
                            int prec, int yprec, Workspace& ws, hipStream_t st) {
-    Q4Args a{};
-    a.codes = static_cast<const unsigned char*>(w.codes);
-    a.scales = w.scales;
-    a.rb = q4_row_bytes(w.n);
-    a.G = (w.n + w.group - 1) / w.group;
-    a.sprec = w.sprec;
-    a.gshift = __builtin_ctzll((unsigned long long)w.group);
-    a.U = w.U;
-    a.k = w.k;
-    a.fprec = w.fprec;
-    a.X = X;
-    a.ldx = ldx;
-    a.Y = Y;
-    a.ldy = ldy;
-    a.yprec = yprec;
-    a.m = w.m;
-    a.n = w.n;
-    a.b = batch;
-    if (prec == P32) return apply_t<float>(w, a, ws, st);
-    if (prec == P16) return apply_t<half_t>(w, a, ws, st);
-    return apply_t<bhalf_t>(w, a, ws, st);
+    for (int64_t b0 = 0; b0 < batch; b0 += kQ4Panel) {
+        Q4Args a{};
+        a.codes = static_cast<const unsigned char*>(w.codes);
+        a.scales = w.scales;
+        a.rb = q4_row_bytes(w.n);
+        a.G = (w.n + w.group - 1) / w.group;
+        a.sprec = w.sprec;
+        a.gshift = __builtin_ctzll((unsigned long long)w.group);
+        a.U = w.U;
+        a.s = w.s;
+        a.k = w.k;
+        a.fprec = w.fprec;
+        a.X = static_cast<const char*>(X) + b0 * ldx * elem_bytes(prec);
+        a.ldx = ldx;
+        a.Y = static_cast<char*>(Y) + b0 * ldy * elem_bytes(yprec);
+        a.ldy = ldy;
+        a.yprec = yprec;
+        a.m = w.m;
+        a.n = w.n;
+        a.b = std::min(batch - b0, kQ4Panel);
+        ws.reset();
+        const hipError_t e = prec == P32   ? apply_t<float>(w, a, prec, ws, st)
+                             : prec == P16 ? apply_t<half_t>(w, a, prec, ws, st)
+                                           : apply_t<bhalf_t>(w, a, prec, ws, st);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace lrc
