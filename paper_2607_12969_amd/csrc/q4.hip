@@ -306,113 +306,144 @@ __device__ __forceinline__ void add_ranks(const Q4Args& a, const int64_t (&tok)[
 }
 
 // ---- few rows: the weights' bytes bound it --------------------------------
-// One workgroup of NW waves: 16 RT rows of W for 16 NB rows of X.  The waves
+// One workgroup of NW waves: 16 RT rows of W for up to 16 rows of X.  The waves
 // take steps of 128 columns in turn (so a workgroup streams whole rows) and add
-// up through LDS in a fixed order; codes, scales and activations of the next
-// step are on their way during this one.  FL: MFMAs (32 columns) per scale group,
-// 4 for groups of 128 and more, whose words then need no transpose.
-template <typename T, int NB, int RT, int FL>
-struct RowStep {
-    using Tr = ActTraits<T>;
-    uint4v_t w[RT];
-    float sc[RT][4 / FL];
-    typename Tr::frag x[NB][4][Tr::P];
-};
+// up through LDS in a fixed order.  Only codes come from memory inside the loop,
+// four steps ahead: activations (as 16-bit planes), scales and T' are in LDS, a
+// chunk of KC columns (a multiple of 512 NW) at a time.  FL: MFMAs (32 columns)
+// per scale group, 4 for groups of 128 and more, whose words need no transpose.
+constexpr int kRowsTm = 4096;         // T' values kept in LDS
 
-template <typename T, int NB, int RT, int FL, int NW>
-__global__ __launch_bounds__(64 * NW) void k_q4_rows(Q4Args a) {
+template <typename T, int RT, int FL, int NW>
+__global__ __launch_bounds__(64 * NW) void k_q4_rows(Q4Args a, int KC) {
     using Tr = ActTraits<T>;
-    __shared__ float red[NW][16 * NB][16 * RT + 1];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int lr = lane & 15, lg = lane >> 4;
-    const int64_t i0 = (int64_t)blockIdx.x * 16 * RT, b0 = (int64_t)blockIdx.y * 16 * NB;
-    int64_t row[RT], tok[NB];
+    using P16 = typename Tr::plane_t;
+    constexpr int P = Tr::P, NT = 64 * NW;
+    extern __shared__ uint4v_t lds[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, lr = lane & 15, lg = lane >> 4;
+    const int b = (int)a.b, pitch = KC + 8, GC = KC >> a.gshift;
+    P16* xs = reinterpret_cast<P16*>(lds);                                   // [P][b][pitch]
+    float* ss = reinterpret_cast<float*>(xs + P * b * pitch);                // [16 RT][GC + 1]
+    float* tm = ss + 16 * RT * (GC + 1);                                     // [b][k]
+    const int64_t i0 = (int64_t)blockIdx.x * 16 * RT;
+    int64_t row[RT], tok[1] = {std::min(lr, b - 1)};
+    const unsigned char* src[RT];
 #pragma unroll
-    for (int r = 0; r < RT; ++r) row[r] = std::min(i0 + 16 * r + lr, a.m - 1);
-#pragma unroll
-    for (int f = 0; f < NB; ++f) tok[f] = std::min(b0 + 16 * f + lr, a.b - 1);
-    float4_t acc[RT][NB];
-#pragma unroll
-    for (int r = 0; r < RT; ++r)
-#pragma unroll
-        for (int f = 0; f < NB; ++f) acc[r][f] = zero_accv<float4_t>();
-
+    for (int r = 0; r < RT; ++r) {
+        row[r] = std::min(i0 + 16 * r + lr, a.m - 1);
+        src[r] = a.codes + row[r] * a.rb + lg * 16;
+    }
     const int64_t blocks = (a.n + 127) / 128;
-    auto load = [&](RowStep<T, NB, RT, FL>& st, int64_t kb) {
-        const int64_t off = kb * 64 + lg * 16;
+    uint4v_t w[4][RT];
+    auto load = [&](int q, int64_t kb) {
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
-            st.w[r] = uint4v_t{0, 0, 0, 0};
-            if (off < a.rb) st.w[r] = __builtin_nontemporal_load(reinterpret_cast<const uint4v_t*>(a.codes + row[r] * a.rb + off));
+            w[q][r] = uint4v_t{0, 0, 0, 0};
+            if (kb * 64 + lg * 16 < a.rb)
+                w[q][r] = __builtin_nontemporal_load(reinterpret_cast<const uint4v_t*>(src[r] + kb * 64));
+        }
+    };
 #pragma unroll
-            for (int q = 0; q < 4 / FL; ++q) {
-                const int64_t j = std::min(kb * 128 + q * 32 * FL, a.n - 1);
-                st.sc[r][q] = load_as_f32(a.scales, row[r] * a.G + (j >> a.gshift), a.sprec);
+    for (int q = 0; q < 4; ++q) load(q, q * NW + wave);
+
+    auto stage = [&](int64_t j0) {
+        for (int e = tid; e < b * (KC / 8); e += NT) {
+            const int t = e / (KC / 8), c = e % (KC / 8) * 8;
+            typename Tr::frag f[P];
+            load_act<T>(static_cast<const T*>(a.X) + t * a.ldx, j0 + c, a.n, f);
+#pragma unroll
+            for (int p = 0; p < P; ++p) *reinterpret_cast<typename Tr::frag*>(xs + (p * b + t) * pitch + c) = f[p];
+        }
+        const int64_t g0 = j0 >> a.gshift;
+        for (int e = tid; e < 16 * RT * GC; e += NT) {
+            const int r = e / GC, g = e % GC;
+            ss[r * (GC + 1) + g] =
+                g0 + g < a.G ? load_as_f32(a.scales, std::min(i0 + r, a.m - 1) * a.G + g0 + g, a.sprec) : 0.0f;
+        }
+    };
+    stage(0);
+    const bool held = a.k > 0 && a.b * a.k <= kRowsTm;
+    if (held)
+        for (int e = tid; e < b * (int)a.k; e += NT) {
+            if (!a.tsplits) {
+                tm[e] = a.Tm[e];
+            } else {
+                float x = 0.0f;
+#pragma unroll 16
+                for (int q = 0; q < a.tsplits; ++q) x += a.Tm[q * a.b * a.k + e];
+                tm[e] = x * load_as_f32(a.s, e % a.k, a.fprec);
             }
         }
+    __syncthreads();
+
+    float4_t acc[RT][1];
 #pragma unroll
-        for (int f = 0; f < NB; ++f)
+    for (int r = 0; r < RT; ++r) acc[r][0] = zero_accv<float4_t>();
+    const P16* xl = xs + (int)tok[0] * pitch + (FL == 4 ? lg * 32 : lg * 8);
+    const float* sl = ss + lr * (GC + 1);
+    int64_t c0 = 0;                                     // first step of the chunk
+    for (int64_t kb0 = wave; kb0 - wave < blocks; kb0 += 4 * NW) {
+        if ((kb0 - wave - c0) * 128 == KC) {
+            c0 = kb0 - wave;
+            __syncthreads();
+            stage(c0 * 128);
+            __syncthreads();
+        }
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
-                load_act<T>(static_cast<const T*>(a.X) + tok[f] * a.ldx, kb * 128 + (FL == 4 ? lg * 32 + t * 8 : t * 32 + lg * 8),
-                            a.n, st.x[f][t]);
-    };
-    auto multiply = [&](RowStep<T, NB, RT, FL>& st) {
+        for (int q = 0; q < 4; ++q) {
+            const int64_t kb = kb0 + q * NW;
+            if (kb < blocks) {
+                const int col = (int)(kb - c0) * 128;
+                unsigned ww[RT][4];
 #pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            unsigned w[4] = {st.w[r][0], st.w[r][1], st.w[r][2], st.w[r][3]};
-            if (FL != 4) transpose4(w);
-            float4_t d[NB];
+                for (int r = 0; r < RT; ++r) {
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const typename Tr::frag wf = Tr::widen(w[t]);
+                    for (int t = 0; t < 4; ++t) ww[r][t] = w[q][r][t];
+                    if (FL != 4) transpose4(ww[r]);
+                }
+                load(q, kb + 4 * NW);
+                float4_t d[RT];
 #pragma unroll
-                for (int f = 0; f < NB; ++f) {
-                    if (t % FL == 0) d[f] = zero_accv<float4_t>();
+                for (int t = 0; t < 4; ++t) {
+                    typename Tr::frag x[P];
 #pragma unroll
-                    for (int p = Tr::P - 1; p >= 0; --p) d[f] = Tr::mfma(st.x[f][t][p], wf, d[f]);
-                    if (t % FL == FL - 1) {
+                    for (int p = 0; p < P; ++p)
+                        x[p] = *reinterpret_cast<const typename Tr::frag*>(xl + p * b * pitch + col + (FL == 4 ? t * 8 : t * 32));
 #pragma unroll
-                        for (int v = 0; v < 4; ++v) acc[r][f][v] += st.sc[r][t / FL] * d[f][v];
+                    for (int r = 0; r < RT; ++r) {
+                        const typename Tr::frag wf = Tr::widen(ww[r][t]);
+                        if (t % FL == 0) d[r] = zero_accv<float4_t>();
+#pragma unroll
+                        for (int p = P - 1; p >= 0; --p) d[r] = Tr::mfma(x[p], wf, d[r]);
+                        if (t % FL == FL - 1) {
+                            const float sc = sl[16 * r * (GC + 1) + ((col + (t / FL) * 32 * FL) >> a.gshift)];
+#pragma unroll
+                            for (int v = 0; v < 4; ++v) acc[r][0][v] += sc * d[r][v];
+                        }
                     }
                 }
             }
         }
-    };
-    RowStep<T, NB, RT, FL> s0, s1;
-    int64_t kb = wave;
-    if (kb < blocks) load(s0, kb);
-    for (; kb < blocks; kb += 2 * NW) {
-        if (kb + NW < blocks) load(s1, kb + NW);
-        multiply(s0);
-        if (kb + NW < blocks) {
-            if (kb + 2 * NW < blocks) load(s0, kb + 2 * NW);
-            multiply(s1);
-        }
     }
     if (a.k) {
-        auto tm = [&](int64_t t, int64_t c) {
-            if (!a.tsplits) return a.Tm[t * a.k + c];
-            float x = 0.0f;
-            for (int q = 0; q < a.tsplits; ++q) x += a.Tm[(q * a.b + t) * a.k + c];
-            return x * load_as_f32(a.s, c, a.fprec);
-        };
-        add_ranks(a, tok, row, 16 * wave, 16 * NW, tm, acc);
+        const float* from = held ? tm : a.Tm;
+        add_ranks(a, tok, row, 16 * wave, 16 * NW, [&](int64_t t, int64_t c) { return from[t * a.k + c]; }, acc);
     }
+    __syncthreads();
+    float* red = reinterpret_cast<float*>(lds);                              // [NW][16][16 RT + 1]
+    constexpr int RP = 16 * RT + 1;
 #pragma unroll
     for (int r = 0; r < RT; ++r)
 #pragma unroll
-        for (int f = 0; f < NB; ++f)
-#pragma unroll
-            for (int v = 0; v < 4; ++v) red[wave][16 * f + 4 * lg + v][16 * r + lr] = acc[r][f][v];
+        for (int v = 0; v < 4; ++v) red[(wave * 16 + 4 * lg + v) * RP + 16 * r + lr] = acc[r][0][v];
     __syncthreads();
-    for (int e = threadIdx.x; e < 256 * NB * RT; e += 64 * NW) {
-        const int i = e % (16 * RT), f = e / (16 * RT);
-        if (i0 + i < a.m && b0 + f < a.b) {
-            float y = red[0][f][i];
+    for (int e = tid; e < 16 * RT * b; e += NT) {
+        const int i = e % (16 * RT), t = e / (16 * RT);
+        if (i0 + i < a.m) {
+            float y = red[t * RP + i];
 #pragma unroll
-            for (int w = 1; w < NW; ++w) y += red[w][f][i];
-            store_from_f32(a.Y, (b0 + f) * a.ldy + i0 + i, a.yprec, y);
+            for (int q = 1; q < NW; ++q) y += red[(q * 16 + t) * RP + i];
+            store_from_f32(a.Y, t * a.ldy + i0 + i, a.yprec, y);
         }
     }
 }
@@ -699,20 +730,39 @@ struct Q4Plan {
     int splits;           // tile: parts of the columns
     bool pack;            // tile: activations copied to padded planes
     int64_t ldp;
+    int kc, nw, rt;       // rows: columns in LDS at a time, waves, row blocks per wave
+    size_t lds;
     int mid_splits, mid_tw;
     int64_t mid_chunk;
     bool mid_finish;      // T' finished by a kernel of its own
     size_t tm, mid_part, planes, part;
 };
 
+// k_q4_rows for up to 16 rows whose activations leave room in LDS: false when
+// the tile kernel is to be taken.
+bool plan_rows(Q4Plan& p, const Q4Weights& w, int64_t b, int prec) {
+    if (b > 16) return false;
+    const int64_t planes = prec == P32 ? 3 : 1, tiles = (w.m + 15) / 16;
+    p.rt = tiles >= 1024 ? 2 : 1;
+    p.nw = tiles <= 512 && b * planes <= 8 ? 8 : 4;
+    // 64 KB of activations, and no more than the columns there are
+    const int64_t unit = 512 * p.nw, most = std::min<int64_t>(65536 / (2 * b * planes), 8192) / unit * unit;
+    if (most < unit) return false;
+    p.kc = (int)std::min<int64_t>(most, round_up(w.n, unit));
+    const size_t x = (size_t)planes * b * (p.kc + 8) * 2, s = (size_t)16 * p.rt * (p.kc / w.group + 1) * 4;
+    const size_t t = w.k && b * w.k <= kRowsTm ? (size_t)b * w.k * 4 : 0;
+    p.lds = std::max(x + s + t, (size_t)p.nw * 16 * (16 * p.rt + 1) * 4);
+    return true;
+}
+
 Q4Plan plan_q4(const Q4Weights& w, const void* X, int64_t ldx, int64_t b, int prec) {
     Q4Plan p{};
     const int64_t blocks = (w.n + 127) / 128;
-    p.tile = b > (prec == P32 ? 16 : 32);
+    p.tile = !plan_rows(p, w, b, prec);
     if (p.tile) {
         p.wx = prec == P32 || b <= 64 ? 1 : 2;
-        p.nx = 4;
-        const int64_t tiles = (w.m + 127) / 128 * ((b + 64 * p.wx - 1) / (64 * p.wx));
+        p.nx = b <= 32 ? 2 : 4;
+        const int64_t tiles = (w.m + 127) / 128 * ((b + 16 * p.nx * p.wx - 1) / (16 * p.nx * p.wx));
         p.splits = (int)std::min<int64_t>(std::max<int64_t>(1, 512 / tiles), std::max<int64_t>(1, blocks / 4));
         const int e = elem_bytes(prec);
         p.ldp = blocks * 128;
@@ -728,7 +778,7 @@ Q4Plan plan_q4(const Q4Weights& w, const void* X, int64_t ldx, int64_t b, int pr
         s = std::min<int64_t>(s, b <= 2 ? 32 : b <= 16 ? 32 : 64);
         p.mid_chunk = (blocks + s - 1) / s * 128;
         p.mid_splits = (int)((w.n + p.mid_chunk - 1) / p.mid_chunk);
-        p.mid_finish = p.tile || b * p.mid_splits > 64;
+        p.mid_finish = p.tile || b * p.mid_splits > 64 || b * w.k > kRowsTm;
         p.mid_part = (size_t)p.mid_splits * b * w.k * 4;
         if (p.mid_finish) p.tm = (size_t)b * w.k * 4;
     }
@@ -740,32 +790,37 @@ size_t plan_bytes(const Q4Plan& p) {
     return r(p.tm) + r(p.mid_part) + r(p.planes) + r(p.part);
 }
 
-template <typename T, int NB, int RT, int FL, int NW>
-void launch_rows(const Q4Args& a, hipStream_t st) {
+template <typename T, int RT, int FL, int NW>
+hipError_t launch_rows(const Q4Plan& p, const Q4Args& a, hipStream_t st) {
+    auto* kern = k_q4_rows<T, RT, FL, NW>;
+    if (p.lds > 65536) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern),
+                                                 hipFuncAttributeMaxDynamicSharedMemorySize, (int)p.lds);
+        if (e != hipSuccess) return e;
+    }
     KernelTimer t("q4_rows", st);
-    hipLaunchKernelGGL((k_q4_rows<T, NB, RT, FL, NW>), dim3((unsigned)((a.m + 16 * RT - 1) / (16 * RT))), dim3(64 * NW), 0,
-                       st, a);
+    hipLaunchKernelGGL(kern, dim3((unsigned)((a.m + 16 * RT - 1) / (16 * RT))), dim3(64 * NW), p.lds, st, a, p.kc);
+    return hipGetLastError();
 }
 template <typename T, int FL>
-void rows_t(const Q4Args& a, hipStream_t st) {
-    if constexpr (sizeof(T) == 2) {
-        if (a.b > 16) return launch_rows<T, 2, 1, FL, 8>(a, st);
-    }
-    launch_rows<T, 1, 1, FL, 8>(a, st);
+hipError_t rows_t(const Q4Plan& p, const Q4Args& a, hipStream_t st) {
+    if (p.rt == 2) return launch_rows<T, 2, FL, 4>(p, a, st);
+    return p.nw == 8 ? launch_rows<T, 1, FL, 8>(p, a, st) : launch_rows<T, 1, FL, 4>(p, a, st);
 }
 
-template <typename T, int WX, int FL>
+template <typename T, int WX, int NX, int FL>
 void launch_tile(const Q4Args& a, hipStream_t st) {
-    const int tm = (int)((a.m + 127) / 128), tb = (int)((a.b + 64 * WX - 1) / (64 * WX));
+    const int tm = (int)((a.m + 127) / 128), tb = (int)((a.b + 16 * NX * WX - 1) / (16 * NX * WX));
     KernelTimer t("q4_tile", st);
-    hipLaunchKernelGGL((k_q4_tile<T, WX, 4, FL>), dim3(xcd_grid((int64_t)tm * tb * a.splits)), dim3(256), 0, st, a, tm, tb);
+    hipLaunchKernelGGL((k_q4_tile<T, WX, NX, FL>), dim3(xcd_grid((int64_t)tm * tb * a.splits)), dim3(256), 0, st, a, tm, tb);
 }
 template <typename T, int FL>
 void tile_t(const Q4Plan& p, const Q4Args& a, hipStream_t st) {
     if constexpr (sizeof(T) == 2) {
-        if (p.wx == 2) return launch_tile<T, 2, FL>(a, st);
+        if (p.wx == 2) return launch_tile<T, 2, 4, FL>(a, st);
     }
-    launch_tile<T, 1, FL>(a, st);
+    if (p.nx == 2) return launch_tile<T, 1, 2, FL>(a, st);
+    launch_tile<T, 1, 4, FL>(a, st);
 }
 
 template <typename T, int F>
@@ -804,10 +859,9 @@ hipError_t apply_t(const Q4Weights& w, Q4Args& a, int prec, Workspace& ws, hipSt
         }
     }
     if (!p.tile) {
-        if (a.gshift == 5) rows_t<T, 1>(a, st);
-        else if (a.gshift == 6) rows_t<T, 2>(a, st);
-        else rows_t<T, 4>(a, st);
-        return hipGetLastError();
+        if (a.gshift == 5) return rows_t<T, 1>(p, a, st);
+        if (a.gshift == 6) return rows_t<T, 2>(p, a, st);
+        return rows_t<T, 4>(p, a, st);
     }
     a.splits = p.splits;
     if (p.pack) {
