@@ -164,8 +164,9 @@ struct Q4Args {
     int64_t rb, G;
     int sprec, gshift;
     const void* U;
-    const float* Tm;      // T' [batch][k], or its `tsplits` partial sums without the factor s
-    int tsplits;
+    const float* Tm;      // T' [batch][kp], kp = k rounded up to 16, zero past k; or tsplits
+    int tsplits;          // partial sums [tsplits][batch][k] without the factor s
+    int64_t kp;
     const void* s;
     int64_t k;
     int fprec;
@@ -281,28 +282,87 @@ __device__ __forceinline__ void transpose4(unsigned (&w)[4]) {
     w[3] = d[1];
 }
 
+// Four ranks of a row of U (as stored; zero past k) from rank c on, widened by
+// the caller: loading and converting apart lets all loads of a step overlap.
+__device__ __forceinline__ uint4v_t load_ranks(const Q4Args& a, int64_t row, int64_t c, bool whole) {
+    uint4v_t v = {0, 0, 0, 0};
+    const int64_t at = row * a.k + c;
+    if (a.fprec == P32) {
+        const unsigned* u = static_cast<const unsigned*>(a.U) + at;
+        if (whole) return load16(u);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (c + e < a.k) v[e] = u[e];
+    } else {
+        const unsigned short* u = static_cast<const unsigned short*>(a.U) + at;
+        if (whole) {
+            uint2v_t h;
+            __builtin_memcpy(&h, u, 8);
+            v[0] = h[0];
+            v[1] = h[1];
+        } else {
+            unsigned w[4] = {0, 0, 0, 0};
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (c + e < a.k) w[e] = u[e];
+            v[0] = w[0] | w[1] << 16;
+            v[1] = w[2] | w[3] << 16;
+        }
+    }
+    return v;
+}
+
 // Adds T' U^T, 16 ranks at a time from rank q0 in steps of `step`, to FA x FB
-// result blocks: tok[a] are the batch rows, row[b] the rows of U of this lane's
-// operand in each block.
-template <int FA, int FB, typename F>
-__device__ __forceinline__ void add_ranks(const Q4Args& a, const int64_t (&tok)[FA], const int64_t (&row)[FB],
-                                          int64_t q0, int64_t step, F&& tm, float4_t (&acc)[FB][FA]) {
+// result blocks: tm[f] points at T' of this lane's batch row in block f (a pitch
+// of whole 16 ranks, zero past k), row[r] is its row of U in block r.
+template <int FA, int FB>
+__device__ __forceinline__ void add_ranks(const Q4Args& a, const float* const (&tm)[FA], const int64_t (&row)[FB],
+                                          int64_t q0, int64_t step, float4_t (&acc)[FB][FA]) {
     const int lg = (threadIdx.x & 63) >> 4;
     for (int64_t q = q0; q < a.k; q += step) {
+        const int64_t c = q + lg * 4;
+        const bool whole = q + 16 <= a.k;
+        uint4v_t ur[FB];
+        float4_t tv[FA];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const int64_t c = q + lg * 4 + t;
-            float tv[FA], uv[FB];
+        for (int r = 0; r < FB; ++r) ur[r] = load_ranks(a, row[r], c, whole);
 #pragma unroll
-            for (int f = 0; f < FA; ++f) tv[f] = c < a.k ? tm(tok[f], c) : 0.0f;
+        for (int f = 0; f < FA; ++f) tv[f] = *reinterpret_cast<const float4_t*>(tm[f] + c);
+        float4_t uv[FB];
+        if (a.fprec == P32) {
 #pragma unroll
-            for (int r = 0; r < FB; ++r) uv[r] = c < a.k ? load_as_f32(a.U, row[r] * a.k + c, a.fprec) : 0.0f;
+            for (int r = 0; r < FB; ++r) uv[r] = __builtin_bit_cast(float4_t, ur[r]);
+        } else if (a.fprec == P16) {
 #pragma unroll
             for (int r = 0; r < FB; ++r)
 #pragma unroll
-                for (int f = 0; f < FA; ++f) acc[r][f] = mfma(tv[f], uv[r], acc[r][f]);
+                for (int e = 0; e < 4; ++e) uv[r][e] = elem<half_t>(ur[r], e);
+        } else {
+#pragma unroll
+            for (int r = 0; r < FB; ++r)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) uv[r][e] = elem<bhalf_t>(ur[r], e);
         }
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int r = 0; r < FB; ++r)
+#pragma unroll
+                for (int f = 0; f < FA; ++f) acc[r][f] = mfma(tv[f][t], uv[r][t], acc[r][f]);
     }
+}
+
+// Sum of `count` values `step` apart, in order, 16 loads at a time.
+__device__ __forceinline__ float sum_splits(const float* from, int count, int64_t step) {
+    float t = 0.0f;
+    for (int q = 0; q < count; q += 16) {
+        float v[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) v[e] = q + e < count ? from[(q + e) * step] : 0.0f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) t += v[e];
+    }
+    return t;
 }
 
 // ---- few rows: the weights' bytes bound it --------------------------------
@@ -324,7 +384,7 @@ __global__ __launch_bounds__(64 * NW) void k_q4_rows(Q4Args a, int KC) {
     const int b = (int)a.b, pitch = KC + 8, GC = KC >> a.gshift;
     P16* xs = reinterpret_cast<P16*>(lds);                                   // [P][b][pitch]
     float* ss = reinterpret_cast<float*>(xs + P * b * pitch);                // [16 RT][GC + 1]
-    float* tm = ss + 16 * RT * (GC + 1);                                     // [b][k]
+    float* tm = ss + ((16 * RT * (GC + 1) + 3) & ~3);                        // [b][kp]
     const int64_t i0 = (int64_t)blockIdx.x * 16 * RT;
     int64_t row[RT], tok[1] = {std::min(lr, b - 1)};
     const unsigned char* src[RT];
@@ -362,17 +422,20 @@ __global__ __launch_bounds__(64 * NW) void k_q4_rows(Q4Args a, int KC) {
         }
     };
     stage(0);
-    const bool held = a.k > 0 && a.b * a.k <= kRowsTm;
+    const bool held = a.k > 0 && a.b * a.kp <= kRowsTm;
     if (held)
-        for (int e = tid; e < b * (int)a.k; e += NT) {
+        for (int e = tid; e < b * (int)a.kp; e += NT) {
+            float x = 0.0f;
             if (!a.tsplits) {
-                tm[e] = a.Tm[e];
+                x = a.Tm[e];
             } else {
-                float x = 0.0f;
-#pragma unroll 16
-                for (int q = 0; q < a.tsplits; ++q) x += a.Tm[q * a.b * a.k + e];
-                tm[e] = x * load_as_f32(a.s, e % a.k, a.fprec);
+                const int t = e / (int)a.kp, c = e % (int)a.kp;
+                if (c < a.k) {
+                    const float* from = a.Tm + t * a.k + c;
+                    x = sum_splits(from, a.tsplits, a.b * a.k) * load_as_f32(a.s, c, a.fprec);
+                }
             }
+            tm[e] = x;
         }
     __syncthreads();
 
@@ -426,8 +489,8 @@ __global__ __launch_bounds__(64 * NW) void k_q4_rows(Q4Args a, int KC) {
         }
     }
     if (a.k) {
-        const float* from = held ? tm : a.Tm;
-        add_ranks(a, tok, row, 16 * wave, 16 * NW, [&](int64_t t, int64_t c) { return from[t * a.k + c]; }, acc);
+        const float* const at[1] = {(held ? tm : a.Tm) + tok[0] * a.kp};
+        add_ranks(a, at, row, 16 * wave, 16 * NW, acc);
     }
     __syncthreads();
     float* red = reinterpret_cast<float*>(lds);                              // [NW][16][16 RT + 1]
@@ -448,21 +511,37 @@ __global__ __launch_bounds__(64 * NW) void k_q4_rows(Q4Args a, int KC) {
     }
 }
 
-// ---- many rows: bound by the matrix cores ----------------------------------
-// One workgroup of 4 waves: 128 rows of W for 16 NX WX rows of X, WX waves along
-// X and 4 / WX along W, a wave 16 NR x 16 NX results.  Steps of 128 columns: the
-// activations move straight into one of two LDS buffers (the other is being
-// multiplied), rows of 256 bytes with their 16-byte chunks XOR-swizzled by the
-// row on the global side; the codes go to registers and are widened there, once
-// for NX MFMAs.  X: 16-bit planes, 16-byte aligned rows, zero from n on to the
-// next multiple of 128.
-template <typename T, int WX, int NX, int FL>
-__global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) void k_q4_tile(Q4Args a, int tiles_m, int tiles_b) {
+// ---- many rows: tiles --------------------------------------------------------
+// One workgroup of 4 waves: 128 rows of W for BT = 16 NX WX rows of X, WX waves
+// along X and 4 / WX along W, a wave 16 NR x 16 NX results.  Steps of 128 columns
+// move codes and activations straight into one of D LDS buffers, D - 1 steps
+// ahead.  Rows of X (256 bytes a step) have their 16-byte chunks XOR-swizzled by
+// the row on the global side; rows of codes are 64 bytes, a wave's 16 of them one
+// contiguous load.  Codes are widened in registers, once for NX MFMAs.  X: 16-bit
+// planes, 16-byte aligned rows, zero from n on to the next multiple of 128 (codes
+// read past a row's end meet these zeros).
+template <typename T, int WX, int NX> struct TileCfg {
+    static constexpr int P = ActTraits<T>::P, NR = 2 * WX, BT = 16 * NX * WX;
+    static constexpr int XB = P * BT * 256, BUF = XB + 128 * 64;                 // bytes of a step
+    static constexpr int D = BUF <= 20480 ? 4 : BUF <= 24576 ? 3 : 2;
+    static constexpr int EU = D * BUF > 81920 ? 1 : 2;
+    static constexpr int LOADS = P * BT / 16 + 2;                                // of a wave in a step
+};
+
+// SB: bytes of a scale.  The two 16-bit types are told apart by a mask, without a branch.
+template <int SB> __device__ __forceinline__ float scale_of_bits(unsigned u, unsigned bf16_mask) {
+    if (SB == 4) return __uint_as_float(u);
+    const unsigned short h = (unsigned short)u;
+    const unsigned x = __float_as_uint((float)__builtin_bit_cast(half_t, h));
+    return __uint_as_float((u << 16 & bf16_mask) | (x & ~bf16_mask));
+}
+
+template <typename T, int WX, int NX, int FL, int SB>
+__global__ __launch_bounds__(256, (TileCfg<T, WX, NX>::EU)) void k_q4_tile(Q4Args a, int tiles_m, int tiles_b) {
     using Tr = ActTraits<T>;
-    using P16 = typename Tr::plane_t;
-    constexpr int P = Tr::P, NR = 2 * WX, BT = 16 * NX * WX;       // rows of X in a tile
-    constexpr int PLANE = BT * 128, BUF = P * PLANE;
-    __shared__ alignas(16) P16 S[2 * BUF];
+    using C = TileCfg<T, WX, NX>;
+    constexpr int P = C::P, NR = C::NR, BT = C::BT, D = C::D;
+    __shared__ alignas(16) char S[D * C::BUF];
     const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wx = wave % WX, wr = wave / WX;
@@ -473,11 +552,6 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) void k_q4_tile(Q4Args 
     const int64_t g = q / (8 * tiles_b), gs = std::min<int64_t>(8, tiles_m - 8 * g), in = q - g * 8 * tiles_b;
     const int64_t i0 = (8 * g + in % gs) * 128, b0 = in / gs * BT;
 
-    int64_t row[NR], tok[NX];
-#pragma unroll
-    for (int r = 0; r < NR; ++r) row[r] = std::min(i0 + wr * 16 * NR + 16 * r + lr, a.m - 1);
-#pragma unroll
-    for (int f = 0; f < NX; ++f) tok[f] = std::min(b0 + wx * 16 * NX + 16 * f + lr, a.b - 1);
     float4_t acc[NR][NX];
 #pragma unroll
     for (int r = 0; r < NR; ++r)
@@ -486,62 +560,74 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) void k_q4_tile(Q4Args 
 
     const int64_t blocks = (a.n + 127) / 128;
     const int64_t k0 = blocks * split / a.splits, k1 = blocks * (split + 1) / a.splits;
-    // wave w moves rows [w BT / 4, (w + 1) BT / 4) of every plane, 4 rows a load
-    const P16* xs[BT / 16];
+    // wave w moves rows [w BT / 4, (w + 1) BT / 4) of every plane, 4 rows a load,
+    // and rows [32 w, 32 w + 32) of codes, 16 rows a load
+    const char* xs[BT / 16];
 #pragma unroll
     for (int h = 0; h < BT / 16; ++h) {
         const int r = wave * (BT / 4) + 4 * h + lg;
-        xs[h] = static_cast<const P16*>(a.X) + std::min(b0 + r, a.b - 1) * a.ldx + ((lr ^ (r & 15)) * 8);
+        xs[h] = static_cast<const char*>(a.X) + (std::min(b0 + r, a.b - 1) * a.ldx + ((lr ^ (r & 15)) * 8)) * 2;
     }
+    const unsigned char* cs[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) cs[h] = a.codes + std::min(i0 + wave * 32 + 16 * h + (lane >> 2), a.m - 1) * a.rb;
     auto move = [&](int64_t kb, int buf) {
+        char* to = S + buf * C::BUF;
 #pragma unroll
         for (int p = 0; p < P; ++p)
 #pragma unroll
             for (int h = 0; h < BT / 16; ++h)
                 __builtin_amdgcn_global_load_lds(
-                    (const __attribute__((address_space(1))) void*)(xs[h] + p * a.plane + kb * 128),
-                    (__attribute__((address_space(3))) void*)(S + buf * BUF + p * PLANE + (wave * (BT / 4) + 4 * h) * 128), 16, 0,
-                    0);
-    };
-    uint4v_t w[NR], wn[NR];
-    float sc[NR][4 / FL], sn[NR][4 / FL];
-    auto fetch = [&](int64_t kb) {
-        const int64_t off = kb * 64 + lg * 16;
+                    (const __attribute__((address_space(1))) void*)(xs[h] + p * a.plane * 2 + kb * 256),
+                    (__attribute__((address_space(3))) void*)(to + p * BT * 256 + (wave * (BT / 4) + 4 * h) * 256), 16, 0, 0);
+        const int64_t off = std::min(kb * 64 + (lane & 3) * 16, a.rb - 16);
 #pragma unroll
-        for (int r = 0; r < NR; ++r) {
-            wn[r] = uint4v_t{0, 0, 0, 0};
-            if (off < a.rb) wn[r] = *reinterpret_cast<const uint4v_t*>(a.codes + row[r] * a.rb + off);
-#pragma unroll
-            for (int t = 0; t < 4 / FL; ++t) {
-                const int64_t j = std::min(kb * 128 + t * 32 * FL, a.n - 1);
-                sn[r][t] = load_as_f32(a.scales, row[r] * a.G + (j >> a.gshift), a.sprec);
-            }
-        }
+        for (int h = 0; h < 2; ++h)
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(cs[h] + off),
+                                             (__attribute__((address_space(3))) void*)(to + C::XB + (wave * 32 + 16 * h) * 64), 16,
+                                             0, 0);
     };
-    if (k0 < k1) {
-        move(k0, 0);
-        fetch(k0);
-    }
+    int64_t srow[NR];                                   // where a row's scales begin
+#pragma unroll
+    for (int r = 0; r < NR; ++r) srow[r] = std::min(i0 + wr * 16 * NR + 16 * r + lr, a.m - 1) * a.G;
+    unsigned sn[NR][4 / FL];
+    auto fetch = [&](int64_t kb) {                      // bits only: converting here would wait for the load
+        int64_t at[4 / FL];
+#pragma unroll
+        for (int t = 0; t < 4 / FL; ++t) at[t] = std::min(kb * 128 + t * 32 * FL, a.n - 1) >> a.gshift;
+#pragma unroll
+        for (int r = 0; r < NR; ++r)
+#pragma unroll
+            for (int t = 0; t < 4 / FL; ++t)
+                sn[r][t] = SB == 4 ? static_cast<const unsigned*>(a.scales)[srow[r] + at[t]]
+                                   : static_cast<const unsigned short*>(a.scales)[srow[r] + at[t]];
+    };
+    const unsigned bf16_mask = a.sprec == PB16 ? ~0u : 0u;
+    if (k0 < k1) fetch(k0);
+#pragma unroll
+    for (int d = 0; d < D - 1; ++d)
+        if (k0 + d < k1) move(k0 + d, d);
+    int buf = 0;
     for (int64_t kb = k0; kb < k1; ++kb) {
-        const int buf = (int)(kb - k0) & 1;
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        // this step has landed when no more than the loads of the D - 2 later ones are on their way
+        if (kb + D - 2 < k1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((D - 2) * C::LOADS) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
+        float sc[NR][4 / FL];
 #pragma unroll
-        for (int r = 0; r < NR; ++r) {
-            w[r] = wn[r];
+        for (int r = 0; r < NR; ++r)
 #pragma unroll
-            for (int t = 0; t < 4 / FL; ++t) sc[r][t] = sn[r][t];
-        }
-        if (kb + 1 < k1) {
-            move(kb + 1, buf ^ 1);
-            fetch(kb + 1);
-        }
+            for (int t = 0; t < 4 / FL; ++t) sc[r][t] = scale_of_bits<SB>(sn[r][t], bf16_mask);
+        if (kb + 1 < k1) fetch(kb + 1);
+        if (kb + D - 1 < k1) move(kb + D - 1, buf == 0 ? D - 1 : buf - 1);
+        const char* from = S + buf * C::BUF;
         unsigned ww[NR][4];
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
+            const uint4v_t w = *reinterpret_cast<const uint4v_t*>(from + C::XB + (wr * 16 * NR + 16 * r + lr) * 64 + lg * 16);
 #pragma unroll
-            for (int t = 0; t < 4; ++t) ww[r][t] = w[r][t];
+            for (int t = 0; t < 4; ++t) ww[r][t] = w[t];
             if (FL != 4) transpose4(ww[r]);
         }
         float4_t d[NR][NX];
@@ -553,7 +639,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) void k_q4_tile(Q4Args 
                 const int r = wx * 16 * NX + 16 * f + lr, ch = (FL == 4 ? lg * 4 + t : t * 4 + lg) ^ (r & 15);
 #pragma unroll
                 for (int p = 0; p < P; ++p)
-                    x[f][p] = *reinterpret_cast<const typename Tr::frag*>(S + buf * BUF + p * PLANE + r * 128 + ch * 8);
+                    x[f][p] = *reinterpret_cast<const typename Tr::frag*>(from + p * BT * 256 + r * 256 + ch * 16);
             }
 #pragma unroll
             for (int r = 0; r < NR; ++r) {
@@ -570,8 +656,17 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) void k_q4_tile(Q4Args 
                 }
             }
         }
+        buf = buf == D - 1 ? 0 : buf + 1;
     }
-    if (split == 0) add_ranks(a, tok, row, 0, 16, [&](int64_t t, int64_t c) { return a.Tm[t * a.k + c]; }, acc);
+    if (split == 0 && a.k) {
+        int64_t row[NR];
+        const float* tm[NX];
+#pragma unroll
+        for (int r = 0; r < NR; ++r) row[r] = std::min(i0 + wr * 16 * NR + 16 * r + lr, a.m - 1);
+#pragma unroll
+        for (int f = 0; f < NX; ++f) tm[f] = a.Tm + std::min(b0 + wx * 16 * NX + 16 * f + lr, a.b - 1) * a.kp;
+        add_ranks(a, tm, row, 0, 16, acc);
+    }
 #pragma unroll
     for (int r = 0; r < NR; ++r)
 #pragma unroll
@@ -709,16 +804,19 @@ __global__ __launch_bounds__(256) void k_q4_mid(const T* __restrict__ X, int64_t
     }
 }
 
-// T'[b][r] = s_r times the sum of the partials, in split order.
+// T'[b][r] = s_r times the sum of the partials, in split order; rows of kp, zero
+// past k.
 __global__ __launch_bounds__(256) void k_q4_mid_finish(const float* __restrict__ part, int splits,
-                                                       const void* __restrict__ s, int fprec, int64_t k, int64_t count,
-                                                       float* __restrict__ Tm) {
+                                                       const void* __restrict__ s, int fprec, int64_t k, int64_t kp,
+                                                       int64_t b, float* __restrict__ Tm) {
     const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (e >= count) return;
+    if (e >= b * kp) return;
+    const int64_t r = e % kp;
     float t = 0.0f;
-#pragma unroll 8
-    for (int q = 0; q < splits; ++q) t += part[q * count + e];
-    Tm[e] = t * load_as_f32(s, e % k, fprec);
+    if (r < k) {
+        t = sum_splits(part + e / kp * k + r, splits, b * k) * load_as_f32(s, r, fprec);
+    }
+    Tm[e] = t;
 }
 
 // ------------------------------------------------------------------ plan --
@@ -738,10 +836,12 @@ struct Q4Plan {
     size_t tm, mid_part, planes, part;
 };
 
-// k_q4_rows for up to 16 rows whose activations leave room in LDS: false when
+// 8192 x 8192: 8 rows 29 us here, 37 on the tiles; 16 rows 31 against 25.
+constexpr int64_t kRowsMax = 8;
+// k_q4_rows for few rows whose activations leave room in LDS: false when
 // the tile kernel is to be taken.
 bool plan_rows(Q4Plan& p, const Q4Weights& w, int64_t b, int prec) {
-    if (b > 16) return false;
+    if (b > kRowsMax) return false;
     const int64_t planes = prec == P32 ? 3 : 1, tiles = (w.m + 15) / 16;
     p.rt = tiles >= 1024 ? 2 : 1;
     p.nw = tiles <= 512 && b * planes <= 8 ? 8 : 4;
@@ -750,7 +850,8 @@ bool plan_rows(Q4Plan& p, const Q4Weights& w, int64_t b, int prec) {
     if (most < unit) return false;
     p.kc = (int)std::min<int64_t>(most, round_up(w.n, unit));
     const size_t x = (size_t)planes * b * (p.kc + 8) * 2, s = (size_t)16 * p.rt * (p.kc / w.group + 1) * 4;
-    const size_t t = w.k && b * w.k <= kRowsTm ? (size_t)b * w.k * 4 : 0;
+    const int64_t kp = round_up(w.k, 16);
+    const size_t t = w.k && b * kp <= kRowsTm ? (size_t)b * kp * 4 + 16 : 0;
     p.lds = std::max(x + s + t, (size_t)p.nw * 16 * (16 * p.rt + 1) * 4);
     return true;
 }
@@ -761,7 +862,7 @@ Q4Plan plan_q4(const Q4Weights& w, const void* X, int64_t ldx, int64_t b, int pr
     p.tile = !plan_rows(p, w, b, prec);
     if (p.tile) {
         p.wx = prec == P32 || b <= 64 ? 1 : 2;
-        p.nx = b <= 32 ? 2 : 4;
+        p.nx = b <= 16 ? 1 : b <= 32 ? 2 : 4;
         const int64_t tiles = (w.m + 127) / 128 * ((b + 16 * p.nx * p.wx - 1) / (16 * p.nx * p.wx));
         p.splits = (int)std::min<int64_t>(std::max<int64_t>(1, 512 / tiles), std::max<int64_t>(1, blocks / 4));
         const int e = elem_bytes(prec);
@@ -771,6 +872,7 @@ Q4Plan plan_q4(const Q4Weights& w, const void* X, int64_t ldx, int64_t b, int pr
         if (p.splits > 1) p.part = (size_t)p.splits * b * w.m * 4;
     }
     if (w.k) {
+        const int64_t kp = round_up(w.k, 16);
         p.mid_tw = b <= 16 ? 1 : 4;
         const int64_t groups = (w.k + 127) / 128 * ((b + 16 * p.mid_tw - 1) / (16 * p.mid_tw));
         // enough workgroups for the chip, few partials for their readers
@@ -778,9 +880,9 @@ Q4Plan plan_q4(const Q4Weights& w, const void* X, int64_t ldx, int64_t b, int pr
         s = std::min<int64_t>(s, b <= 2 ? 32 : b <= 16 ? 32 : 64);
         p.mid_chunk = (blocks + s - 1) / s * 128;
         p.mid_splits = (int)((w.n + p.mid_chunk - 1) / p.mid_chunk);
-        p.mid_finish = p.tile || b * p.mid_splits > 64 || b * w.k > kRowsTm;
+        p.mid_finish = p.tile || b * p.mid_splits > 64 || b * kp > kRowsTm;
         p.mid_part = (size_t)p.mid_splits * b * w.k * 4;
-        if (p.mid_finish) p.tm = (size_t)b * w.k * 4;
+        if (p.mid_finish) p.tm = (size_t)b * kp * 4;
     }
     return p;
 }
@@ -808,19 +910,25 @@ hipError_t rows_t(const Q4Plan& p, const Q4Args& a, hipStream_t st) {
     return p.nw == 8 ? launch_rows<T, 1, FL, 8>(p, a, st) : launch_rows<T, 1, FL, 4>(p, a, st);
 }
 
-template <typename T, int WX, int NX, int FL>
+template <typename T, int WX, int NX, int FL, int SB>
 void launch_tile(const Q4Args& a, hipStream_t st) {
     const int tm = (int)((a.m + 127) / 128), tb = (int)((a.b + 16 * NX * WX - 1) / (16 * NX * WX));
     KernelTimer t("q4_tile", st);
-    hipLaunchKernelGGL((k_q4_tile<T, WX, NX, FL>), dim3(xcd_grid((int64_t)tm * tb * a.splits)), dim3(256), 0, st, a, tm, tb);
+    hipLaunchKernelGGL((k_q4_tile<T, WX, NX, FL, SB>), dim3(xcd_grid((int64_t)tm * tb * a.splits)), dim3(256), 0, st, a, tm, tb);
+}
+template <typename T, int FL, int SB>
+void tile_sb(const Q4Plan& p, const Q4Args& a, hipStream_t st) {
+    if constexpr (sizeof(T) == 2) {
+        if (p.wx == 2) return launch_tile<T, 2, 4, FL, SB>(a, st);
+    }
+    if (p.nx == 1) return launch_tile<T, 1, 1, FL, SB>(a, st);
+    if (p.nx == 2) return launch_tile<T, 1, 2, FL, SB>(a, st);
+    launch_tile<T, 1, 4, FL, SB>(a, st);
 }
 template <typename T, int FL>
 void tile_t(const Q4Plan& p, const Q4Args& a, hipStream_t st) {
-    if constexpr (sizeof(T) == 2) {
-        if (p.wx == 2) return launch_tile<T, 2, 4, FL>(a, st);
-    }
-    if (p.nx == 2) return launch_tile<T, 1, 2, FL>(a, st);
-    launch_tile<T, 1, 4, FL>(a, st);
+    if (a.sprec == P32) tile_sb<T, FL, 4>(p, a, st);
+    else tile_sb<T, FL, 2>(p, a, st);
 }
 
 template <typename T, int F>
@@ -849,9 +957,8 @@ hipError_t apply_t(const Q4Weights& w, Q4Args& a, int prec, Workspace& ws, hipSt
         else mid_f<T, 8>(p, w, a, mid, st);
         if (p.mid_finish) {
             KernelTimer t("q4_mid_finish", st);
-            const int64_t count = a.b * w.k;
-            hipLaunchKernelGGL(k_q4_mid_finish, dim3((unsigned)((count + 255) / 256)), dim3(256), 0, st, mid, p.mid_splits,
-                               w.s, w.fprec, w.k, count, Tm);
+            hipLaunchKernelGGL(k_q4_mid_finish, dim3((unsigned)((a.b * a.kp + 255) / 256)), dim3(256), 0, st, mid,
+                               p.mid_splits, w.s, w.fprec, w.k, a.kp, a.b, Tm);
             a.Tm = Tm;
         } else {
             a.Tm = mid;
@@ -907,6 +1014,7 @@ hipError_t launch_q4_apply(const Q4Weights& w, const void* X, int64_t ldx, void*
         a.U = w.U;
         a.s = w.s;
         a.k = w.k;
+        a.kp = round_up(w.k, 16);
         a.fprec = w.fprec;
         a.X = static_cast<const char*>(X) + b0 * ldx * elem_bytes(prec);
         a.ldx = ldx;
