@@ -28,7 +28,6 @@ namespace {
 
 constexpr int kSlab = 1 << 18;           // logits whose bitmap is held at a time
 constexpr float kNegInf = -__builtin_inff();
-constexpr float kLog2e = 1.4426950408889634f;
 
 enum { FORWARD = 0, BOTH = 1, BACKWARD = 2 };
 

@@ -15,6 +15,8 @@ typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
 typedef unsigned uint4v_t __attribute__((ext_vector_type(4)));
 typedef unsigned uint2v_t __attribute__((ext_vector_type(2)));
 
+constexpr float kLog2e = 1.4426950408889634f;
+
 // Conversions round to nearest even; bfloat16 keeps subnormals and NaN.
 template <typename T> __device__ __forceinline__ float to_f32(T x) { return (float)x; }
 template <typename T> __device__ __forceinline__ T from_f32(float x) { return (T)x; }

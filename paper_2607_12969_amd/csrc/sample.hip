@@ -10,9 +10,24 @@
 //   min-p  of those, w >= min_p (the likeliest always stays);
 //   draw   the first index at which the running sum of the kept q passes u S.
 // top-k and top-p keep a prefix of the order by logit: every logit above some
-// v, and the first r of those equal to v.  v and r come from histograms of
-// counts and masses: 2048 bins over z in (-32, 0], then over the bits of the
-// logits inside the bin that holds the cut.
+// v, and the first r of those equal to v.
+//
+// One workgroup of 16 waves per row, wave w the w-th part of it.  The vector units
+// bound it (131072 logits: 0.9 us per instruction and element on one compute
+// unit), so a row is passed as few times as its filters allow, in loops short
+// enough to stay in the instruction cache (a row held in registers, its passes
+// unrolled, ran three times slower), with the row coming from L2 after the first
+// pass:
+//   top-k        maximum; counts over 2048 bins of z in (-32, 0]; the tokens down
+//                to the bin that holds the cut go, in index order, to a list in
+//                LDS, where the rest happens;
+//   top-p alone  maximum; masses over the bins; the values in the bin of the cut
+//                to LDS, where v and r are found; kept mass of each part; the draw
+//                inside one part;
+//   neither      maximum; kept mass; draw.
+// Inside a bin, v comes from histograms over the bits of the values.  What does not
+// fit its list (thousands of equal logits, say), and rows with an infinite
+// maximum, find v by histograms over the row itself.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -23,53 +38,40 @@ namespace lrc {
 
 namespace {
 
+typedef unsigned long long u64;
 constexpr int kBins = 2048;
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
+constexpr int kPart = 512;               // list entries of a wave
 constexpr float kNegInf = -__builtin_inff();
 
-// Order of binary32 values as unsigned integers (no NaN; -0 just below 0 is
-// folded onto 0 by the caller).
+// Order of binary32 values as unsigned integers (no NaN; -0 counts as 0).
 __device__ __forceinline__ unsigned key_of(float x) {
-    const unsigned u = __float_as_uint(x);
+    const unsigned u = __float_as_uint(x + 0.0f);
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 __device__ __forceinline__ float of_key(unsigned k) {
     return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k);
 }
 
-
-
-// A logit as the draw sees it: NaN counts as -infinity, -0 as 0.
-__device__ __forceinline__ float logit(float x) { return x != x ? kNegInf : x + 0.0f; }
-
-// kVec consecutive logits from index i on; -infinity past the row's end.
-template <typename T, bool VEC>
-__device__ __forceinline__ void load_logits(const T* row, int64_t i, int64_t V, float (&l)[kVec<T>]) {
-    if (VEC && i + kVec<T> <= V) {
-        typedef T vec_t __attribute__((ext_vector_type(kVec<T>)));
-        const vec_t v = *reinterpret_cast<const vec_t*>(row + i);
-#pragma unroll
-        for (int e = 0; e < kVec<T>; ++e) l[e] = logit((float)v[e]);
-    } else {
-#pragma unroll
-        for (int e = 0; e < kVec<T>; ++e) l[e] = i + e < V ? logit((float)row[i + e]) : kNegInf;
-    }
-}
-
+// NaN logits fail every comparison below and weigh (unsigned)NaN = 0.
 struct Weigh {
     float M, c;
-    __device__ __forceinline__ float z(float l) const { return l == M ? 0.0f : (l - M) * c; }
+    __device__ __forceinline__ float z(float l) const { return (l - M) * c; }
     __device__ __forceinline__ float w(float l) const { return __builtin_amdgcn_exp2f(z(l)); }
     static __device__ __forceinline__ unsigned q(float w) { return (unsigned)(w * 2147483648.0f); }
 };
+// The row whose maximum is +infinity: only that logit weighs.
+struct WeighInf {
+    __device__ __forceinline__ float z(float l) const { return l == __builtin_inff() ? 0.0f : kNegInf; }
+    __device__ __forceinline__ float w(float l) const { return l == __builtin_inff() ? 1.0f : 0.0f; }
+};
+__device__ __forceinline__ int bin_of(float z) { return (int)(z * -64.0f); }       // z in [-31, 0]
 
 __device__ __forceinline__ float scale_of(float T) {
-    return __builtin_fminf(__builtin_fmaxf((1.0f / T) * 1.4426950408889634f, 1.17549435e-38f), 3.4028234663852886e38f);
+    return __builtin_fminf(__builtin_fmaxf((1.0f / T) * kLog2e, 1.17549435e-38f), 3.4028234663852886e38f);
 }
 
-typedef unsigned long long u64;
-
-__device__ __forceinline__ u64 wave_add(u64 x) {
+template <typename X> __device__ __forceinline__ X wave_add(X x) {
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) x += __shfl_xor(x, off, 64);
     return x;
@@ -78,6 +80,10 @@ __device__ __forceinline__ u64 wave_add(u64 x) {
 struct Shared {
     unsigned count[kBins];
     u64 mass[kBins];
+    float lv[kWaves * kPart];            // list: logits ...
+    unsigned li[kWaves * kPart];              // ... and, for top-k, indices
+    int ln[kWaves];                      // entries of each wave
+    int n;                               // entries without order
     u64 red[kWaves];
     unsigned redc[kWaves];
     float redf[kWaves];
@@ -86,6 +92,14 @@ struct Shared {
     unsigned beforec;
     unsigned kmin, kmax;
 };
+
+__device__ __forceinline__ void clear_bins(Shared& s) {
+    for (int b = threadIdx.x; b < kBins; b += kThreads) {
+        s.count[b] = 0;
+        s.mass[b] = 0;
+    }
+    __syncthreads();
+}
 
 // The first bin at which the running count (by_count) or mass reaches
 // `target` (>= 1), and the running count and mass before it.  Every thread
@@ -130,276 +144,487 @@ __device__ __forceinline__ void find_bin(Shared& s, bool by_count, u64 target, i
     __syncthreads();
 }
 
-// Visits the row: wave w takes the contiguous part [w L, (w + 1) L), blocks of
-// 64 kVec logits, a lane kVec consecutive ones.
-template <typename T, bool VEC, typename F>
-__device__ __forceinline__ void visit(const T* row, int64_t V, int64_t L, F&& f) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t end = std::min(V, (wave + 1) * L);
-    for (int64_t i = wave * L; i < end; i += 64 * kVec<T>) {
-        float l[kVec<T>];
-        load_logits<T, VEC>(row, i + lane * kVec<T>, V, l);
-        f(i, l);
-    }
-}
+struct Cut {
+    float v;             // all logits above v ...
+    u64 above;           // ... their mass ...
+    unsigned count;      // ... and number
+};
 
-// The cut at `target` in the order by logit: all logits above v, and of those
-// equal to v as many as reach the target.  above: mass above v.  qv: weight of
-// v, ties: tokens equal to v.  false when the row does not reach the target.
-template <typename T, bool VEC>
-__device__ bool select(Shared& s, const T* row, int64_t V, int64_t L, const Weigh& wt, bool by_count, u64 target,
-                       float& v, u64& above, unsigned& countabove) {
+// A row in memory: wave w takes the contiguous part [w L, (w + 1) L) in blocks of 64
+// vectors, a lane kVec consecutive logits of each.
+template <typename T> struct Row {
+    static constexpr int E = kVec<T>, B = 64 * E;
+    const T* row;
+    unsigned V, L;
+    // f(index of the lane's first logit, logits) for the blocks of [begin, end), in
+    // order; four loads at a time
+    template <typename F> __device__ __forceinline__ void visit(unsigned begin, unsigned end, F&& f) const {
+        const unsigned lane = (threadIdx.x & 63) * E;
+        unsigned i = begin;
+        for (; i + 4 * B <= end; i += 4 * B) {
+            uint4v_t v[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[q] = load16(row + (size_t)i + q * B + lane);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) f(i + q * B + lane, v[q]);
+        }
+#pragma unroll 1
+        for (; i < end; i += B) f(i + lane, load_row16(row, (int64_t)i + lane, (int64_t)V));
+    }
+    __device__ __forceinline__ unsigned begin(int wave) const { return (unsigned)std::min<uint64_t>(V, (uint64_t)wave * L); }
+    // every logit of this wave's part
+    template <typename F> __device__ __forceinline__ void each(F&& f) const {
+        const int wave = threadIdx.x >> 6;
+        visit(begin(wave), begin(wave + 1), [&](unsigned, const uint4v_t& v) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) f(elem<T>(v, e));
+        });
+    }
+};
+
+// Entries begin, begin + step, .. below end of the list in LDS.
+struct List {
+    const float* lv;
+    int begin, end, step;
+    template <typename F> __device__ __forceinline__ void each(F&& f) const {
+        for (int e = begin; e < end; e += step) f(lv[e]);
+    }
+};
+
+// The cut inside bin `zb`, with `before` mass and `beforec` tokens in the bins
+// above it; `from` holds every logit of the bin, and may hold others.
+template <typename W, typename From>
+__device__ __noinline__ Cut refine(Shared& s, W wt, bool by_count, u64 target, int zb, u64 before, unsigned beforec,
+                                   From from) {
     const int t = threadIdx.x;
-    auto clear = [&] {
-        for (int b = t; b < kBins; b += kThreads) {
-            s.count[b] = 0;
-            s.mass[b] = 0;
-        }
-        if (t == 0) {
-            s.kmin = ~0u;
-            s.kmax = 0u;
-        }
-        __syncthreads();
-    };
-    auto zbin = [](float z) { return std::min((int)(z * -64.0f), kBins - 1); };
-    clear();
-    visit<T, VEC>(row, V, L, [&](int64_t, const float (&l)[kVec<T>]) {
-#pragma unroll
-        for (int e = 0; e < kVec<T>; ++e) {
-            const float z = wt.z(l[e]);
-            if (z >= -31.0f) {
-                const int b = zbin(z);
-                atomicAdd(&s.count[b], 1u);
-                atomicAdd(&s.mass[b], (u64)Weigh::q(__builtin_amdgcn_exp2f(z)));
-            }
-        }
-    });
-    __syncthreads();
-    int bin;
-    u64 before;
-    unsigned beforec;
-    find_bin(s, by_count, target, bin, before, beforec);
-    if (bin < 0) return false;
-    const int zb = bin;
-    // range of keys inside the bin
-    auto inside = [&](float l) {
-        const float z = wt.z(l);
-        return z >= -31.0f && zbin(z) == zb;
-    };
     unsigned lo = ~0u, hi = 0u;
-    visit<T, VEC>(row, V, L, [&](int64_t, const float (&l)[kVec<T>]) {
-#pragma unroll
-        for (int e = 0; e < kVec<T>; ++e)
-            if (inside(l[e])) {
-                const unsigned k = key_of(l[e]);
-                lo = std::min(lo, k);
-                hi = std::max(hi, k);
-            }
+    from.each([&](float l) {
+        const float z = wt.z(l);
+        if (z >= -31.0f && bin_of(z) == zb) {
+            const unsigned k = key_of(l);
+            lo = std::min(lo, k);
+            hi = std::max(hi, k);
+        }
     });
     if (t == 0) {
         s.kmin = ~0u;
         s.kmax = 0u;
     }
     __syncthreads();
-    atomicMin(&s.kmin, lo);
-    atomicMax(&s.kmax, hi);
+    if (lo <= hi) {
+        atomicMin(&s.kmin, lo);
+        atomicMax(&s.kmax, hi);
+    }
     __syncthreads();
     lo = s.kmin;
     hi = s.kmax;
-    __syncthreads();
-    u64 base = before;
-    unsigned basec = beforec;
     while (lo < hi) {
         // bins of 2^sh keys from the top
         int sh = 0;
         while (((hi - lo) >> sh) >= (unsigned)kBins) ++sh;
-        clear();
-        visit<T, VEC>(row, V, L, [&](int64_t, const float (&l)[kVec<T>]) {
-#pragma unroll
-            for (int e = 0; e < kVec<T>; ++e) {
-                const unsigned k = key_of(l[e]);
-                if (k >= lo && k <= hi) {
-                    const unsigned b = (hi - k) >> sh;
-                    atomicAdd(&s.count[b], 1u);
-                    atomicAdd(&s.mass[b], (u64)Weigh::q(wt.w(l[e])));
-                }
+        __syncthreads();
+        clear_bins(s);
+        from.each([&](float l) {
+            const unsigned k = key_of(l);
+            if (l == l && k >= lo && k <= hi) {
+                const unsigned b = (hi - k) >> sh;
+                atomicAdd(&s.count[b], 1u);
+                if (!by_count) atomicAdd(&s.mass[b], (u64)Weigh::q(wt.w(l)));
             }
         });
         __syncthreads();
-        find_bin(s, by_count, target - (by_count ? basec : base), bin, before, beforec);
+        int bin;
+        u64 m;
+        unsigned c;
+        find_bin(s, by_count, target - (by_count ? beforec : before), bin, m, c);
         if (bin < 0) break;
-        base += before;
-        basec += beforec;
+        before += m;
+        beforec += c;
         const unsigned top = hi - ((unsigned)bin << sh);
         lo = std::max(lo, top - ((1u << sh) - 1u));
         hi = top;
     }
-    v = of_key(hi);
-    above = base;
-    countabove = basec;
-    return true;
+    __syncthreads();
+    return Cut{of_key(hi), before, beforec};
 }
 
-}  // namespace
-
-template <typename T, bool VEC>
-__global__ __launch_bounds__(kThreads) void k_sample_row(SampleArgs a, int64_t L) {
-    __shared__ Shared s;
-    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-    const int64_t r = blockIdx.x, V = a.vocab;
-    const T* row = static_cast<const T*>(a.logits) + r * a.ld;
-
-    float M = kNegInf;
-    visit<T, VEC>(row, V, L, [&](int64_t, const float (&l)[kVec<T>]) {
-#pragma unroll
-        for (int e = 0; e < kVec<T>; ++e) M = __builtin_fmaxf(M, l[e]);
-    });
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) M = __builtin_fmaxf(M, __shfl_xor(M, off, 64));
-    if (lane == 0) s.redf[wave] = M;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) M = __builtin_fmaxf(M, s.redf[w]);
-    if (M == kNegInf) {          // nothing to draw from
-        if (t == 0) a.tokens[r] = -1;
-        return;
+// Kept tokens: logits above v and the first `ties` equal to v, of weight at least
+// floor_w.
+template <typename W> struct Kept {
+    W wt;
+    float v, floor_w;
+    u64 ties, qv;        // qv: weight of a tie
+    bool all;            // no cut
+    __device__ __forceinline__ void cut(float at, u64 t) {
+        v = at;
+        ties = t;
+        all = false;
+        const float w = wt.w(at);
+        qv = w >= floor_w ? Weigh::q(w) : 0u;
     }
-    const float temp = a.temperature ? a.temperature[r] : 1.0f;
-    const bool greedy = !(temp > 0.0f);
-    Weigh wt{M, greedy ? 1.0f : scale_of(temp)};
-    float v = kNegInf, floor_w = 0.0f;
-    u64 ties = ~0ull;            // kept tokens equal to v
-    if (greedy) {
-        v = M;
-        ties = 1;
-    } else {
-        const int64_t k = a.top_k ? a.top_k[r] : 0;
-        const float p = a.top_p ? a.top_p[r] : 1.0f, mp = a.min_p ? a.min_p[r] : 0.0f;
-        if (mp > 0.0f) floor_w = std::min(mp, 1.0f);
-        u64 mass = 0;
-        bool have = false;
-        if (k > 0 && k < V) {
-            float vk;
-            u64 above;
-            unsigned ca;
-            if (select<T, VEC>(s, row, V, L, wt, true, (u64)k, vk, above, ca)) {
-                v = vk;
-                ties = (u64)k - ca;
-                mass = above + ties * Weigh::q(wt.w(vk));
-                have = true;
-            }
-        }
-        if (p < 1.0f) {
-            if (!have) {
-                u64 m = 0;
-                visit<T, VEC>(row, V, L, [&](int64_t, const float (&l)[kVec<T>]) {
-#pragma unroll
-                    for (int e = 0; e < kVec<T>; ++e) m += Weigh::q(wt.w(l[e]));
-                });
-                m = wave_add(m);
-                if (lane == 0) s.red[wave] = m;
-                __syncthreads();
-                for (int w = 0; w < kWaves; ++w) mass += s.red[w];
-                __syncthreads();
-            }
-            const double P = __builtin_ceil((double)p * (double)mass);
-            const u64 target = P >= 1.0 ? (u64)P : 1ull;
-            float vp;
-            u64 above;
-            unsigned ca;
-            if (select<T, VEC>(s, row, V, L, wt, false, target, vp, above, ca)) {
-                const u64 q = Weigh::q(wt.w(vp));
-                v = vp;
-                ties = (target - above + q - 1) / q;
-            }
-        }
-    }
-    // kept mass of each wave's part
-    u64 sum = 0;
-    unsigned eq = 0;
-    const u64 qv = v == kNegInf ? 0 : Weigh::q(wt.w(v)) * (u64)(wt.w(v) >= floor_w);
-    auto kept_above = [&](float l) {
+    __device__ __forceinline__ unsigned above(float l) const {
         const float w = wt.w(l);
-        return l > v && w >= floor_w ? Weigh::q(w) : 0u;
-    };
-    visit<T, VEC>(row, V, L, [&](int64_t, const float (&l)[kVec<T>]) {
-#pragma unroll
-        for (int e = 0; e < kVec<T>; ++e) {
-            sum += kept_above(l[e]);
-            eq += l[e] == v && v != kNegInf;
-        }
-    });
+        return (all || l > v) && w >= floor_w ? Weigh::q(w) : 0u;
+    }
+    __device__ __forceinline__ bool tied(float l) const { return !all && l == v; }
+    // mass of `count` ties after `from` earlier ones
+    __device__ __forceinline__ u64 of_ties(u64 from, u64 count) const {
+        return from >= ties ? 0ull : qv * std::min(count, ties - from);
+    }
+};
+
+// Which wave's part holds the draw.  sum, eq: this lane's kept mass above v and
+// ties.  FIRST: the target is u times the total; else it is given, with the mass
+// and the ties before the parts in run and run_eq.  Leaves in run and run_eq those
+// before the part it returns (-1: none).
+template <bool FIRST, typename W>
+__device__ __forceinline__ int find_part(Shared& s, const Kept<W>& k, u64 sum, unsigned eq, float u, u64& target, u64& run,
+                                         u64& run_eq) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     sum = wave_add(sum);
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) eq += __shfl_xor(eq, off, 64);
+    eq = wave_add(eq);
     __syncthreads();
     if (lane == 0) {
         s.red[wave] = sum;
         s.redc[wave] = eq;
     }
     __syncthreads();
-    u64 S = 0, before = 0, eqb = 0, mine = 0, eqmine = 0;
-    for (int w = 0; w < kWaves; ++w) {
-        const u64 c = s.redc[w], left = ties > eqb ? ties - eqb : 0;
-        const u64 add = s.red[w] + qv * std::min(c, left);
-        if (w < wave) before += add;
-        if (w == wave) {
-            mine = add;
-            eqmine = eqb;
+    if (FIRST) {
+        u64 S = 0, c = 0;
+        for (int w = 0; w < kWaves; ++w) {
+            S += s.red[w] + k.of_ties(c, s.redc[w]);
+            c += s.redc[w];
         }
-        S += add;
-        eqb += c;
+        const double td = (double)(u > 0.0f ? u : 0.0f) * (double)S;
+        target = td >= (double)S ? S - 1 : (u64)td;
+        run = run_eq = 0;
     }
-    const float u = greedy || !(a.u[r] > 0.0f) ? 0.0f : a.u[r];
-    const double td = (double)u * (double)S;
-    const u64 target = td >= (double)S ? S - 1 : (u64)td;
-    if (target < before || target >= before + mine) return;
-    // this wave's part holds the token: block by block, then lane by lane
-    u64 run = before, run_eq = eqmine;
-    const int64_t end = std::min(V, (wave + 1) * L);
-    for (int64_t i = wave * L; i < end; i += 64 * kVec<T>) {
-        float l[kVec<T>];
-        load_logits<T, VEC>(row, i + lane * kVec<T>, V, l);
-        u64 ps = 0;
-        unsigned pe = 0;
+    for (int w = 0; w < kWaves; ++w) {
+        const u64 add = s.red[w] + k.of_ties(run_eq, s.redc[w]);
+        if (target < run + add) return w;
+        run += add;
+        run_eq += s.redc[w];
+    }
+    return -1;
+}
+
+// Writes the token if it is among this wave's E logits a lane; else moves run and
+// run_eq past them and returns true.
+template <int E, typename W>
+__device__ __forceinline__ bool find_lane(const Kept<W>& k, u64 target, u64& run, u64& run_eq, const float (&l)[E],
+                                          const unsigned (&at)[E], int64_t* token) {
+    const int lane = threadIdx.x & 63;
+    u64 is = 0;
+    unsigned ie = 0;
 #pragma unroll
-        for (int e = 0; e < kVec<T>; ++e) {
-            ps += kept_above(l[e]);
-            pe += l[e] == v && v != kNegInf;
-        }
-        u64 is = ps;
-        unsigned ie = pe;
+    for (int e = 0; e < E; ++e) {
+        is += k.above(l[e]);
+        ie += k.tied(l[e]);
+    }
+    const u64 ps = is;
+    const unsigned pe = ie;
 #pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            const u64 os = __shfl_up(is, off, 64);
-            const unsigned oe = __shfl_up(ie, off, 64);
-            if (lane >= off) {
-                is += os;
-                ie += oe;
-            }
+    for (int off = 1; off < 64; off <<= 1) {
+        const u64 os = __shfl_up(is, off, 64);
+        const unsigned oe = __shfl_up(ie, off, 64);
+        if (lane >= off) {
+            is += os;
+            ie += oe;
         }
-        auto kept_eq = [&](u64 from, u64 count) {      // of `count` ties after `from` earlier ones
-            return from >= ties ? 0ull : std::min(count, ties - from);
-        };
-        const u64 total = __shfl(is, 63, 64), totale = __shfl(ie, 63, 64);
-        const u64 block = total + qv * kept_eq(run_eq, totale);
-        if (target < run + block) {
-            u64 at = run + is - ps + qv * kept_eq(run_eq, ie - pe);
-            u64 ne = run_eq + ie - pe;
-#pragma unroll
-            for (int e = 0; e < kVec<T>; ++e) {
-                u64 add = kept_above(l[e]);
-                if (l[e] == v && v != kNegInf) {
-                    if (ne < ties) add += qv;
-                    ++ne;
-                }
-                if (target >= at && target < at + add) a.tokens[r] = i + lane * kVec<T> + e;
-                at += add;
-            }
-            return;
-        }
+    }
+    const u64 total = __shfl(is, 63, 64), totale = __shfl(ie, 63, 64);
+    const u64 block = total + k.of_ties(run_eq, totale);
+    if (target >= run + block) {
         run += block;
         run_eq += totale;
+        return true;
+    }
+    u64 ne = run_eq + ie - pe, here = run + is - ps + k.of_ties(run_eq, ie - pe);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        u64 add = k.above(l[e]);
+        if (k.tied(l[e])) {
+            if (ne < k.ties) add += k.qv;
+            ++ne;
+        }
+        if (target >= here && target < here + add) *token = at[e];
+        here += add;
+    }
+    return false;
+}
+
+// The draw over the row: kept mass of each wave's part, then of 16 parts of the
+// one that holds the token, then that part itself.
+template <typename T, typename W>
+__device__ __forceinline__ void draw_row(Shared& s, const Row<T>& row, const Kept<W>& k, float u, int64_t* token) {
+    constexpr int E = kVec<T>;
+    const int wave = threadIdx.x >> 6;
+    u64 target = 0, run, run_eq, sum = 0;
+    unsigned eq = 0;
+    auto add = [&](float l) {
+        sum += k.above(l);
+        eq += k.tied(l);
+    };
+    row.each(add);
+    const int part = find_part<true>(s, k, sum, eq, u, target, run, run_eq);
+    if (part < 0) return;
+    const unsigned from = row.begin(part), to = row.begin(part + 1);
+    const unsigned sub = ((to - from + kWaves * row.B - 1) / (kWaves * row.B)) * row.B;
+    auto sub_begin = [&](int w) { return (unsigned)std::min<uint64_t>(to, (uint64_t)from + (uint64_t)w * sub); };
+    sum = 0;
+    eq = 0;
+    row.visit(sub_begin(wave), sub_begin(wave + 1), [&](unsigned, const uint4v_t& v) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) add(elem<T>(v, e));
+    });
+    const int w = find_part<false>(s, k, sum, eq, u, target, run, run_eq);
+    if (wave != w) return;
+    const unsigned lane = (threadIdx.x & 63) * E, end = sub_begin(w + 1);
+#pragma unroll 1
+    for (unsigned i = sub_begin(w); i < end; i += row.B) {
+        const uint4v_t v = load_row16(row.row, (int64_t)i + lane, (int64_t)row.V);
+        float l[E];
+        unsigned at[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            l[e] = elem<T>(v, e);
+            at[e] = i + lane + e;
+        }
+        if (!find_lane<E>(k, target, run, run_eq, l, at, token)) return;
+    }
+}
+
+// Number of smallest weights that reach `target` from `above`.
+__device__ __forceinline__ u64 ties_to(u64 target, u64 above, u64 q) { return (target - above + q - 1) / q; }
+__device__ __forceinline__ u64 mass_target(float p, u64 mass) {
+    const double P = __builtin_ceil((double)p * (double)mass);
+    return P >= 1.0 ? (u64)P : 1ull;
+}
+
+// Any filters, all passes over the row.
+template <typename T, typename W>
+__device__ __noinline__ void sample_any(Shared& s, Row<T> row, W wt, int64_t k, float p, float floor_w, float u,
+                                        int64_t* token) {
+    Kept<W> kept{wt, 0.0f, floor_w, 0, 0, true};
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    Cut cut;
+    auto select = [&](bool by_count, u64 target) {
+        __syncthreads();
+        clear_bins(s);
+        row.each([&](float l) {
+            const float z = wt.z(l);
+            if (z >= -31.0f) {
+                atomicAdd(&s.count[bin_of(z)], 1u);
+                atomicAdd(&s.mass[bin_of(z)], (u64)Weigh::q(wt.w(l)));
+            }
+        });
+        __syncthreads();
+        int bin;
+        u64 before;
+        unsigned beforec;
+        find_bin(s, by_count, target, bin, before, beforec);
+        if (bin < 0) return false;
+        cut = refine(s, wt, by_count, target, bin, before, beforec, row);
+        return true;
+    };
+    if (k > 0 && k < (int64_t)row.V && select(true, (u64)k)) kept.cut(cut.v, (u64)k - cut.count);
+    if (p < 1.0f) {
+        // mass of what top-k keeps
+        u64 m = 0;
+        row.each([&](float l) {
+            if (kept.all || l > kept.v) m += Weigh::q(wt.w(l));
+        });
+        m = wave_add(m);
+        __syncthreads();
+        if (lane == 0) s.red[wave] = m;
+        __syncthreads();
+        u64 mass = kept.all ? 0 : kept.ties * Weigh::q(wt.w(kept.v));
+        for (int w = 0; w < kWaves; ++w) mass += s.red[w];
+        const u64 target = mass_target(p, mass);
+        if (select(false, target)) kept.cut(cut.v, ties_to(target, cut.above, Weigh::q(wt.w(cut.v))));
+    }
+    draw_row(s, row, kept, u, token);
+}
+
+}  // namespace
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_sample_row(SampleArgs a, unsigned L) {
+    __shared__ Shared s;
+    constexpr int E = kVec<T>;
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    const int64_t r = blockIdx.x;
+    const unsigned V = (unsigned)a.vocab;
+    const Row<T> row{static_cast<const T*>(a.logits) + r * a.ld, V, L};
+    const float temp = a.temperature ? a.temperature[r] : 1.0f, u = a.u[r];
+    const int64_t k = a.top_k ? a.top_k[r] : 0;
+    const float p = a.top_p ? a.top_p[r] : 1.0f, mp = a.min_p ? a.min_p[r] : 0.0f;
+    for (int b = t; b < kBins; b += kThreads) {
+        s.count[b] = 0;
+        s.mass[b] = 0;
+    }
+    if (t == 0) s.n = 0;
+
+    float M = kNegInf;
+    row.each([&](float l) { M = __builtin_fmaxf(M, l); });
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) M = __builtin_fmaxf(M, __shfl_xor(M, off, 64));
+    if (lane == 0) s.redf[wave] = M;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) M = __builtin_fmaxf(M, s.redf[w]);
+    int64_t* token = a.tokens + r;
+    if (M == kNegInf) {          // nothing to draw from
+        if (t == 0) *token = -1;
+        return;
+    }
+    if (!(temp > 0.0f)) {        // the first logit equal to the maximum
+        unsigned at = V;
+        row.visit(row.begin(wave), row.begin(wave + 1), [&](unsigned i, const uint4v_t& v) {
+#pragma unroll
+            for (int e = E - 1; e >= 0; --e)
+                if (elem<T>(v, e) == M) at = std::min(at, i + e);
+        });
+#pragma unroll
+        for (int off = 32; off >= 1; off >>= 1) at = std::min(at, __shfl_xor(at, off, 64));
+        if (lane == 0) s.redc[wave] = at;
+        __syncthreads();
+        if (t == 0) {
+            for (int w = 1; w < kWaves; ++w) at = std::min(at, s.redc[w]);
+            *token = at;
+        }
+        return;
+    }
+    const float floor_w = mp > 0.0f ? std::min(mp, 1.0f) : 0.0f;
+    if (M == __builtin_inff()) {
+        sample_any(s, row, WeighInf{}, k, p, floor_w, u, token);
+        return;
+    }
+    const Weigh wt{M, scale_of(temp)};
+    Kept<Weigh> kept{wt, 0.0f, floor_w, 0, 0, true};
+    const bool topk = k > 0 && k < (int64_t)V, topp = p < 1.0f;
+    int bin;
+    u64 before;
+    unsigned beforec;
+    if (!topk) {
+        if (topp) {
+            // masses; their total is the mass that p is of
+            row.each([&](float l) {
+                const float z = wt.z(l);
+                if (z >= -31.0f) atomicAdd(&s.mass[bin_of(z)], (u64)Weigh::q(__builtin_amdgcn_exp2f(z)));
+            });
+            __syncthreads();
+            const u64 m = wave_add(s.mass[2 * t] + s.mass[2 * t + 1]);
+            if (lane == 0) s.red[wave] = m;
+            __syncthreads();
+            u64 mass = 0;
+            for (int w = 0; w < kWaves; ++w) mass += s.red[w];
+            __syncthreads();
+            const u64 target = mass_target(p, mass);
+            find_bin(s, false, target, bin, before, beforec);
+            // the values in that bin, in any order
+            row.each([&](float l) {
+                const float z = wt.z(l);
+                if (z >= -31.0f && bin_of(z) == bin) {
+                    const int at = atomicAdd(&s.n, 1);
+                    if (at < kWaves * kPart) s.lv[at] = l;
+                }
+            });
+            __syncthreads();
+            const int n = s.n;
+            if (bin < 0 || n > kWaves * kPart) {
+                sample_any(s, row, wt, 0, p, floor_w, u, token);
+                return;
+            }
+            const Cut cut = refine(s, wt, false, target, bin, before, 0u, List{s.lv, t, n, kThreads});
+            kept.cut(cut.v, ties_to(target, cut.above, Weigh::q(wt.w(cut.v))));
+        }
+        draw_row(s, row, kept, u, token);
+        return;
+    }
+    // top-k: counts, then the tokens down to the bin of the k-th, in index order
+    row.each([&](float l) {
+        const float z = wt.z(l);
+        if (z >= -31.0f) atomicAdd(&s.count[bin_of(z)], 1u);
+    });
+    __syncthreads();
+    find_bin(s, true, (u64)k, bin, before, beforec);
+    const int last = bin < 0 ? kBins : bin;          // fewer than k tokens weigh anything: all of them
+    int n = 0;
+    row.visit(row.begin(wave), row.begin(wave + 1), [&](unsigned i, const uint4v_t& v) {
+        unsigned mask = 0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const float z = wt.z(elem<T>(v, e));
+            if (z >= -31.0f && bin_of(z) <= last) mask |= 1u << e;
+        }
+        if (__builtin_amdgcn_ballot_w64(mask != 0)) {
+            const int c = __builtin_popcount(mask);
+            int at = c;
+#pragma unroll
+            for (int off = 1; off < 64; off <<= 1) {
+                const int o = __shfl_up(at, off, 64);
+                if (lane >= off) at += o;
+            }
+            const int total = __shfl(at, 63, 64);
+            at += n - c;
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (mask >> e & 1u) {
+                    if (at < kPart) {
+                        s.lv[wave * kPart + at] = elem<T>(v, e);
+                        s.li[wave * kPart + at] = i + e;
+                    }
+                    ++at;
+                }
+            n += total;
+        }
+    });
+    if (lane == 0) s.ln[wave] = n;
+    __syncthreads();
+    bool fits = true;
+    for (int w = 0; w < kWaves; ++w) fits &= s.ln[w] <= kPart;
+    if (!fits) {
+        sample_any(s, row, wt, k, p, floor_w, u, token);
+        return;
+    }
+    const List list{s.lv, wave * kPart + lane, wave * kPart + n, 64};
+    if (bin >= 0) {
+        const Cut cut = refine(s, wt, true, (u64)k, bin, 0, beforec, list);
+        kept.cut(cut.v, (u64)k - cut.count);
+    }
+    if (topp) {
+        u64 m = 0;
+        list.each([&](float l) {
+            if (kept.all || l > kept.v) m += Weigh::q(wt.w(l));
+        });
+        m = wave_add(m);
+        __syncthreads();
+        if (lane == 0) s.red[wave] = m;
+        clear_bins(s);
+        u64 mass = kept.all ? 0 : kept.ties * Weigh::q(wt.w(kept.v));
+        for (int w = 0; w < kWaves; ++w) mass += s.red[w];
+        const u64 target = mass_target(p, mass);
+        list.each([&](float l) { atomicAdd(&s.mass[bin_of(wt.z(l))], (u64)Weigh::q(wt.w(l))); });
+        __syncthreads();
+        find_bin(s, false, target, bin, before, beforec);
+        if (bin >= 0) {
+            const Cut cut = refine(s, wt, false, target, bin, before, 0u, list);
+            kept.cut(cut.v, ties_to(target, cut.above, Weigh::q(wt.w(cut.v))));
+        }
+    }
+    u64 target = 0, run, run_eq, sum = 0;
+    unsigned eq = 0;
+    list.each([&](float l) {
+        sum += kept.above(l);
+        eq += kept.tied(l);
+    });
+    if (find_part<true>(s, kept, sum, eq, u, target, run, run_eq) != wave) return;
+    for (int e0 = 0; e0 < n; e0 += 64) {
+        const int e = wave * kPart + e0 + lane;
+        const float l[1] = {e0 + lane < n ? s.lv[e] : __builtin_nanf("")};
+        const unsigned at[1] = {e0 + lane < n ? s.li[e] : 0u};
+        if (!find_lane<1>(kept, target, run, run_eq, l, at, token)) return;
     }
 }
 
@@ -407,10 +632,8 @@ size_t sample_workspace_bytes(const SampleArgs&) { return 0; }
 
 template <typename T>
 static void launch_rows(const SampleArgs& a, hipStream_t st) {
-    const bool vec = reinterpret_cast<uintptr_t>(a.logits) % 16 == 0 && a.ld * sizeof(T) % 16 == 0;
     const int64_t L = round_up((a.vocab + kWaves - 1) / kWaves, 64 * kVec<T>);
-    auto* kern = vec ? k_sample_row<T, true> : k_sample_row<T, false>;
-    hipLaunchKernelGGL(kern, dim3((unsigned)a.rows), dim3(kThreads), 0, st, a, L);
+    hipLaunchKernelGGL(k_sample_row<T>, dim3((unsigned)a.rows), dim3(kThreads), 0, st, a, (unsigned)L);
 }
 
 hipError_t launch_sample(const SampleArgs& a, Workspace&, hipStream_t st) {
