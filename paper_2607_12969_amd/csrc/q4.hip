@@ -512,20 +512,22 @@ __global__ __launch_bounds__(64 * NW) void k_q4_rows(Q4Args a, int KC) {
 }
 
 // ---- many rows: tiles --------------------------------------------------------
-// One workgroup of 4 waves: 128 rows of W for BT = 16 NX WX rows of X, WX waves
-// along X and 4 / WX along W, a wave 16 NR x 16 NX results.  Steps of 128 columns
+// One workgroup of WX x WR waves: BM = 16 NR WR rows of W for BT = 16 NX WX rows of
+// X, a wave 16 NR x 16 NX results.  Steps of 128 columns
 // move codes and activations straight into one of D LDS buffers, D - 1 steps
 // ahead.  Rows of X (256 bytes a step) have their 16-byte chunks XOR-swizzled by
 // the row on the global side; rows of codes are 64 bytes, a wave's 16 of them one
 // contiguous load.  Codes are widened in registers, once for NX MFMAs.  X: 16-bit
 // planes, 16-byte aligned rows, zero from n on to the next multiple of 128 (codes
 // read past a row's end meet these zeros).
-template <typename T, int WX, int NX> struct TileCfg {
-    static constexpr int P = ActTraits<T>::P, NR = 2 * WX, BT = 16 * NX * WX;
-    static constexpr int XB = P * BT * 256, BUF = XB + 128 * 64;                 // bytes of a step
-    static constexpr int D = BUF <= 20480 ? 4 : BUF <= 24576 ? 3 : 2;
-    static constexpr int EU = D * BUF > 81920 ? 1 : 2;
-    static constexpr int LOADS = P * BT / 16 + 2;                                // of a wave in a step
+template <typename T, int WX, int NX, int WR> struct TileCfg {
+    static constexpr int P = ActTraits<T>::P, NW = WX * WR, NR = WR == 4 && WX == 1 ? 2 : 4;
+    static constexpr int BM = 16 * NR * WR, BT = 16 * NX * WX;                   // rows of W and of X
+    static constexpr int XB = P * BT * 256, BUF = XB + BM * 64;                  // bytes of a step
+    static constexpr int D = BUF <= 20480 ? 4 : BUF <= 24576 || (BUF <= 49152 && NW == 8) ? 3 : 2;
+    static constexpr int EU = NW == 8 || D * BUF <= 81920 ? 2 : 1;
+    static constexpr int XL = BT / 4 / NW, WL = BM / 16 / NW;                    // loads of a wave in a step
+    static constexpr int LOADS = P * XL + WL;
 };
 
 // SB: bytes of a scale.  The two 16-bit types are told apart by a mask, without a branch.
@@ -536,11 +538,11 @@ template <int SB> __device__ __forceinline__ float scale_of_bits(unsigned u, uns
     return __uint_as_float((u << 16 & bf16_mask) | (x & ~bf16_mask));
 }
 
-template <typename T, int WX, int NX, int FL, int SB>
-__global__ __launch_bounds__(256, (TileCfg<T, WX, NX>::EU)) void k_q4_tile(Q4Args a, int tiles_m, int tiles_b) {
+template <typename T, int WX, int NX, int WR, int FL, int SB>
+__global__ __launch_bounds__(64 * WX * WR, (TileCfg<T, WX, NX, WR>::EU)) void k_q4_tile(Q4Args a, int tiles_m, int tiles_b) {
     using Tr = ActTraits<T>;
-    using C = TileCfg<T, WX, NX>;
-    constexpr int P = C::P, NR = C::NR, BT = C::BT, D = C::D;
+    using C = TileCfg<T, WX, NX, WR>;
+    constexpr int P = C::P, NR = C::NR, BT = C::BT, BM = C::BM, D = C::D, XL = C::XL, WL = C::WL;
     __shared__ alignas(16) char S[D * C::BUF];
     const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -550,7 +552,7 @@ __global__ __launch_bounds__(256, (TileCfg<T, WX, NX>::EU)) void k_q4_tile(Q4Arg
     if (lt >= (int64_t)tiles_m * tiles_b * a.splits) return;
     const int64_t split = lt / ((int64_t)tiles_m * tiles_b), q = lt % ((int64_t)tiles_m * tiles_b);
     const int64_t g = q / (8 * tiles_b), gs = std::min<int64_t>(8, tiles_m - 8 * g), in = q - g * 8 * tiles_b;
-    const int64_t i0 = (8 * g + in % gs) * 128, b0 = in / gs * BT;
+    const int64_t i0 = (8 * g + in % gs) * BM, b0 = in / gs * BT;
 
     float4_t acc[NR][NX];
 #pragma unroll
@@ -560,32 +562,31 @@ __global__ __launch_bounds__(256, (TileCfg<T, WX, NX>::EU)) void k_q4_tile(Q4Arg
 
     const int64_t blocks = (a.n + 127) / 128;
     const int64_t k0 = blocks * split / a.splits, k1 = blocks * (split + 1) / a.splits;
-    // wave w moves rows [w BT / 4, (w + 1) BT / 4) of every plane, 4 rows a load,
-    // and rows [32 w, 32 w + 32) of codes, 16 rows a load
-    const char* xs[BT / 16];
+    // a wave moves 4 XL rows of every plane, 4 a load, and 16 WL rows of codes, 16 a load
+    const char* xs[XL];
 #pragma unroll
-    for (int h = 0; h < BT / 16; ++h) {
-        const int r = wave * (BT / 4) + 4 * h + lg;
+    for (int h = 0; h < XL; ++h) {
+        const int r = (wave * XL + h) * 4 + lg;
         xs[h] = static_cast<const char*>(a.X) + (std::min(b0 + r, a.b - 1) * a.ldx + ((lr ^ (r & 15)) * 8)) * 2;
     }
-    const unsigned char* cs[2];
+    const unsigned char* cs[WL];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) cs[h] = a.codes + std::min(i0 + wave * 32 + 16 * h + (lane >> 2), a.m - 1) * a.rb;
+    for (int h = 0; h < WL; ++h) cs[h] = a.codes + std::min(i0 + (wave * WL + h) * 16 + (lane >> 2), a.m - 1) * a.rb;
     auto move = [&](int64_t kb, int buf) {
         char* to = S + buf * C::BUF;
 #pragma unroll
         for (int p = 0; p < P; ++p)
 #pragma unroll
-            for (int h = 0; h < BT / 16; ++h)
+            for (int h = 0; h < XL; ++h)
                 __builtin_amdgcn_global_load_lds(
                     (const __attribute__((address_space(1))) void*)(xs[h] + p * a.plane * 2 + kb * 256),
-                    (__attribute__((address_space(3))) void*)(to + p * BT * 256 + (wave * (BT / 4) + 4 * h) * 256), 16, 0, 0);
+                    (__attribute__((address_space(3))) void*)(to + p * BT * 256 + (wave * XL + h) * 1024), 16, 0, 0);
         const int64_t off = std::min(kb * 64 + (lane & 3) * 16, a.rb - 16);
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < WL; ++h)
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(cs[h] + off),
-                                             (__attribute__((address_space(3))) void*)(to + C::XB + (wave * 32 + 16 * h) * 64), 16,
-                                             0, 0);
+                                             (__attribute__((address_space(3))) void*)(to + C::XB + (wave * WL + h) * 1024), 16, 0,
+                                             0);
     };
     int64_t srow[NR];                                   // where a row's scales begin
 #pragma unroll
@@ -607,6 +608,18 @@ __global__ __launch_bounds__(256, (TileCfg<T, WX, NX>::EU)) void k_q4_tile(Q4Arg
 #pragma unroll
     for (int d = 0; d < D - 1; ++d)
         if (k0 + d < k1) move(k0 + d, d);
+    // A group's products d join acc with its scale, each block of them one block
+    // of products later, the last one in the next step (scale `carry`).
+    float4_t d[NR][NX];
+#pragma unroll
+    for (int f = 0; f < NX; ++f) d[NR - 1][f] = zero_accv<float4_t>();
+    float carry = 0.0f;
+    auto flush = [&](int r, float scale) {
+#pragma unroll
+        for (int f = 0; f < NX; ++f)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) acc[r][f][v] += scale * d[r][f][v];
+    };
     int buf = 0;
     for (int64_t kb = k0; kb < k1; ++kb) {
         // this step has landed when no more than the loads of the D - 2 later ones are on their way
@@ -630,17 +643,20 @@ __global__ __launch_bounds__(256, (TileCfg<T, WX, NX>::EU)) void k_q4_tile(Q4Arg
             for (int t = 0; t < 4; ++t) ww[r][t] = w[t];
             if (FL != 4) transpose4(ww[r]);
         }
-        float4_t d[NR][NX];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            typename Tr::frag x[NX][P];
+        typename Tr::frag x[2][NX][P];
+        auto read = [&](int t) {
 #pragma unroll
             for (int f = 0; f < NX; ++f) {
                 const int r = wx * 16 * NX + 16 * f + lr, ch = (FL == 4 ? lg * 4 + t : t * 4 + lg) ^ (r & 15);
 #pragma unroll
                 for (int p = 0; p < P; ++p)
-                    x[f][p] = *reinterpret_cast<const typename Tr::frag*>(from + p * BT * 256 + r * 256 + ch * 16);
+                    x[t & 1][f][p] = *reinterpret_cast<const typename Tr::frag*>(from + p * BT * 256 + r * 256 + ch * 16);
             }
+        };
+        read(0);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            if (t < 3) read(t + 1);
 #pragma unroll
             for (int r = 0; r < NR; ++r) {
                 const typename Tr::frag wf = Tr::widen(ww[r][t]);
@@ -648,16 +664,17 @@ __global__ __launch_bounds__(256, (TileCfg<T, WX, NX>::EU)) void k_q4_tile(Q4Arg
                 for (int f = 0; f < NX; ++f) {
                     if (t % FL == 0) d[r][f] = zero_accv<float4_t>();
 #pragma unroll
-                    for (int p = P - 1; p >= 0; --p) d[r][f] = Tr::mfma(x[f][p], wf, d[r][f]);
-                    if (t % FL == FL - 1) {
-#pragma unroll
-                        for (int v = 0; v < 4; ++v) acc[r][f][v] += sc[r][t / FL] * d[r][f][v];
-                    }
+                    for (int p = P - 1; p >= 0; --p) d[r][f] = Tr::mfma(x[t & 1][f][p], wf, d[r][f]);
                 }
+                // the block before this one, whose products are done by now
+                if (r == 0 && t % FL == 0) flush(NR - 1, t == 0 ? carry : sc[NR - 1][(t - 1) / FL]);
+                if (r > 0 && t % FL == FL - 1) flush(r - 1, sc[r - 1][t / FL]);
             }
         }
+        carry = sc[NR - 1][4 / FL - 1];
         buf = buf == D - 1 ? 0 : buf + 1;
     }
+    flush(NR - 1, carry);
     if (split == 0 && a.k) {
         int64_t row[NR];
         const float* tm[NX];
@@ -824,7 +841,7 @@ namespace {
 
 struct Q4Plan {
     bool tile;            // k_q4_tile, else k_q4_rows
-    int wx, nx;           // tile: waves along X, 16-row blocks of X per wave
+    int wx, nx, wr;       // tile: waves along X, 16-row blocks of X per wave, waves along W
     int splits;           // tile: parts of the columns
     bool pack;            // tile: activations copied to padded planes
     int64_t ldp;
@@ -863,6 +880,8 @@ Q4Plan plan_q4(const Q4Weights& w, const void* X, int64_t ldx, int64_t b, int pr
     if (p.tile) {
         p.wx = prec == P32 || b <= 64 ? 1 : 2;
         p.nx = b <= 16 ? 1 : b <= 32 ? 2 : 4;
+        p.wr = p.wx == 1 ? 4 : 2;
+        if (p.wx == 2 && (w.m + 255) / 256 * ((b + 127) / 128) >= 256 && !getenv("NO8")) p.wr = 4;
         const int64_t tiles = (w.m + 127) / 128 * ((b + 16 * p.nx * p.wx - 1) / (16 * p.nx * p.wx));
         p.splits = (int)std::min<int64_t>(std::max<int64_t>(1, 512 / tiles), std::max<int64_t>(1, blocks / 4));
         const int e = elem_bytes(prec);
@@ -910,20 +929,23 @@ hipError_t rows_t(const Q4Plan& p, const Q4Args& a, hipStream_t st) {
     return p.nw == 8 ? launch_rows<T, 1, FL, 8>(p, a, st) : launch_rows<T, 1, FL, 4>(p, a, st);
 }
 
-template <typename T, int WX, int NX, int FL, int SB>
+template <typename T, int WX, int NX, int WR, int FL, int SB>
 void launch_tile(const Q4Args& a, hipStream_t st) {
-    const int tm = (int)((a.m + 127) / 128), tb = (int)((a.b + 16 * NX * WX - 1) / (16 * NX * WX));
+    using C = TileCfg<T, WX, NX, WR>;
+    const int tm = (int)((a.m + C::BM - 1) / C::BM), tb = (int)((a.b + C::BT - 1) / C::BT);
     KernelTimer t("q4_tile", st);
-    hipLaunchKernelGGL((k_q4_tile<T, WX, NX, FL, SB>), dim3(xcd_grid((int64_t)tm * tb * a.splits)), dim3(256), 0, st, a, tm, tb);
+    hipLaunchKernelGGL((k_q4_tile<T, WX, NX, WR, FL, SB>), dim3(xcd_grid((int64_t)tm * tb * a.splits)),
+                       dim3(64 * C::NW), 0, st, a, tm, tb);
 }
 template <typename T, int FL, int SB>
 void tile_sb(const Q4Plan& p, const Q4Args& a, hipStream_t st) {
     if constexpr (sizeof(T) == 2) {
-        if (p.wx == 2) return launch_tile<T, 2, 4, FL, SB>(a, st);
+        if (p.wx == 2 && p.wr == 4) return launch_tile<T, 2, 4, 4, FL, SB>(a, st);
+        if (p.wx == 2) return launch_tile<T, 2, 4, 2, FL, SB>(a, st);
     }
-    if (p.nx == 1) return launch_tile<T, 1, 1, FL, SB>(a, st);
-    if (p.nx == 2) return launch_tile<T, 1, 2, FL, SB>(a, st);
-    launch_tile<T, 1, 4, FL, SB>(a, st);
+    if (p.nx == 1) return launch_tile<T, 1, 1, 4, FL, SB>(a, st);
+    if (p.nx == 2) return launch_tile<T, 1, 2, 4, FL, SB>(a, st);
+    launch_tile<T, 1, 4, 4, FL, SB>(a, st);
 }
 template <typename T, int FL>
 void tile_t(const Q4Plan& p, const Q4Args& a, hipStream_t st) {
