@@ -10,6 +10,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "head_device.h"
 
@@ -821,6 +822,142 @@ __global__ __launch_bounds__(256) void k_q4_mid(const T* __restrict__ X, int64_t
     }
 }
 
+// The same for 16-bit activations and factors, on the 16-bit matrix cores with
+// exact products: both binary16, or bfloat16 with the one of the two that is
+// binary16 as the sum of two bfloat16 values (8 + 3 bits).  Steps of 128 rows of V
+// lie transposed in LDS ([rank][column], PV planes).  FV: V is binary16.
+// 4096 x 8192, k = 65: 86 -> FIXME us.
+template <typename T, bool FV, int F, int TW>
+__global__ __launch_bounds__(256) void k_q4_mid16(const T* __restrict__ X, int64_t ldx,
+                                                  const unsigned short* __restrict__ V, int64_t n, int64_t k, int64_t b,
+                                                  int64_t chunk, float* __restrict__ part) {
+    constexpr bool XH = std::is_same_v<T, half_t>;
+    constexpr bool HALF = XH && FV;                       // else bfloat16 products
+    constexpr int PX = XH && !FV ? 2 : 1, PV = !XH && FV ? 2 : 1, PITCH = 136;
+    using M = ActTraits<std::conditional_t<HALF, half_t, bhalf_t>>;
+    using frag = typename M::frag;
+    extern __shared__ uint4v_t lds16[];
+    unsigned short* lv = reinterpret_cast<unsigned short*>(lds16);                // [PV][16 F][PITCH]
+    const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4, wave = tid >> 6;
+    const int64_t r0 = (int64_t)blockIdx.x * 16 * F, s = blockIdx.y, b0 = (int64_t)blockIdx.z * 16 * TW;
+    const int w = (int)std::min<int64_t>(k - r0, 16 * F);
+    const int64_t j0 = s * chunk, j1 = std::min(n, j0 + chunk);
+    const T* x = X + std::min(b0 + (TW == 4 ? 16 * wave : 0) + lr, b - 1) * ldx;
+    auto put = [&](int r, int j, unsigned h) {
+        if (PV == 1) {
+            lv[r * PITCH + j] = (unsigned short)h;
+        } else {
+            const unsigned short hh = (unsigned short)h;
+            const float f = (float)__builtin_bit_cast(half_t, hh);
+            const unsigned u = __float_as_uint(f);
+            const bool special = (u & 0x7F800000u) == 0x7F800000u;
+            const float lo = special ? 0.0f : f - __uint_as_float(u & 0xFFFF0000u);
+            lv[r * PITCH + j] = (unsigned short)(f != f ? 0x7FC0u : u >> 16);
+            lv[(16 * F + r) * PITCH + j] = (unsigned short)(__float_as_uint(lo) >> 16);
+        }
+    };
+    float4_t acc[F];
+#pragma unroll
+    for (int f = 0; f < F; ++f) acc[f] = zero_accv<float4_t>();
+    for (int64_t j = j0; j < j1; j += 128) {
+        const int rows = (int)std::min<int64_t>(128, j1 - j);
+        frag xa[TW == 4 ? 4 : 1][PX];
+#pragma unroll
+        for (int h = 0; h < (TW == 4 ? 4 : 1); ++h) {
+            typename ActTraits<T>::frag raw[1];
+            load_act<T>(x, j + (TW == 4 ? h : wave) * 32 + lg * 8, j1, raw);
+            if constexpr (PX == 1) {
+                xa[h][0] = __builtin_bit_cast(frag, raw[0]);
+            } else {
+                const uint4v_t v = __builtin_bit_cast(uint4v_t, raw[0]);
+                uint4v_t hi, lo;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    unsigned p[2][3];
+                    split3(elem<half_t>(v, 2 * q), p[0]);
+                    split3(elem<half_t>(v, 2 * q + 1), p[1]);
+                    hi[q] = p[0][0] | p[1][0] << 16;
+                    lo[q] = p[0][1] | p[1][1] << 16;
+                }
+                xa[h][0] = __builtin_bit_cast(frag, hi);
+                xa[h][PX - 1] = __builtin_bit_cast(frag, lo);
+            }
+        }
+        __syncthreads();
+        if (rows < 128) {                                 // columns past the end meet zeros of x: no NaN here
+            for (int e = tid; e < PV * 16 * F * PITCH / 8; e += 256) lds16[e] = uint4v_t{0, 0, 0, 0};
+            __syncthreads();
+        }
+        if (w == k) {
+            const unsigned short* src = V + j * k;
+            const int count = rows * w;
+#pragma unroll 2
+            for (int e = tid * 8; e < count; e += 2048) {
+                uint4v_t v = {0, 0, 0, 0};
+                if (e + 8 <= count) {
+                    v = load16(src + e);
+                } else {
+#pragma unroll
+                    for (int h = 0; h < 8; ++h)
+                        if (e + h < count) set_bits<half_t>(v, h, src[e + h]);
+                }
+                int jj = e / w, r = e % w;
+#pragma unroll
+                for (int h = 0; h < 8; ++h) {
+                    if (e + h < count) put(r, jj, h & 1 ? v[h >> 1] >> 16 : v[h >> 1] & 0xFFFFu);
+                    if (++r == w) {
+                        r = 0;
+                        ++jj;
+                    }
+                }
+            }
+        } else {
+            for (int e = tid; e < rows * 16 * F; e += 256) {
+                const int r = e % (16 * F), jj = e / (16 * F);
+                if (r < w) put(r, jj, V[(j + jj) * k + r0 + r]);
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int h = 0; h < (TW == 4 ? 4 : 1); ++h)
+#pragma unroll
+            for (int f = 0; f < F; ++f) {
+                const int at = (16 * f + lr) * PITCH + (TW == 4 ? h : wave) * 32 + lg * 8;
+#pragma unroll
+                for (int q = PV - 1; q >= 0; --q) {
+                    const frag vf = *reinterpret_cast<const frag*>(lv + q * 16 * F * PITCH + at);
+#pragma unroll
+                    for (int p = PX - 1; p >= 0; --p) acc[f] = M::mfma(xa[h][p], vf, acc[f]);
+                }
+            }
+    }
+    if (TW == 4) {
+#pragma unroll
+        for (int f = 0; f < F; ++f)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const int64_t bb = b0 + 16 * wave + 4 * lg + v;
+                const int r = 16 * f + lr;
+                if (bb < b && r < w) part[(s * b + bb) * k + r0 + r] = acc[f][v];
+            }
+    } else {
+        float* red = reinterpret_cast<float*>(lds16);     // [4][16][16 F]
+        __syncthreads();
+#pragma unroll
+        for (int f = 0; f < F; ++f)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) red[(wave * 16 + 4 * lg + v) * 16 * F + 16 * f + lr] = acc[f][v];
+        __syncthreads();
+        for (int e = tid; e < 256 * F; e += 256) {
+            const int r = e % (16 * F), t = e / (16 * F);
+            float y = red[t * 16 * F + r];
+#pragma unroll
+            for (int q = 1; q < 4; ++q) y += red[(q * 16 + t) * 16 * F + r];
+            if (b0 + t < b && r < w) part[(s * b + b0 + t) * k + r0 + r] = y;
+        }
+    }
+}
+
 // T'[b][r] = s_r times the sum of the partials, in split order; rows of kp, zero
 // past k.
 __global__ __launch_bounds__(256) void k_q4_mid_finish(const float* __restrict__ part, int splits,
@@ -958,11 +1095,23 @@ void mid_f(const Q4Plan& p, const Q4Weights& w, const Q4Args& a, float* part, hi
     KernelTimer t("q4_mid", st);
     const dim3 grid((unsigned)((w.k + 16 * F - 1) / (16 * F)), p.mid_splits,
                     (unsigned)((a.b + 16 * p.mid_tw - 1) / (16 * p.mid_tw)));
+    const T* x = static_cast<const T*>(a.X);
+    const size_t red = (size_t)4 * 16 * 16 * F * 4;
+    if constexpr (sizeof(T) == 2) {
+        if (w.fprec != P32) {
+            const bool fv = w.fprec == P16;
+            const size_t lds = std::max<size_t>((size_t)(fv && !std::is_same_v<T, half_t> ? 2 : 1) * 16 * F * 136 * 2, red);
+            auto* kern = p.mid_tw == 4 ? (fv ? k_q4_mid16<T, true, F, 4> : k_q4_mid16<T, false, F, 4>)
+                                       : (fv ? k_q4_mid16<T, true, F, 1> : k_q4_mid16<T, false, F, 1>);
+            hipLaunchKernelGGL(kern, grid, dim3(256), lds, st, x, a.ldx, static_cast<const unsigned short*>(w.V), w.n, w.k,
+                               a.b, p.mid_chunk, part);
+            return;
+        }
+    }
     const int64_t wide = std::min<int64_t>(w.k, 16 * F);
-    const size_t lds = std::max<size_t>((size_t)128 * wide, (size_t)4 * 16 * 16 * F) * 4;
+    const size_t lds = std::max<size_t>((size_t)128 * wide * 4, red);
     auto* kern = p.mid_tw == 4 ? k_q4_mid<T, F, 4> : k_q4_mid<T, F, 1>;
-    hipLaunchKernelGGL(kern, grid, dim3(256), lds, st, static_cast<const T*>(a.X), a.ldx, w.V, w.fprec, w.n, w.k, a.b,
-                       p.mid_chunk, part);
+    hipLaunchKernelGGL(kern, grid, dim3(256), lds, st, x, a.ldx, w.V, w.fprec, w.n, w.k, a.b, p.mid_chunk, part);
 }
 
 template <typename T>
