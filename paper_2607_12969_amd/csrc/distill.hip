@@ -224,7 +224,8 @@ __global__ __launch_bounds__(NT, NV <= 4 ? 8 : NV <= 8 ? 6 : 4) void k_distill_r
                     m = mx;
                 }
             }
-            for (int j = j0 + t * E; j + E <= j1; j += NT * E) {
+            for (int x = t; x < (j1 - j0) / E; x += NT) {
+                const int j = j0 + x * E;
                 uint4v_t v = load16(row + j);
                 if (tail) hide(v, j, j0);
                 float mx = m;

@@ -18,7 +18,6 @@ typedef unsigned uint2v_t __attribute__((ext_vector_type(2)));
 constexpr float kLog2e = 1.4426950408889634f;
 
 // Conversions round to nearest even; bfloat16 keeps subnormals and NaN.
-template <typename T> __device__ __forceinline__ float to_f32(T x) { return (float)x; }
 template <typename T> __device__ __forceinline__ T from_f32(float x) { return (T)x; }
 
 // Element i of an array whose type is known at run time only.
@@ -106,15 +105,6 @@ template <typename T> __device__ __forceinline__ uint4v_t pack16(const float (&g
         else v[q] = pack2<T>(g[2 * q], g[2 * q + 1]);
     }
     return v;
-}
-template <typename T> __device__ __forceinline__ void store_row16(T* row, int64_t i, int64_t V, const float (&g)[kVec<T>]) {
-    if (i + kVec<T> <= V) {
-        store16(row + i, pack16<T>(g));
-    } else {
-#pragma unroll
-        for (int e = 0; e < kVec<T>; ++e)
-            if (i + e < V) row[i + e] = from_f32<T>(g[e]);
-    }
 }
 
 }  // namespace lrc

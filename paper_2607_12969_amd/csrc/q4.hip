@@ -826,7 +826,7 @@ __global__ __launch_bounds__(256) void k_q4_mid(const T* __restrict__ X, int64_t
 // exact products: both binary16, or bfloat16 with the one of the two that is
 // binary16 as the sum of two bfloat16 values (8 + 3 bits).  Steps of 128 rows of V
 // lie transposed in LDS ([rank][column], PV planes).  FV: V is binary16.
-// 4096 x 8192, k = 65: 86 -> FIXME us.
+// 4096 rows of 8192, k = 65: 53 us, k_q4_mid 86.
 template <typename T, bool FV, int F, int TW>
 __global__ __launch_bounds__(256) void k_q4_mid16(const T* __restrict__ X, int64_t ldx,
                                                   const unsigned short* __restrict__ V, int64_t n, int64_t k, int64_t b,
@@ -1018,7 +1018,7 @@ Q4Plan plan_q4(const Q4Weights& w, const void* X, int64_t ldx, int64_t b, int pr
         p.wx = prec == P32 || b <= 64 ? 1 : 2;
         p.nx = b <= 16 ? 1 : b <= 32 ? 2 : 4;
         p.wr = p.wx == 1 ? 4 : 2;
-        if (p.wx == 2 && (w.m + 255) / 256 * ((b + 127) / 128) >= 256 && !getenv("NO8")) p.wr = 4;
+        if (p.wx == 2 && (w.m + 255) / 256 * ((b + 127) / 128) >= 256) p.wr = 4;
         const int64_t tiles = (w.m + 127) / 128 * ((b + 16 * p.nx * p.wx - 1) / (16 * p.nx * p.wx));
         p.splits = (int)std::min<int64_t>(std::max<int64_t>(1, 512 / tiles), std::max<int64_t>(1, blocks / 4));
         const int e = elem_bytes(prec);
