@@ -66,6 +66,27 @@ template <int N> __device__ __forceinline__ void stay(uint4v_t (&v)[N]) {
         for (int q = 0; q < 4; ++q) asm volatile("" : "+v"(v[i][q]));
 }
 
+// log x, to a few 2^-26: the logarithm of the significand alone is binary32 (one of x
+// would carry half an ulp of its size, 2.4e-7 for sums of a few hundred).
+__device__ __forceinline__ double log_of(double x) {
+    int e;
+    double m = frexp(x, &e);                // [0.5, 1)
+    if (m < 0.70710678) {
+        m *= 2.0;
+        e -= 1;
+    }
+    if (!(m > 0.0 && m < 2.0)) return (double)logf((float)x);
+    const float f = (float)m;
+    return (double)e * 0.6931471805599453 + (double)logf(f) + (m - (double)f);
+}
+// exp x, to a few 2^-24 of itself: the argument's whole part stays out of binary32.
+__device__ __forceinline__ double exp_of(double x) {
+    const double y = x * 1.4426950408889634;
+    if (!(y > -1000.0 && y < 1000.0)) return (double)__builtin_amdgcn_exp2f((float)y);
+    const double n = rint(y);
+    return ldexp((double)__builtin_amdgcn_exp2f((float)(y - n)), (int)n);
+}
+
 template <typename T>
 __device__ void zero_row(T* out, int V, int nt) {
     const int full = V / kVec<T>;
@@ -144,7 +165,6 @@ __global__ __launch_bounds__(NT, NV <= 4 ? 8 : NV <= 8 ? 6 : 4) void k_distill_r
     // the teacher: differences of its logits in binary64, K values a row
     const double invT = 1.0 / (double)a.temperature;
     auto teacher = [&](int k) { return (double)tk[k] * invT; };
-    auto exp_of = [](double x) { return __builtin_amdgcn_exp2f((float)(x * 1.4426950408889634)); };
     double lse;
     if (tail) {
         lse = (double)a.teacher_lse[i];
@@ -160,10 +180,10 @@ __global__ __launch_bounds__(NT, NV <= 4 ? 8 : NV <= 8 ? 6 : 4) void k_distill_r
         const double m = (double)mx * invT;
         double x = 0.0;
         for (int k = lane; k < K; k += 64)
-            if (ids[k] >= 0) x += (double)exp_of(teacher(k) - m);
-        lse = m + (double)logf((float)wave_sum(x));
+            if (ids[k] >= 0) x += exp_of(teacher(k) - m);
+        lse = m + log_of(wave_sum(x));
     }
-    auto prob = [&](int k) { return ids[k] >= 0 ? (double)exp_of(teacher(k) - lse) : 0.0; };
+    auto prob = [&](int k) { return ids[k] >= 0 ? exp_of(teacher(k) - lse) : 0.0; };
     double r = 0.0;
     if (tail) {
         double sp = 0.0;
@@ -280,7 +300,7 @@ __global__ __launch_bounds__(NT, NV <= 4 ? 8 : NV <= 8 ? 6 : 4) void k_distill_r
         S += s == 0.0f ? 0.0 : (double)s * (double)__builtin_amdgcn_exp2f((m - M) * c);
     }
     if (MODE != BACKWARD && t < 64) {
-        const double logS = (double)logf((float)S);
+        const double logS = log_of(S);
         double kl = 0.0;
         for (int k = lane; k < K; k += 64) {
             const double p = prob(k);
@@ -289,7 +309,7 @@ __global__ __launch_bounds__(NT, NV <= 4 ? 8 : NV <= 8 ? 6 : 4) void k_distill_r
         kl = wave_sum(kl);
         if (t == 0) {
             if (r != 0.0)
-                kl += r * ((double)logf((float)r) - ((double)(m - M) * invT + (double)logf(s) - logS));
+                kl += r * (log_of(r) - ((double)(m - M) * invT + log_of((double)s) - logS));
             loss[i] = (float)((double)w * (double)a.temperature * (double)a.temperature * kl);
         }
         if (MODE == FORWARD && stats && t < 4) stats[i * 4 + t] = t == 0 ? M : t == 1 ? (float)S : t == 2 ? m : s;
