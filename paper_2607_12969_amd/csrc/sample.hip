@@ -25,7 +25,8 @@
 //                to LDS, where v and r are found; kept mass of each part; the draw
 //                inside one part;
 //   neither      maximum; kept mass; draw.
-// Inside a bin, v comes from histograms over the bits of the values.  What does not
+// Inside a bin, v comes from ranking its values one against all, or, above kRanked of
+// them, from histograms over their bits.  What does not
 // fit its list (thousands of equal logits, say), and rows with an infinite
 // maximum, find v by histograms over the row itself.
 #include <hip/hip_runtime.h>
@@ -42,6 +43,7 @@ typedef unsigned long long u64;
 constexpr int kBins = 2048;
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kPart = 512;               // list entries of a wave
+constexpr int kRanked = kThreads;        // values of a bin that are ranked one against all
 constexpr float kNegInf = -__builtin_inff();
 
 // Order of binary32 values as unsigned integers (no NaN; -0 counts as 0).
@@ -91,6 +93,7 @@ struct Shared {
     u64 before;
     unsigned beforec;
     unsigned kmin, kmax;
+    int nb;                              // values in the bin of the cut
 };
 
 __device__ __forceinline__ void clear_bins(Shared& s) {
@@ -150,12 +153,13 @@ struct Cut {
     unsigned count;      // ... and number
 };
 
-// A row in memory: wave w takes the contiguous part [w L, (w + 1) L) in blocks of 64
-// vectors, a lane kVec consecutive logits of each.
+// A row in memory, or the 16 L logits of it from `base` on: wave w takes the
+// contiguous part [base + w L, base + (w + 1) L) in blocks of 64 vectors, a lane
+// kVec consecutive logits of each.
 template <typename T> struct Row {
     static constexpr int E = kVec<T>, B = 64 * E;
     const T* row;
-    unsigned V, L;
+    unsigned V, L, base;
     // f(index of the lane's first logit, logits) for the blocks of [begin, end), in
     // order; four loads at a time
     template <typename F> __device__ __forceinline__ void visit(unsigned begin, unsigned end, F&& f) const {
@@ -171,7 +175,9 @@ template <typename T> struct Row {
 #pragma unroll 1
         for (; i < end; i += B) f(i + lane, load_row16(row, (int64_t)i + lane, (int64_t)V));
     }
-    __device__ __forceinline__ unsigned begin(int wave) const { return (unsigned)std::min<uint64_t>(V, (uint64_t)wave * L); }
+    __device__ __forceinline__ unsigned begin(int wave) const {
+        return (unsigned)std::min<uint64_t>(V, (uint64_t)base + (uint64_t)wave * L);
+    }
     // every logit of this wave's part
     template <typename F> __device__ __forceinline__ void each(F&& f) const {
         const int wave = threadIdx.x >> 6;
@@ -198,24 +204,57 @@ __device__ __noinline__ Cut refine(Shared& s, W wt, bool by_count, u64 target, i
                                    From from) {
     const int t = threadIdx.x;
     unsigned lo = ~0u, hi = 0u;
+    if (t == 0) {
+        s.kmin = ~0u;
+        s.kmax = 0u;
+        s.nb = 0;
+        s.before = before;
+        s.beforec = beforec;
+    }
+    __syncthreads();
     from.each([&](float l) {
         const float z = wt.z(l);
         if (z >= -31.0f && bin_of(z) == zb) {
             const unsigned k = key_of(l);
             lo = std::min(lo, k);
             hi = std::max(hi, k);
+            const int at = atomicAdd(&s.nb, 1);
+            if (at < kRanked) s.mass[at] = (u64)k << 32 | Weigh::q(wt.w(l));
         }
     });
-    if (t == 0) {
-        s.kmin = ~0u;
-        s.kmax = 0u;
-    }
-    __syncthreads();
     if (lo <= hi) {
         atomicMin(&s.kmin, lo);
         atomicMax(&s.kmax, hi);
     }
     __syncthreads();
+    const int n = s.nb;
+    if (n <= kRanked) {
+        // each value against all: what lies above it and how often it occurs
+        if (t < n) {
+            const u64 mine = s.mass[t];
+            const unsigned key = (unsigned)(mine >> 32);
+            u64 above = before;
+            unsigned c = beforec, eq = 0;
+#pragma unroll 8
+            for (int j = 0; j < n; ++j) {
+                const u64 o = s.mass[j];
+                const unsigned ok = (unsigned)(o >> 32);
+                above += ok > key ? (unsigned)o : 0u;
+                c += ok > key;
+                eq += ok == key;
+            }
+            const u64 prior = by_count ? c : above, reached = prior + (by_count ? eq : (u64)eq * (unsigned)mine);
+            if (prior < target && reached >= target) {      // equal values write the same
+                s.kmin = key;
+                s.before = above;
+                s.beforec = c;
+            }
+        }
+        __syncthreads();
+        const Cut cut{of_key(s.kmin), s.before, s.beforec};
+        __syncthreads();
+        return cut;
+    }
     lo = s.kmin;
     hi = s.kmax;
     while (lo < hi) {
@@ -353,29 +392,23 @@ __device__ __forceinline__ bool find_lane(const Kept<W>& k, u64 target, u64& run
     return false;
 }
 
-// The draw over the row: kept mass of each wave's part, then of 16 parts of the
-// one that holds the token, then that part itself.
+// The draw inside [from, to), which holds the token: kept mass of 16 parts of it,
+// then the part that holds the token.  run, run_eq: kept mass and ties before it.
 template <typename T, typename W>
-__device__ __forceinline__ void draw_row(Shared& s, const Row<T>& row, const Kept<W>& k, float u, int64_t* token) {
+__device__ __forceinline__ void draw_range(Shared& s, const Row<T>& row, const Kept<W>& k, float u, u64 target, u64 run,
+                                           u64 run_eq, unsigned from, unsigned to, int64_t* token) {
     constexpr int E = kVec<T>;
     const int wave = threadIdx.x >> 6;
-    u64 target = 0, run, run_eq, sum = 0;
+    u64 sum = 0;
     unsigned eq = 0;
-    auto add = [&](float l) {
-        sum += k.above(l);
-        eq += k.tied(l);
-    };
-    row.each(add);
-    const int part = find_part<true>(s, k, sum, eq, u, target, run, run_eq);
-    if (part < 0) return;
-    const unsigned from = row.begin(part), to = row.begin(part + 1);
     const unsigned sub = ((to - from + kWaves * row.B - 1) / (kWaves * row.B)) * row.B;
     auto sub_begin = [&](int w) { return (unsigned)std::min<uint64_t>(to, (uint64_t)from + (uint64_t)w * sub); };
-    sum = 0;
-    eq = 0;
     row.visit(sub_begin(wave), sub_begin(wave + 1), [&](unsigned, const uint4v_t& v) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) add(elem<T>(v, e));
+        for (int e = 0; e < E; ++e) {
+            sum += k.above(elem<T>(v, e));
+            eq += k.tied(elem<T>(v, e));
+        }
     });
     const int w = find_part<false>(s, k, sum, eq, u, target, run, run_eq);
     if (wave != w) return;
@@ -392,6 +425,21 @@ __device__ __forceinline__ void draw_row(Shared& s, const Row<T>& row, const Kep
         }
         if (!find_lane<E>(k, target, run, run_eq, l, at, token)) return;
     }
+}
+
+// The draw over the row: kept mass of each wave's part, then inside the one that
+// holds the token.
+template <typename T, typename W>
+__device__ __forceinline__ void draw_row(Shared& s, const Row<T>& row, const Kept<W>& k, float u, int64_t* token) {
+    u64 target = 0, run, run_eq, sum = 0;
+    unsigned eq = 0;
+    row.each([&](float l) {
+        sum += k.above(l);
+        eq += k.tied(l);
+    });
+    const int part = find_part<true>(s, k, sum, eq, u, target, run, run_eq);
+    if (part < 0) return;
+    draw_range(s, row, k, u, target, run, run_eq, row.begin(part), row.begin(part + 1), token);
 }
 
 // Number of smallest weights that reach `target` from `above`.
@@ -446,6 +494,93 @@ __device__ __noinline__ void sample_any(Shared& s, Row<T> row, W wt, int64_t k, 
     draw_row(s, row, kept, u, token);
 }
 
+// The tokens of this wave's part down to bin `last`, in index order, to its list in
+// LDS; their number, which may pass the list's kPart entries.
+template <typename T>
+__device__ __forceinline__ int gather_down_to(Shared& s, const Row<T>& row, const Weigh& wt, int last) {
+    constexpr int E = kVec<T>;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int n = 0;
+    row.visit(row.begin(wave), row.begin(wave + 1), [&](unsigned i, const uint4v_t& v) {
+        unsigned mask = 0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const float z = wt.z(elem<T>(v, e));
+            if (z >= -31.0f && bin_of(z) <= last) mask |= 1u << e;
+        }
+        if (__builtin_amdgcn_ballot_w64(mask != 0)) {
+            const int c = __builtin_popcount(mask);
+            int at = c;
+#pragma unroll
+            for (int off = 1; off < 64; off <<= 1) {
+                const int o = __shfl_up(at, off, 64);
+                if (lane >= off) at += o;
+            }
+            const int total = __shfl(at, 63, 64);
+            at += n - c;
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (mask >> e & 1u) {
+                    if (at < kPart) {
+                        s.lv[wave * kPart + at] = elem<T>(v, e);
+                        s.li[wave * kPart + at] = i + e;
+                    }
+                    ++at;
+                }
+            n += total;
+        }
+    });
+    return n;
+}
+
+// top-k, top-p, min-p and the draw over the waves' lists (n entries of this wave),
+// which hold every token down to the bin of the k-th (bin < 0: every token that
+// weighs anything).
+__device__ __forceinline__ void finish_topk(Shared& s, Kept<Weigh>& kept, int64_t k, int bin, unsigned beforec, int n,
+                                            bool topp, float p, float u, int64_t* token) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const Weigh wt = kept.wt;
+    u64 before;
+    const List list{s.lv, wave * kPart + lane, wave * kPart + n, 64};
+    if (bin >= 0) {
+        const Cut cut = refine(s, wt, true, (u64)k, bin, 0, beforec, list);
+        kept.cut(cut.v, (u64)k - cut.count);
+    }
+    if (topp) {
+        u64 m = 0;
+        list.each([&](float l) {
+            if (kept.all || l > kept.v) m += Weigh::q(wt.w(l));
+        });
+        m = wave_add(m);
+        __syncthreads();
+        if (lane == 0) s.red[wave] = m;
+        clear_bins(s);
+        u64 mass = kept.all ? 0 : kept.ties * Weigh::q(wt.w(kept.v));
+        for (int w = 0; w < kWaves; ++w) mass += s.red[w];
+        const u64 target = mass_target(p, mass);
+        list.each([&](float l) { atomicAdd(&s.mass[bin_of(wt.z(l))], (u64)Weigh::q(wt.w(l))); });
+        __syncthreads();
+        find_bin(s, false, target, bin, before, beforec);
+        if (bin >= 0) {
+            const Cut cut = refine(s, wt, false, target, bin, before, 0u, list);
+            kept.cut(cut.v, ties_to(target, cut.above, Weigh::q(wt.w(cut.v))));
+        }
+    }
+    u64 target = 0, run, run_eq, sum = 0;
+    unsigned eq = 0;
+    list.each([&](float l) {
+        sum += kept.above(l);
+        eq += kept.tied(l);
+    });
+    if (find_part<true>(s, kept, sum, eq, u, target, run, run_eq) != wave) return;
+    for (int e0 = 0; e0 < n; e0 += 64) {
+        const int e = wave * kPart + e0 + lane;
+        const float l[1] = {e0 + lane < n ? s.lv[e] : __builtin_nanf("")};
+        const unsigned at[1] = {e0 + lane < n ? s.li[e] : 0u};
+        if (!find_lane<1>(kept, target, run, run_eq, l, at, token)) return;
+    }
+}
+
 }  // namespace
 
 template <typename T>
@@ -455,7 +590,7 @@ __global__ __launch_bounds__(kThreads) void k_sample_row(SampleArgs a, unsigned 
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
     const int64_t r = blockIdx.x;
     const unsigned V = (unsigned)a.vocab;
-    const Row<T> row{static_cast<const T*>(a.logits) + r * a.ld, V, L};
+    const Row<T> row{static_cast<const T*>(a.logits) + r * a.ld, V, L, 0};
     const float temp = a.temperature ? a.temperature[r] : 1.0f, u = a.u[r];
     const int64_t k = a.top_k ? a.top_k[r] : 0;
     const float p = a.top_p ? a.top_p[r] : 1.0f, mp = a.min_p ? a.min_p[r] : 0.0f;
@@ -550,36 +685,7 @@ __global__ __launch_bounds__(kThreads) void k_sample_row(SampleArgs a, unsigned 
     __syncthreads();
     find_bin(s, true, (u64)k, bin, before, beforec);
     const int last = bin < 0 ? kBins : bin;          // fewer than k tokens weigh anything: all of them
-    int n = 0;
-    row.visit(row.begin(wave), row.begin(wave + 1), [&](unsigned i, const uint4v_t& v) {
-        unsigned mask = 0;
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const float z = wt.z(elem<T>(v, e));
-            if (z >= -31.0f && bin_of(z) <= last) mask |= 1u << e;
-        }
-        if (__builtin_amdgcn_ballot_w64(mask != 0)) {
-            const int c = __builtin_popcount(mask);
-            int at = c;
-#pragma unroll
-            for (int off = 1; off < 64; off <<= 1) {
-                const int o = __shfl_up(at, off, 64);
-                if (lane >= off) at += o;
-            }
-            const int total = __shfl(at, 63, 64);
-            at += n - c;
-#pragma unroll
-            for (int e = 0; e < E; ++e)
-                if (mask >> e & 1u) {
-                    if (at < kPart) {
-                        s.lv[wave * kPart + at] = elem<T>(v, e);
-                        s.li[wave * kPart + at] = i + e;
-                    }
-                    ++at;
-                }
-            n += total;
-        }
-    });
+    const int n = gather_down_to(s, row, wt, last);
     if (lane == 0) s.ln[wave] = n;
     __syncthreads();
     bool fits = true;
@@ -588,60 +694,338 @@ __global__ __launch_bounds__(kThreads) void k_sample_row(SampleArgs a, unsigned 
         sample_any(s, row, wt, k, p, floor_w, u, token);
         return;
     }
-    const List list{s.lv, wave * kPart + lane, wave * kPart + n, 64};
-    if (bin >= 0) {
-        const Cut cut = refine(s, wt, true, (u64)k, bin, 0, beforec, list);
-        kept.cut(cut.v, (u64)k - cut.count);
-    }
-    if (topp) {
-        u64 m = 0;
-        list.each([&](float l) {
-            if (kept.all || l > kept.v) m += Weigh::q(wt.w(l));
-        });
-        m = wave_add(m);
-        __syncthreads();
-        if (lane == 0) s.red[wave] = m;
-        clear_bins(s);
-        u64 mass = kept.all ? 0 : kept.ties * Weigh::q(wt.w(kept.v));
-        for (int w = 0; w < kWaves; ++w) mass += s.red[w];
-        const u64 target = mass_target(p, mass);
-        list.each([&](float l) { atomicAdd(&s.mass[bin_of(wt.z(l))], (u64)Weigh::q(wt.w(l))); });
-        __syncthreads();
-        find_bin(s, false, target, bin, before, beforec);
-        if (bin >= 0) {
-            const Cut cut = refine(s, wt, false, target, bin, before, 0u, list);
-            kept.cut(cut.v, ties_to(target, cut.above, Weigh::q(wt.w(cut.v))));
-        }
-    }
-    u64 target = 0, run, run_eq, sum = 0;
-    unsigned eq = 0;
-    list.each([&](float l) {
-        sum += kept.above(l);
-        eq += kept.tied(l);
-    });
-    if (find_part<true>(s, kept, sum, eq, u, target, run, run_eq) != wave) return;
-    for (int e0 = 0; e0 < n; e0 += 64) {
-        const int e = wave * kPart + e0 + lane;
-        const float l[1] = {e0 + lane < n ? s.lv[e] : __builtin_nanf("")};
-        const unsigned at[1] = {e0 + lane < n ? s.li[e] : 0u};
-        if (!find_lane<1>(kept, target, run, run_eq, l, at, token)) return;
-    }
+    finish_topk(s, kept, k, bin, beforec, n, topp, p, u, token);
 }
 
-size_t sample_workspace_bytes(const SampleArgs&) { return 0; }
+// ---- few rows: a row on several workgroups ------------------------------------
+// The passes over a row become launches, each on `parts` workgroups a row (16 L
+// logits each), joined through memory; the last one, a workgroup a row, does what
+// concerns the lists and draws inside one part.  One workgroup per row leaves most of
+// the chip idle when rows are few: 48 x 65536 FP32 39 us there.
+namespace {
+
+struct SplitBuffers {
+    float* max;          // [rows][parts]: maximum ...
+    unsigned* first;     // ... and the first index that holds it
+    u64* hist;           // [rows][kBins]: counts (top-k) or masses (top-p alone)
+    u64* mass;           // [rows][parts]: kept mass (above the bin of the cut)
+    int* n;              // [rows][parts]: entries of the list; above kPart: does not fit
+    float* lv;           // [rows][parts][kPart]
+    unsigned* li;
+};
+
+// What a row asks for.
+struct Asked {
+    float temp, u, p, mp, M;
+    int64_t k;
+    bool topk, topp;
+    __device__ __forceinline__ Asked(const SampleArgs& a, const SplitBuffers& b, int64_t r, int parts) {
+        temp = a.temperature ? a.temperature[r] : 1.0f;
+        u = a.u[r];
+        k = a.top_k ? a.top_k[r] : 0;
+        p = a.top_p ? a.top_p[r] : 1.0f;
+        mp = a.min_p ? a.min_p[r] : 0.0f;
+        topk = k > 0 && k < a.vocab;
+        topp = p < 1.0f;
+        M = kNegInf;
+        for (int q = 0; q < parts; ++q) M = __builtin_fmaxf(M, b.max[r * parts + q]);
+    }
+    // a draw by weights of finite logits
+    __device__ __forceinline__ bool weighs() const { return temp > 0.0f && M != kNegInf && M != __builtin_inff(); }
+    __device__ __forceinline__ float floor_w() const { return mp > 0.0f ? std::min(mp, 1.0f) : 0.0f; }
+};
+
+}  // namespace
 
 template <typename T>
-static void launch_rows(const SampleArgs& a, hipStream_t st) {
-    const int64_t L = round_up((a.vocab + kWaves - 1) / kWaves, 64 * kVec<T>);
-    hipLaunchKernelGGL(k_sample_row<T>, dim3((unsigned)a.rows), dim3(kThreads), 0, st, a, (unsigned)L);
+__global__ __launch_bounds__(kThreads) void k_sample_max(SampleArgs a, SplitBuffers b, unsigned L, int parts) {
+    __shared__ float redf[kWaves];
+    __shared__ unsigned redc[kWaves];
+    constexpr int E = kVec<T>;
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6, part = blockIdx.x;
+    const int64_t r = blockIdx.y;
+    const Row<T> row{static_cast<const T*>(a.logits) + r * a.ld, (unsigned)a.vocab, L, (unsigned)part * kWaves * L};
+    for (int q = part * kThreads + t; q < kBins; q += parts * kThreads) b.hist[r * kBins + q] = 0;
+    float M = kNegInf;
+    unsigned at = ~0u;
+    row.visit(row.begin(wave), row.begin(wave + 1), [&](unsigned i, const uint4v_t& v) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const float l = elem<T>(v, e);
+            if (l > M) {
+                M = l;
+                at = i + e;
+            }
+        }
+    });
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) {
+        const float m = __shfl_xor(M, off, 64);
+        const unsigned o = __shfl_xor(at, off, 64);
+        if (m > M || (m == M && o < at)) {
+            M = m;
+            at = o;
+        }
+    }
+    if (lane == 0) {
+        redf[wave] = M;
+        redc[wave] = at;
+    }
+    __syncthreads();
+    if (t == 0) {
+        for (int w = 1; w < kWaves; ++w)
+            if (redf[w] > M) {
+                M = redf[w];
+                at = redc[w];
+            }
+        b.max[r * parts + part] = M;
+        b.first[r * parts + part] = at;
+    }
 }
 
-hipError_t launch_sample(const SampleArgs& a, Workspace&, hipStream_t st) {
-    KernelTimer t("sample_row", st);
-    if (a.prec == P32) launch_rows<float>(a, st);
-    else if (a.prec == P16) launch_rows<half_t>(a, st);
-    else launch_rows<bhalf_t>(a, st);
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_sample_hist(SampleArgs a, SplitBuffers b, unsigned L, int parts) {
+    __shared__ u64 mass[kBins];
+    const int64_t r = blockIdx.y;
+    const Asked q(a, b, r, parts);
+    if (!q.weighs() || !(q.topk || q.topp)) return;
+    const Row<T> row{static_cast<const T*>(a.logits) + r * a.ld, (unsigned)a.vocab, L, blockIdx.x * kWaves * L};
+    for (int e = threadIdx.x; e < kBins; e += kThreads) mass[e] = 0;
+    __syncthreads();
+    const Weigh wt{q.M, scale_of(q.temp)};
+    if (q.topk) {
+        row.each([&](float l) {
+            const float z = wt.z(l);
+            if (z >= -31.0f) atomicAdd(reinterpret_cast<unsigned*>(&mass[bin_of(z)]), 1u);
+        });
+    } else {
+        row.each([&](float l) {
+            const float z = wt.z(l);
+            if (z >= -31.0f) atomicAdd(&mass[bin_of(z)], (u64)Weigh::q(__builtin_amdgcn_exp2f(z)));
+        });
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < kBins; e += kThreads)
+        if (mass[e]) atomicAdd(&b.hist[r * kBins + e], mass[e]);
+}
+
+namespace {
+
+// The bin of the cut from the row's histogram.
+__device__ __forceinline__ void find_cut_bin(Shared& s, const Asked& q, const u64* hist, u64& target, int& bin, u64& before,
+                                             unsigned& beforec) {
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    u64 h[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        h[e] = hist[2 * t + e];
+        s.count[2 * t + e] = q.topk ? (unsigned)h[e] : 0u;
+        s.mass[2 * t + e] = q.topk ? 0ull : h[e];
+    }
+    target = (u64)q.k;
+    if (!q.topk) {
+        const u64 m = wave_add(h[0] + h[1]);
+        if (lane == 0) s.red[wave] = m;
+        __syncthreads();
+        u64 mass = 0;
+        for (int w = 0; w < kWaves; ++w) mass += s.red[w];
+        target = mass_target(q.p, mass);
+    }
+    __syncthreads();
+    find_bin(s, q.topk, target, bin, before, beforec);
+}
+
+}  // namespace
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_sample_gather(SampleArgs a, SplitBuffers b, unsigned L, int parts) {
+    __shared__ Shared s;
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    const int64_t r = blockIdx.y, at = r * parts + blockIdx.x;
+    const Asked q(a, b, r, parts);
+    if (!q.weighs()) return;
+    const Row<T> row{static_cast<const T*>(a.logits) + r * a.ld, (unsigned)a.vocab, L, blockIdx.x * kWaves * L};
+    const Weigh wt{q.M, scale_of(q.temp)};
+    const float floor_w = q.floor_w();
+    u64 target, before;
+    int bin = kBins;
+    unsigned beforec;
+    if (t == 0) s.n = 0;
+    if (q.topk || q.topp) find_cut_bin(s, q, b.hist + r * kBins, target, bin, before, beforec);
+    if (q.topk) {
+        // in index order: the waves' lists one after another
+        const int n = gather_down_to(s, row, wt, bin < 0 ? kBins : bin);
+        if (lane == 0) s.ln[wave] = n;
+        __syncthreads();
+        int from = 0, total = 0;
+        bool fits = true;
+        for (int w = 0; w < kWaves; ++w) {
+            if (w < wave) from += s.ln[w];
+            total += s.ln[w];
+            fits &= s.ln[w] <= kPart;
+        }
+        fits &= total <= kPart;
+        if (fits)
+            for (int e = lane; e < n; e += 64) {
+                b.lv[at * kPart + from + e] = s.lv[wave * kPart + e];
+                b.li[at * kPart + from + e] = s.li[wave * kPart + e];
+            }
+        if (t == 0) b.n[at] = fits ? total : kPart + 1;
+        return;
+    }
+    // kept mass above the bin of the cut (all, without one); the values in it, in any order
+    u64 sum = 0;
+    row.each([&](float l) {
+        const float z = wt.z(l);
+        if (z >= -31.0f) {
+            const int zb = bin_of(z);
+            if (zb < bin) {
+                const float w = wt.w(l);
+                sum += w >= floor_w ? Weigh::q(w) : 0u;
+            } else if (zb == bin) {
+                const int e = atomicAdd(&s.n, 1);
+                if (e < kPart) b.lv[at * kPart + e] = l;
+            }
+        }
+    });
+    sum = wave_add(sum);
+    if (lane == 0) s.red[wave] = sum;
+    __syncthreads();
+    if (t == 0) {
+        u64 m = 0;
+        for (int w = 0; w < kWaves; ++w) m += s.red[w];
+        b.mass[at] = m;
+        b.n[at] = bin < 0 ? kPart + 1 : s.n;
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_sample_pick(SampleArgs a, SplitBuffers b, unsigned L, int parts,
+                                                          unsigned whole) {
+    __shared__ Shared s;
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    const int64_t r = blockIdx.x;
+    const Asked q(a, b, r, parts);
+    int64_t* token = a.tokens + r;
+    const Row<T> row{static_cast<const T*>(a.logits) + r * a.ld, (unsigned)a.vocab, whole, 0};
+    if (q.M == kNegInf) {
+        if (t == 0) *token = -1;
+        return;
+    }
+    if (!(q.temp > 0.0f)) {
+        if (t == 0) {
+            int at = 0;
+            while (b.max[r * parts + at] != q.M) ++at;
+            *token = b.first[r * parts + at];
+        }
+        return;
+    }
+    const float floor_w = q.floor_w();
+    if (q.M == __builtin_inff()) {
+        sample_any(s, row, WeighInf{}, q.k, q.p, floor_w, q.u, token);
+        return;
+    }
+    const Weigh wt{q.M, scale_of(q.temp)};
+    Kept<Weigh> kept{wt, 0.0f, floor_w, 0, 0, true};
+    u64 target = 0, before, run, run_eq, sum = 0;
+    int bin = -1, n = 0;
+    unsigned beforec, eq = 0;
+    if (q.topk || q.topp) {
+        bool fits = true;
+        for (int w = 0; w < parts; ++w) fits &= b.n[r * parts + w] <= kPart;
+        if (!fits) {
+            sample_any(s, row, wt, q.k, q.p, floor_w, q.u, token);
+            return;
+        }
+        if (wave < parts) {
+            const int64_t at = r * parts + wave;
+            n = b.n[at];
+            for (int e = lane; e < n; e += 64) {
+                s.lv[wave * kPart + e] = b.lv[at * kPart + e];
+                s.li[wave * kPart + e] = q.topk ? b.li[at * kPart + e] : 0u;
+            }
+        }
+        find_cut_bin(s, q, b.hist + r * kBins, target, bin, before, beforec);
+    }
+    if (q.topk) {
+        finish_topk(s, kept, q.k, bin, beforec, n, q.topp, q.p, q.u, token);
+        return;
+    }
+    if (q.topp) {
+        const List list{s.lv, wave * kPart + lane, wave * kPart + n, 64};
+        const Cut cut = refine(s, wt, false, target, bin, before, 0u, list);
+        kept.cut(cut.v, ties_to(target, cut.above, Weigh::q(wt.w(cut.v))));
+        list.each([&](float l) {
+            sum += kept.above(l);
+            eq += kept.tied(l);
+        });
+    }
+    if (wave < parts && lane == 0) sum += b.mass[r * parts + wave];
+    const int part = find_part<true>(s, kept, sum, eq, q.u, target, run, run_eq);
+    if (part < 0) return;
+    const unsigned from = (unsigned)part * kWaves * L;
+    draw_range(s, row, kept, q.u, target, run, run_eq, from, std::min((unsigned)a.vocab, from + kWaves * L), token);
+}
+
+namespace {
+
+// Parts of a row (at most one for each wave of k_sample_pick), or 1: k_sample_row.
+struct SamplePlan {
+    int parts;
+    unsigned L, whole;   // logits of a wave: in a part, in the row
+};
+SamplePlan plan_sample(const SampleArgs& a) {
+    const int64_t block = 64 * (a.prec == P32 ? kVec<float> : kVec<half_t>);
+    SamplePlan p{1, 0, (unsigned)round_up((a.vocab + kWaves - 1) / kWaves, block)};
+    if (a.rows > 128 || a.vocab < 16384) return p;
+    const int64_t want = std::min<int64_t>(kWaves, 256 / a.rows);
+    p.L = (unsigned)round_up((a.vocab + kWaves * want - 1) / (kWaves * want), block);
+    p.parts = (int)((a.vocab + (int64_t)kWaves * p.L - 1) / ((int64_t)kWaves * p.L));
+    return p;
+}
+
+SplitBuffers split_buffers(const SampleArgs& a, int parts, Workspace& ws) {
+    const size_t rp = (size_t)a.rows * parts;
+    SplitBuffers b;
+    b.max = static_cast<float*>(ws.take(rp * 4));
+    b.first = static_cast<unsigned*>(ws.take(rp * 4));
+    b.hist = static_cast<u64*>(ws.take((size_t)a.rows * kBins * 8));
+    b.mass = static_cast<u64*>(ws.take(rp * 8));
+    b.n = static_cast<int*>(ws.take(rp * 4));
+    b.lv = static_cast<float*>(ws.take(rp * kPart * 4));
+    b.li = static_cast<unsigned*>(ws.take(rp * kPart * 4));
+    return b;
+}
+
+template <typename T> hipError_t sample_t(const SampleArgs& a, Workspace& ws, hipStream_t st) {
+    const SamplePlan p = plan_sample(a);
+    const dim3 rows((unsigned)a.rows), split(p.parts, (unsigned)a.rows), threads(kThreads);
+    if (p.parts == 1) {
+        KernelTimer t("sample_row", st);
+        hipLaunchKernelGGL(k_sample_row<T>, rows, threads, 0, st, a, p.whole);
+        return hipGetLastError();
+    }
+    const SplitBuffers b = split_buffers(a, p.parts, ws);
+    if (ws.overrun) return hipErrorOutOfMemory;
+    KernelTimer t("sample_split", st);
+    hipLaunchKernelGGL(k_sample_max<T>, split, threads, 0, st, a, b, p.L, p.parts);
+    hipLaunchKernelGGL(k_sample_hist<T>, split, threads, 0, st, a, b, p.L, p.parts);
+    hipLaunchKernelGGL(k_sample_gather<T>, split, threads, 0, st, a, b, p.L, p.parts);
+    hipLaunchKernelGGL(k_sample_pick<T>, rows, threads, 0, st, a, b, p.L, p.parts, p.whole);
     return hipGetLastError();
+}
+
+}  // namespace
+
+size_t sample_workspace_bytes(const SampleArgs& a) {
+    const int parts = plan_sample(a).parts;
+    if (parts == 1) return 0;
+    const size_t rp = (size_t)a.rows * parts;
+    return 7 * 256 + rp * (4 + 4 + 8 + 4 + 8 * kPart) + (size_t)a.rows * kBins * 8;
+}
+
+hipError_t launch_sample(const SampleArgs& a, Workspace& ws, hipStream_t st) {
+    return a.prec == P32 ? sample_t<float>(a, ws, st) : a.prec == P16 ? sample_t<half_t>(a, ws, st) : sample_t<bhalf_t>(a, ws, st);
 }
 
 }  // namespace lrc
