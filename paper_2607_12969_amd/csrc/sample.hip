@@ -700,8 +700,13 @@ __global__ __launch_bounds__(kThreads) void k_sample_row(SampleArgs a, unsigned 
 // ---- few rows: a row on several workgroups ------------------------------------
 // The passes over a row become launches, each on `parts` workgroups a row (16 L
 // logits each), joined through memory; the last one, a workgroup a row, does what
-// concerns the lists and draws inside one part.  One workgroup per row leaves most of
-// the chip idle when rows are few: 48 x 65536 FP32 39 us there.
+// concerns the lists and draws inside one part.  Four launches cost more than the
+// passes save until few rows are long.  FP32, us, one workgroup a row against this,
+// no filter / top-p / top-k / both:
+//     1 x 65536     16 34 22 27    18 31 25 31
+//     1 x 131072    22 55 30 34    19 36 25 31
+//     8 x 131072    25 56 32 37    22 38 29 34
+//     48 x 131072   26 58 33 38    29 50 33 38
 namespace {
 
 struct SplitBuffers {
@@ -977,8 +982,8 @@ struct SamplePlan {
 SamplePlan plan_sample(const SampleArgs& a) {
     const int64_t block = 64 * (a.prec == P32 ? kVec<float> : kVec<half_t>);
     SamplePlan p{1, 0, (unsigned)round_up((a.vocab + kWaves - 1) / kWaves, block)};
-    if (a.rows > 128 || a.vocab < 16384) return p;
-    const int64_t want = std::min<int64_t>(kWaves, 256 / a.rows);
+    if (a.rows > 16 || a.vocab < 98304) return p;    // measured above
+    const int64_t want = kWaves;                      // 16 rows: 256 workgroups
     p.L = (unsigned)round_up((a.vocab + kWaves * want - 1) / (kWaves * want), block);
     p.parts = (int)((a.vocab + (int64_t)kWaves * p.L - 1) / ((int64_t)kWaves * p.L));
     return p;
