@@ -1031,9 +1031,10 @@ Q4Plan plan_q4(const Q4Weights& w, const void* X, int64_t ldx, int64_t b, int pr
         const int64_t kp = round_up(w.k, 16);
         p.mid_tw = b <= 16 ? 1 : 4;
         const int64_t groups = (w.k + 127) / 128 * ((b + 16 * p.mid_tw - 1) / (16 * p.mid_tw));
-        // enough workgroups for the chip, few partials for their readers
+        // enough workgroups for the chip, few partials for their readers (one row of
+        // 8192 columns, k = 65: 64 parts 6.4 us, 32 parts 9.5, their reader 1 us longer)
         int64_t s = std::min<int64_t>(blocks, std::max<int64_t>(1, 512 / groups));
-        s = std::min<int64_t>(s, b <= 2 ? 32 : b <= 16 ? 32 : 64);
+        s = std::min<int64_t>(s, b == 1 ? 64 : b <= 16 ? 32 : 64);
         p.mid_chunk = (blocks + s - 1) / s * 128;
         p.mid_splits = (int)((w.n + p.mid_chunk - 1) / p.mid_chunk);
         p.mid_finish = p.tile || b * p.mid_splits > 64 || b * kp > kRowsTm;
