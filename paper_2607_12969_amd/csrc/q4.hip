@@ -1168,8 +1168,9 @@ hipError_t apply_t(const Q4Weights& w, Q4Args& a, int prec, Workspace& ws, hipSt
 constexpr int64_t kQ4Panel = 1 << 20;
 
 size_t q4_apply_workspace_bytes(const Q4Weights& w, const void* X, int64_t ldx, int64_t batch, int prec) {
+    const int64_t rest = batch > kQ4Panel ? batch % kQ4Panel : 0;      // 0: whole panels alone
     size_t bytes = plan_bytes(plan_q4(w, X, ldx, std::min(batch, kQ4Panel), prec));
-    if (batch > kQ4Panel) bytes = std::max(bytes, plan_bytes(plan_q4(w, X, ldx, batch % kQ4Panel, prec)));
+    if (rest) bytes = std::max(bytes, plan_bytes(plan_q4(w, X, ldx, rest, prec)));
     return bytes;
 }
 
