@@ -449,7 +449,8 @@ int64_t lrc_q4_storage_bytes(int64_t m, int64_t n, int64_t group, int sprec);
  * stream; without n_nonfinite it returns without synchronizing.
  * Errors: LRC_EINVAL for NULL pointers, m or n < 1, ldw < n, another group,
  * unknown precisions, misaligned codes or an output that overlaps W or another
- * output; LRC_EOVERFLOW, LRC_ENOMEM, LRC_EHIP, LRC_ENODEV as elsewhere.
+ * output; LRC_EOVERFLOW as elsewhere and for n above 2^34; LRC_ENOMEM, LRC_EHIP,
+ * LRC_ENODEV as elsewhere.
  */
 int lrc_q4_quantize(const void* W, int64_t ldw, int64_t m, int64_t n, int64_t group, int prec, void* codes,
                     void* scales, int sprec, void* values, int64_t* n_nonfinite);

@@ -385,10 +385,23 @@ void launch_t(const DistillArgs& a, float* loss, float* stats, const float* dlos
 template <int MODE>
 hipError_t launch_mode(const DistillArgs& a, float* loss, float* stats, const float* dloss, void* grad, int64_t ldg,
                        hipStream_t st) {
-    if (a.prec == P32) launch_t<float, MODE>(a, loss, stats, dloss, grad, ldg, st);
-    else if (a.prec == P16) launch_t<half_t, MODE>(a, loss, stats, dloss, grad, ldg, st);
-    else launch_t<bhalf_t, MODE>(a, loss, stats, dloss, grad, ldg, st);
-    return hipGetLastError();
+    return in_panels(a.rows, kRowPanel, [&](int64_t r, int64_t count) {
+        auto from = [&](auto* x, int64_t each = 1) { return x ? x + r * each : x; };
+        DistillArgs p = a;
+        p.logits = static_cast<const char*>(a.logits) + r * a.ld * elem_bytes(a.prec);
+        p.rows = count;
+        p.ids = a.ids + r * a.K;
+        p.top = static_cast<const char*>(a.top) + r * a.K * elem_bytes(a.tprec);
+        p.teacher_lse = from(a.teacher_lse);
+        p.weight = from(a.weight);
+        void* g = from(static_cast<char*>(grad), ldg * elem_bytes(a.prec));
+        float *l = from(loss), *s = from(stats, 4);
+        const float* d = from(dloss);
+        if (a.prec == P32) launch_t<float, MODE>(p, l, s, d, g, ldg, st);
+        else if (a.prec == P16) launch_t<half_t, MODE>(p, l, s, d, g, ldg, st);
+        else launch_t<bhalf_t, MODE>(p, l, s, d, g, ldg, st);
+        return hipGetLastError();
+    });
 }
 }  // namespace
 

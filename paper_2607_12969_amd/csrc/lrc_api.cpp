@@ -915,7 +915,7 @@ int lrc_q4_quantize(const void* W, int64_t ldw, int64_t m, int64_t n, int64_t gr
     if (ldw < n) return fail(LRC_EINVAL, "pitch %lld below n = %lld", (long long)ldw, (long long)n);
     if (!span_bytes(m, ldw, n, elem_bytes(prec), &wb) || !span_bytes(m, n, n, elem_bytes(prec), &vb))
         return fail(LRC_EOVERFLOW, "array sizes overflow int64");
-    if ((m * ((n + 511) / 512) + 3) / 4 > INT32_MAX) return fail(LRC_EOVERFLOW, "more than 2^31 - 1 workgroups");
+    if (n > (int64_t)1 << 34) return fail(LRC_EOVERFLOW, "n = %lld above 2^34", (long long)n);   // a row is one launch
     if (reinterpret_cast<uintptr_t>(codes) % 16) return fail(LRC_EINVAL, "codes must be 16-byte aligned");
     const Span w{W, wb, "W"}, c{codes, cb, "codes"}, s{scales, sb, "scales"}, v{values, vb, "values"};
     if ((rc = check_out(c, {w, s, v})) || (rc = check_out(s, {w, v})) || (rc = check_out(v, {w}))) return rc;

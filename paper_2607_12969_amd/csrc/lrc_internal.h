@@ -8,6 +8,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 namespace lrc {
 
 enum Prec { P64 = 0, P32 = 1, P16 = 2, PB16 = 3 };
@@ -206,6 +208,18 @@ hipError_t launch_reduce_rows(const double* part, int64_t count, int nsums, doub
                               hipStream_t stream);
 
 // ------------------------------------------------------------ output head
+// A grid holds fewer than 2^32 threads in a dimension; the launch of a larger one
+// returns no error and leaves the workgroups past the wrapped number out.  So
+// f(first, count) runs panels of at most `panel` rows, in order.
+template <typename F> inline hipError_t in_panels(int64_t total, int64_t panel, F&& f) {
+    for (int64_t i = 0; i < total; i += panel) {
+        const hipError_t e = f(i, std::min(panel, total - i));
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+// Rows of a panel where a row is a workgroup of up to 1024 threads.
+constexpr int64_t kRowPanel = (int64_t)1 << 21;
 // 4-bit weights: rows of E2M1 codes, two a byte, padded to whole 16 bytes, and
 // one scale per `group` (a power of two, 32 to 512) weights of a row.
 inline int64_t q4_row_bytes(int64_t n) { return (n + 31) / 32 * 16; }

@@ -123,16 +123,22 @@ __global__ __launch_bounds__(256) void k_q4_quantize(const T* __restrict__ W, in
 
 static __global__ void k_q4_zero(unsigned long long* p) { *p = 0ull; }
 
+constexpr int64_t kQ4Waves = (int64_t)1 << 25;        // of one launch: 2^31 threads
+
 template <typename T>
 static void quantize_t(const void* W, int64_t ldw, int64_t m, int64_t n, int64_t group, void* codes, void* scales,
                        int sprec, void* values, unsigned long long* nbad, hipStream_t st) {
     const int64_t wpr = q4_row_bytes(n) / 4, chunks = (wpr + 63) / 64, G = (n + group - 1) / group;
     const bool vec = reinterpret_cast<uintptr_t>(W) % 16 == 0 && ldw * sizeof(T) % 16 == 0 &&
                      (!values || (reinterpret_cast<uintptr_t>(values) % 16 == 0 && n * sizeof(T) % 16 == 0));
-    const unsigned grid = (unsigned)((m * chunks + 3) / 4);
     auto* kern = vec ? k_q4_quantize<T, true> : k_q4_quantize<T, false>;
-    hipLaunchKernelGGL(kern, dim3(grid), dim3(256), 0, st, (const T*)W, ldw, m, n, (int)(group / 8), (int)chunks,
-                       (unsigned*)codes, wpr, scales, G, sprec, (T*)values, nbad);
+    (void)in_panels(m, std::max<int64_t>(1, kQ4Waves / chunks), [&](int64_t i, int64_t rows) {
+        hipLaunchKernelGGL(kern, dim3((unsigned)((rows * chunks + 3) / 4)), dim3(256), 0, st, (const T*)W + i * ldw, ldw, rows,
+                           n, (int)(group / 8), (int)chunks, (unsigned*)codes + i * wpr, wpr,
+                           static_cast<char*>(scales) + i * G * elem_bytes(sprec), G, sprec,
+                           values ? (T*)values + i * n : nullptr, nbad);
+        return hipSuccess;
+    });
 }
 
 hipError_t launch_q4_quantize(const void* W, int64_t ldw, int prec, int64_t m, int64_t n, int64_t group, void* codes,
@@ -713,13 +719,14 @@ __global__ __launch_bounds__(256) void k_q4_join(const float* __restrict__ part,
 template <typename T>
 __global__ __launch_bounds__(256) void k_q4_pack(const T* __restrict__ X, int64_t ldx, int64_t n, int64_t b,
                                                  unsigned short* __restrict__ out, int64_t ldp) {
-    const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x, per = ldp / 8;
-    if (c >= b * per) return;
-    typename ActTraits<T>::frag f[ActTraits<T>::P];
-    load_act<T>(X + c / per * ldx, c % per * 8, n, f);
+    const int64_t per = ldp / 8, step = (int64_t)gridDim.x * 256;
+    for (int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x; c < b * per; c += step) {
+        typename ActTraits<T>::frag f[ActTraits<T>::P];
+        load_act<T>(X + c / per * ldx, c % per * 8, n, f);
 #pragma unroll
-    for (int p = 0; p < ActTraits<T>::P; ++p)
-        *reinterpret_cast<typename ActTraits<T>::frag*>(out + p * b * ldp + c * 8) = f[p];
+        for (int p = 0; p < ActTraits<T>::P; ++p)
+            *reinterpret_cast<typename ActTraits<T>::frag*>(out + p * b * ldp + c * 8) = f[p];
+    }
 }
 
 // ---- T' = diag(s) V^T x -----------------------------------------------------
@@ -963,18 +970,20 @@ __global__ __launch_bounds__(256) void k_q4_mid16(const T* __restrict__ X, int64
 __global__ __launch_bounds__(256) void k_q4_mid_finish(const float* __restrict__ part, int splits,
                                                        const void* __restrict__ s, int fprec, int64_t k, int64_t kp,
                                                        int64_t b, float* __restrict__ Tm) {
-    const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (e >= b * kp) return;
-    const int64_t r = e % kp;
-    float t = 0.0f;
-    if (r < k) {
-        t = sum_splits(part + e / kp * k + r, splits, b * k) * load_as_f32(s, r, fprec);
+    const int64_t step = (int64_t)gridDim.x * 256;
+    for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < b * kp; e += step) {
+        const int64_t r = e % kp;
+        float t = 0.0f;
+        if (r < k) t = sum_splits(part + e / kp * k + r, splits, b * k) * load_as_f32(s, r, fprec);
+        Tm[e] = t;
     }
-    Tm[e] = t;
 }
 
 // ------------------------------------------------------------------ plan --
 namespace {
+
+// Workgroups of the strided kernels above for `items`, one a thread up to 2^24.
+unsigned strided_grid(int64_t items) { return (unsigned)std::min<int64_t>((items + 255) / 256, 65536); }
 
 struct Q4Plan {
     bool tile;            // k_q4_tile, else k_q4_rows
@@ -1129,7 +1138,7 @@ hipError_t apply_t(const Q4Weights& w, Q4Args& a, int prec, Workspace& ws, hipSt
         else mid_f<T, 8>(p, w, a, mid, st);
         if (p.mid_finish) {
             KernelTimer t("q4_mid_finish", st);
-            hipLaunchKernelGGL(k_q4_mid_finish, dim3((unsigned)((a.b * a.kp + 255) / 256)), dim3(256), 0, st, mid,
+            hipLaunchKernelGGL(k_q4_mid_finish, dim3(strided_grid(a.b * a.kp)), dim3(256), 0, st, mid,
                                p.mid_splits, w.s, w.fprec, w.k, a.kp, a.b, Tm);
             a.Tm = Tm;
         } else {
@@ -1145,7 +1154,7 @@ hipError_t apply_t(const Q4Weights& w, Q4Args& a, int prec, Workspace& ws, hipSt
     a.splits = p.splits;
     if (p.pack) {
         KernelTimer t("q4_pack", st);
-        hipLaunchKernelGGL(k_q4_pack<T>, dim3((unsigned)((a.b * (p.ldp / 8) + 255) / 256)), dim3(256), 0, st,
+        hipLaunchKernelGGL(k_q4_pack<T>, dim3(strided_grid(a.b * (p.ldp / 8))), dim3(256), 0, st,
                            static_cast<const T*>(a.X), a.ldx, w.n, a.b, planes, p.ldp);
         a.X = planes;
         a.ldx = p.ldp;
@@ -1164,46 +1173,62 @@ hipError_t apply_t(const Q4Weights& w, Q4Args& a, int prec, Workspace& ws, hipSt
 
 }  // namespace
 
-// Larger batches run in panels (the grids' third dimension ends at 2^16).
+// Larger calls run in panels of X (the grids' third dimension ends at 2^16) and of W
+// (the tiles' grids: a thread for 32 outputs or more, for 8 or 16 in batches up to 32;
+// the row kernel's: 8 threads a row of W; so at most 2^31 and a half).
 constexpr int64_t kQ4Panel = 1 << 20;
+int64_t weight_panel(int64_t batch) { return std::min<int64_t>(1 << 28, ((int64_t)1 << 36) / batch); }
 
 size_t q4_apply_workspace_bytes(const Q4Weights& w, const void* X, int64_t ldx, int64_t batch, int prec) {
-    const int64_t rest = batch > kQ4Panel ? batch % kQ4Panel : 0;      // 0: whole panels alone
-    size_t bytes = plan_bytes(plan_q4(w, X, ldx, std::min(batch, kQ4Panel), prec));
-    if (rest) bytes = std::max(bytes, plan_bytes(plan_q4(w, X, ldx, rest, prec)));
+    size_t bytes = 0;
+    auto panel = [&](int64_t m, int64_t b) {
+        Q4Weights part = w;
+        part.m = m;
+        if (m && b) bytes = std::max(bytes, plan_bytes(plan_q4(part, X, ldx, b, prec)));
+    };
+    const int64_t b = std::min(batch, kQ4Panel), m = std::min(w.m, weight_panel(b));
+    for (int64_t rows : {b, batch % b}) {
+        panel(m, rows);
+        panel(w.m % m, rows);
+    }
     return bytes;
 }
 
 hipError_t launch_q4_apply(const Q4Weights& w, const void* X, int64_t ldx, void* Y, int64_t ldy, int64_t batch,
                            int prec, int yprec, Workspace& ws, hipStream_t st) {
-    for (int64_t b0 = 0; b0 < batch; b0 += kQ4Panel) {
+    const int64_t rb = q4_row_bytes(w.n), G = (w.n + w.group - 1) / w.group;
+    auto panel = [&](int64_t i0, int64_t rows, int64_t b0, int64_t b) {
+        Q4Weights part = w;
+        part.m = rows;
         Q4Args a{};
-        a.codes = static_cast<const unsigned char*>(w.codes);
-        a.scales = w.scales;
-        a.rb = q4_row_bytes(w.n);
-        a.G = (w.n + w.group - 1) / w.group;
+        a.codes = static_cast<const unsigned char*>(w.codes) + i0 * rb;
+        a.scales = static_cast<const char*>(w.scales) + i0 * G * elem_bytes(w.sprec);
+        a.rb = rb;
+        a.G = G;
         a.sprec = w.sprec;
         a.gshift = __builtin_ctzll((unsigned long long)w.group);
-        a.U = w.U;
+        a.U = w.k ? static_cast<const char*>(w.U) + i0 * w.k * elem_bytes(w.fprec) : nullptr;
         a.s = w.s;
         a.k = w.k;
         a.kp = round_up(w.k, 16);
         a.fprec = w.fprec;
         a.X = static_cast<const char*>(X) + b0 * ldx * elem_bytes(prec);
         a.ldx = ldx;
-        a.Y = static_cast<char*>(Y) + b0 * ldy * elem_bytes(yprec);
+        a.Y = static_cast<char*>(Y) + (b0 * ldy + i0) * elem_bytes(yprec);
         a.ldy = ldy;
         a.yprec = yprec;
-        a.m = w.m;
+        a.m = rows;
         a.n = w.n;
-        a.b = std::min(batch - b0, kQ4Panel);
+        a.b = b;
         ws.reset();
-        const hipError_t e = prec == P32   ? apply_t<float>(w, a, prec, ws, st)
-                             : prec == P16 ? apply_t<half_t>(w, a, prec, ws, st)
-                                           : apply_t<bhalf_t>(w, a, prec, ws, st);
-        if (e != hipSuccess) return e;
-    }
-    return hipSuccess;
+        return prec == P32   ? apply_t<float>(part, a, prec, ws, st)
+               : prec == P16 ? apply_t<half_t>(part, a, prec, ws, st)
+                             : apply_t<bhalf_t>(part, a, prec, ws, st);
+    };
+    const int64_t most = weight_panel(std::min(batch, kQ4Panel));
+    return in_panels(batch, kQ4Panel, [&](int64_t b0, int64_t b) {
+        return in_panels(w.m, most, [&](int64_t i0, int64_t rows) { return panel(i0, rows, b0, b); });
+    });
 }
 
 }  // namespace lrc

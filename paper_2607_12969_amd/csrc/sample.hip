@@ -1004,12 +1004,24 @@ SplitBuffers split_buffers(const SampleArgs& a, int parts, Workspace& ws) {
 
 template <typename T> hipError_t sample_t(const SampleArgs& a, Workspace& ws, hipStream_t st) {
     const SamplePlan p = plan_sample(a);
-    const dim3 rows((unsigned)a.rows), split(p.parts, (unsigned)a.rows), threads(kThreads);
-    if (p.parts == 1) {
-        KernelTimer t("sample_row", st);
-        hipLaunchKernelGGL(k_sample_row<T>, rows, threads, 0, st, a, p.whole);
-        return hipGetLastError();
-    }
+    const dim3 threads(kThreads);
+    if (p.parts == 1)
+        return in_panels(a.rows, kRowPanel, [&](int64_t r, int64_t count) {
+            auto from = [&](auto* x) { return x ? x + r : x; };
+            SampleArgs q = a;
+            q.logits = static_cast<const T*>(a.logits) + r * a.ld;
+            q.rows = count;
+            q.u = a.u + r;
+            q.temperature = from(a.temperature);
+            q.top_k = from(a.top_k);
+            q.top_p = from(a.top_p);
+            q.min_p = from(a.min_p);
+            q.tokens = a.tokens + r;
+            KernelTimer t("sample_row", st);
+            hipLaunchKernelGGL(k_sample_row<T>, dim3((unsigned)count), threads, 0, st, q, p.whole);
+            return hipGetLastError();
+        });
+    const dim3 rows((unsigned)a.rows), split(p.parts, (unsigned)a.rows);      // 16 rows at most
     const SplitBuffers b = split_buffers(a, p.parts, ws);
     if (ws.overrun) return hipErrorOutOfMemory;
     KernelTimer t("sample_split", st);
