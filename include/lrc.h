@@ -525,8 +525,10 @@ int lrc_sample(const void* logits, int64_t ld, int64_t rows, int64_t vocab, int 
  *   temperature   T > 0
  *   loss    device, rows:  w T^2 [ sum_k p_k (log p_k - log q_k)
  *                                  + r (log r - log Q) ],
- *           q = softmax(z / T), p_k = exp(t_k / T - lse), r = 1 - sum_k p_k (0
- *           without teacher_lse), Q the student's mass outside the named tokens
+ *           q = softmax(z / T), p_k = exp(t_k / T - lse), r = max(1 - sum_k p_k,
+ *           0) (0 without teacher_lse), Q the student's mass outside the named
+ *           tokens.  The p_k may sum above 1 (teacher_lse of other logits than
+ *           the stored ones, an id named twice); the gradient is that of this loss
  *   stats   device, rows x 4, or NULL: what lrc_distill_backward needs
  *   grad    device, rows x vocab of pitch ldg, in `prec`, or NULL: d (sum of
  *           the losses) / d logits; may be `logits` itself (ldg = ld)

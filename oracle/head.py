@@ -111,9 +111,10 @@ def distill(z, ids, top, T=1.0, lse=None, weight=None):
                 other = np.ones(V, bool)
                 other[named] = False
                 r, Q = max(1.0 - p.sum(), 0.0), q[other].sum()
+                g *= p.sum() + r                          # the teacher's whole mass: above 1 where the named ones are
                 if r > 0:
                     kl += r * (np.log(r) - np.log(Q))
-                    g[other] *= 1.0 - r / Q
+                    g[other] -= r * q[other] / Q
                 g[other & (q == 0)] = 0.0
         np.add.at(g, named, -p)
         loss[i] = w * T * T * kl

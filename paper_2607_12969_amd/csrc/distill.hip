@@ -4,14 +4,16 @@
 // With z the student's logits, q = softmax(z / T), and p the teacher's
 // probabilities of its K named tokens (p_k = exp(t_k / T - lse)),
 //   loss = w T^2 [ sum_k p_k (log p_k - log q_k) + r (log r - log Q) ],
-//   dloss/dz_j = w T (q_j - p_j)            for a named token j,
-//                w T (q_j - r q_j / Q)      for any other.
-// Without a given lse, lse = log sum_k exp(t_k / T) and r = 0 (the teacher
-// renormalized over the named tokens).  With the teacher's own lse, r = 1 -
-// sum_k p_k and Q = the student's mass outside the named tokens are one more
-// class.  The row is then summed without the named tokens (a bitmap of them in
-// LDS), relative to its own maximum: Q neither cancels nor underflows, and the
-// K named ones are added to the whole sum afterwards.
+//   dloss/dz_j = w T (P q_j - p_j)          for a named token j,
+//                w T (P q_j - r q_j / Q)    for any other,   P = sum_k p_k + r.
+// Without a given lse, lse = log sum_k exp(t_k / T), r = 0 and P = 1 (the teacher
+// renormalized over the named tokens).  With the teacher's own lse, r =
+// max(1 - sum_k p_k, 0) and Q = the student's mass outside the named tokens are
+// one more class; P is above 1 where the named probabilities are (logits rounded
+// after their lse was taken, a token named twice).  The row is then summed without
+// the named tokens (a bitmap of them in LDS), relative to its own maximum: Q
+// neither cancels nor underflows, and the K named ones are added to the whole sum
+// afterwards.
 //
 // Bound by memory: the logits are read once and the gradient written once.  A
 // row stays in registers between the maximum, the sum and the gradient (up to
@@ -184,12 +186,13 @@ __global__ __launch_bounds__(NT, NV <= 4 ? 8 : NV <= 8 ? 6 : 4) void k_distill_r
         lse = m + log_of(wave_sum(x));
     }
     auto prob = [&](int k) { return ids[k] >= 0 ? exp_of(teacher(k) - lse) : 0.0; };
-    double r = 0.0;
+    double r = 0.0, P = 1.0;
     if (tail) {
         double sp = 0.0;
         for (int k = lane; k < K; k += 64) sp += prob(k);
         sp = wave_sum(sp);
         r = sp < 1.0 ? 1.0 - sp : (sp != sp ? sp : 0.0);
+        P = sp > 1.0 ? sp : 1.0;
     }
 
     // m, s: maximum and sum of exp((z - m) / T) over the row, without the named
@@ -318,7 +321,7 @@ __global__ __launch_bounds__(NT, NV <= 4 ? 8 : NV <= 8 ? 6 : 4) void k_distill_r
 
     const double scale = (double)w * (double)a.temperature * (double)(MODE == BACKWARD && dloss ? dloss[i] : 1.0f);
     const bool sound = S > 0.0 && S <= 1e300;            // else the row holds NaN or nothing
-    double coef = scale * (double)__builtin_amdgcn_exp2f((m - M) * c) / S;
+    double coef = scale * P * (double)__builtin_amdgcn_exp2f((m - M) * c) / S;
     if (r != 0.0) coef -= s > 0.0f ? scale * r / (double)s : 0.0;
     const float cf = sound ? (float)coef : __builtin_nanf("");
     auto put = [&](T* at, const uint4v_t& v) {
@@ -342,7 +345,7 @@ __global__ __launch_bounds__(NT, NV <= 4 ? 8 : NV <= 8 ? 6 : 4) void k_distill_r
         double p = prob(k);
         if (dup)
             for (int q = k + 1; q < K; ++q) p += ids[q] == ids[k] ? prob(q) : 0.0;
-        const double q = sound ? (double)__builtin_amdgcn_exp2f((zk[k] - M) * c) / S : (double)__builtin_nanf("");
+        const double q = sound ? P * (double)__builtin_amdgcn_exp2f((zk[k] - M) * c) / S : (double)__builtin_nanf("");
         out[ids[k]] = from_f32<T>((float)(scale * (q - p)));
     }
 }

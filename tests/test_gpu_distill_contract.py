@@ -1,0 +1,92 @@
+"""What the interface says of the distillation loss beyond the common case, against the binary64 oracle.
+
+Tolerances.  A probability of the student is held to 1e-5 of itself (a few 2^-24 and the rounding of its argument, at most
+40 here), one of the teacher to a few 2^-24 of itself, so a gradient entry to 1e-5 w T (mass q + p) plus one rounding to its
+type, mass being the sum of the teacher's classes; the loss to 1e-5 of its terms' size w T^2 (|loss| + mass)."""
+import numpy as np
+import pytest
+
+from oracle import head as H
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+DT = {"fp32": torch.float32, "fp16": torch.float16, "bf16": torch.bfloat16}
+UNIT = {"fp32": 2.0 ** -24, "fp16": 2.0 ** -11, "bf16": 2.0 ** -8}
+TINY = {"fp32": 1e-38, "fp16": 2.0 ** -25, "bf16": 1e-38}
+
+
+@pytest.fixture(scope="module")
+def lrc():
+    from paper_2607_12969_amd import lrc as mod
+    assert torch.cuda.is_available()
+    mod.lib()
+    return mod
+
+
+def up(t):
+    return t.double().cpu().numpy()
+
+
+def heavy(seed, rows, V, K, prec, tprec, T):
+    """Teachers whose named probabilities sum above 1: by a lse of other logits than the stored ones, by the stored
+    logits' rounding, by a token named twice.  Every fourth row stays below 1."""
+    rng = np.random.default_rng(seed)
+    teacher = 2.5 * rng.normal(size=(rows, V))
+    z = torch.from_numpy(teacher + 0.5 * rng.normal(size=(rows, V))).to(DT[prec]).cuda()
+    ids = np.argsort(-teacher, 1)[:, :K].copy()
+    ids[2::4, 1] = ids[2::4, 0]
+    top = torch.from_numpy(np.take_along_axis(teacher, ids, 1)).to(DT[tprec]).cuda()
+    lse = np.log(np.exp(teacher / T).sum(1))
+    named = np.exp(np.take_along_axis(teacher, ids, 1) / T - lse[:, None]).sum(1)
+    lse[0::4] += np.log(named[0::4]) - 0.4               # sums of about 1.5
+    lse[1::4] += np.log(named[1::4])                     # about 1, by rounding above or below
+    lse[2::4] += np.log(named[2::4]) - 0.1
+    lse[3::4] += 0.5
+    w = torch.from_numpy((rng.random(rows) + 0.5).astype(np.float32)).cuda()
+    return z, torch.from_numpy(ids).cuda(), top, torch.from_numpy(lse.astype(np.float32)).cuda(), w
+
+
+def check(loss, grad, z, ids, top, T, lse, w, prec, scale=None):
+    host_w = up(w) if scale is None else up(w) * up(scale)
+    L, _ = H.distill(up(z), ids.cpu().numpy(), up(top), T, up(lse), up(w))
+    _, G = H.distill(up(z), ids.cpu().numpy(), up(top), T, up(lse), host_w)
+    p = np.exp(up(top) / T - up(lse)[:, None])
+    mass = np.maximum(p.sum(1), 1.0)
+    if loss is not None:
+        assert (abs(up(loss) - L) <= 1e-5 * up(w) * T * T * (abs(L) / (up(w) * T * T) + mass)).all()
+    if grad is not None:
+        q = np.exp(up(z) / T - (up(z) / T).max(1, keepdims=True))
+        size = mass[:, None] * q / q.sum(1, keepdims=True)
+        np.add.at(size, (np.arange(len(p))[:, None], ids.cpu().numpy()), p)
+        tol = 1e-5 * (host_w * T)[:, None] * size + UNIT[prec] * abs(G) + TINY[prec]
+        assert (abs(up(grad) - G) <= tol).all(), float((abs(up(grad) - G) / tol).max())
+
+
+@pytest.mark.parametrize("prec", ["fp32", "fp16", "bf16"])
+@pytest.mark.parametrize("tprec", ["fp32", "fp16", "bf16"])
+@pytest.mark.parametrize("rows,V,K,T", [(8, 200, 64, 1.0), (5, 1001, 20, 2.0), (4, 70001, 40, 1.0), (4, 300007, 9, 1.5)])
+def test_named_probabilities_above_one(lrc, prec, tprec, rows, V, K, T):
+    z, ids, top, lse, w = heavy(V + K, rows, V, K, prec, tprec, T)
+    kw = dict(temperature=T, teacher_lse=lse, weight=w)
+    loss, grad = lrc.distill(z, ids, top, **kw)
+    check(loss, grad, z, ids, top, T, lse, w, prec)
+    loss, stats = lrc.distill_forward(z, ids, top, **kw)
+    check(loss, None, z, ids, top, T, lse, w, prec)
+    check(None, lrc.distill_backward(z, ids, top, stats, **kw), z, ids, top, T, lse, w, prec)
+    scale = torch.rand(rows, device="cuda") + 0.5
+    check(None, lrc.distill_backward(z, ids, top, stats, dloss=scale, **kw), z, ids, top, T, lse, w, prec, scale)
+
+
+def test_named_probabilities_above_one_against_differences(lrc):
+    """Differences of the kernel's own loss: 1e-6 of loss rounding over the step, and the third derivative's h^2 / 6."""
+    z, ids, top, lse, w = heavy(3, 8, 11, 4, "fp32", "bf16", 1.5)
+    kw = dict(temperature=1.5, teacher_lse=lse, weight=w)
+    _, grad = lrc.distill(z, ids, top, **kw)
+    h = 2.0 ** -6
+    for j in range(11):
+        d = torch.zeros_like(z)
+        d[:, j] = h
+        num = (lrc.distill_forward(z + d, ids, top, **kw)[0] - lrc.distill_forward(z - d, ids, top, **kw)[0]) / (2 * h)
+        assert (num - grad[:, j]).abs().max() < 1e-3
+    assert grad.double().sum(1).abs().max() < 1e-4       # the entries' tolerances summed: 1e-5 w T 2 mass
