@@ -123,7 +123,7 @@ __global__ __launch_bounds__(NT, NV <= 4 ? 8 : NV <= 8 ? 6 : 4) void k_distill_r
     const bool tail = a.teacher_lse != nullptr;
     auto nothing = [&] {
         if (MODE != BACKWARD && t == 0) loss[i] = 0.0f;
-        if (MODE == FORWARD && stats && t < 4) stats[i * 4 + t] = 0.0f;
+        if (MODE != BACKWARD && stats && t < 4) stats[i * 4 + t] = 0.0f;
         if (MODE != FORWARD) zero_row(out, V, NT);
     };
     if (w == 0.0f) {                        // a row that does not count
@@ -315,7 +315,7 @@ __global__ __launch_bounds__(NT, NV <= 4 ? 8 : NV <= 8 ? 6 : 4) void k_distill_r
                 kl += r * (log_of(r) - ((double)(m - M) * invT + log_of((double)s) - logS));
             loss[i] = (float)((double)w * (double)a.temperature * (double)a.temperature * kl);
         }
-        if (MODE == FORWARD && stats && t < 4) stats[i * 4 + t] = t == 0 ? M : t == 1 ? (float)S : t == 2 ? m : s;
+        if (stats && t < 4) stats[i * 4 + t] = t == 0 ? M : t == 1 ? (float)S : t == 2 ? m : s;
     }
     if (MODE == FORWARD) return;
 

@@ -90,3 +90,31 @@ def test_named_probabilities_above_one_against_differences(lrc):
         num = (lrc.distill_forward(z + d, ids, top, **kw)[0] - lrc.distill_forward(z - d, ids, top, **kw)[0]) / (2 * h)
         assert (num - grad[:, j]).abs().max() < 1e-3
     assert grad.double().sum(1).abs().max() < 1e-4       # the entries' tolerances summed: 1e-5 w T 2 mass
+
+
+@pytest.mark.parametrize("prec", ["fp32", "fp16", "bf16"])
+@pytest.mark.parametrize("V", [1, 203, 20011, 70001, 300007])
+@pytest.mark.parametrize("tail", [False, True])
+def test_one_call_gives_loss_statistics_and_gradient(lrc, prec, V, tail):
+    """The C entry with all three outputs: the statistics are those that the gradient alone takes."""
+    rows, K, T = 5, min(V, 7), 1.5
+    z, ids, top, lse, w = heavy(V, rows, V, K, prec, "fp32", T) if V > 1 else (
+        torch.ones(rows, 1, dtype=DT[prec], device="cuda"), torch.zeros(rows, 1, dtype=torch.int64, device="cuda"),
+        torch.ones(rows, 1, device="cuda"), torch.ones(rows, device="cuda"), torch.ones(rows, device="cuda"))
+    w[3] = 0                                             # a row that does not count
+    ids[4] = -1                                          # a teacher that names nothing
+    lse = lse if tail else None
+    kw = dict(temperature=T, teacher_lse=lse, weight=w)
+    grad = torch.empty_like(z)
+    loss, stats = torch.empty(rows, device="cuda"), torch.full((rows, 4), float("nan"), device="cuda")
+    code = {"fp32": lrc.FP32, "fp16": lrc.FP16, "bf16": lrc.BF16}
+    lrc.lib().lrc_set_stream(torch.cuda.current_stream().cuda_stream)
+    assert lrc.lib().lrc_distill(z.data_ptr(), V, rows, V, code[prec], ids.data_ptr(), top.data_ptr(), K, lrc.FP32,
+                                 lse.data_ptr() if tail else None, w.data_ptr(), T, loss.data_ptr(), stats.data_ptr(),
+                                 grad.data_ptr(), V) == 0
+    want_loss, want_stats = lrc.distill_forward(z, ids, top, **kw)
+    # the two calls sum a row in their own fixed orders; w T^2 (|loss| + mass) is below 10, w T 2 mass below 7
+    assert torch.allclose(loss, want_loss, rtol=0, atol=1e-4)
+    assert torch.allclose(stats, want_stats, rtol=1e-5, atol=0)
+    back = lrc.distill_backward(z, ids, top, stats, **kw)
+    assert torch.allclose(back.float(), grad.float(), rtol=2.1 * UNIT[prec], atol=1.4e-4)
