@@ -534,8 +534,9 @@ int lrc_sample(const void* logits, int64_t ld, int64_t rows, int64_t vocab, int 
  *           the losses) / d logits; may be `logits` itself (ldg = ld)
  * A row whose teacher names nothing gives 0 without teacher_lse.  Terms of
  * p_k = 0 are 0; a named token that the student gives -infinity makes the loss
- * infinite; a row that holds a NaN or nothing but -infinity gives NaN.  Sums are split in a
- * fixed order: bitwise reproducible.
+ * infinite; a row that holds a NaN or nothing but -infinity gives NaN, and so does
+ * a NaN among the named teacher logits (in the loss and the named tokens'
+ * gradients).  Sums are split in a fixed order: bitwise reproducible.
  * Errors: LRC_EINVAL for NULL logits, ids, top or loss, rows < 0, vocab < 1 or
  * >= 2^31, K outside [1, LRC_DISTILL_MAX_TOP], pitches below vocab, T not a
  * positive finite number, unknown precisions or an output that overlaps an

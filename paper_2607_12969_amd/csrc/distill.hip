@@ -172,10 +172,15 @@ __global__ __launch_bounds__(NT, NV <= 4 ? 8 : NV <= 8 ? 6 : 4) void k_distill_r
         lse = (double)a.teacher_lse[i];
     } else {
         float mx = kNegInf;
+        bool nan = false;
         for (int k = lane; k < K; k += 64)
-            if (ids[k] >= 0) mx = __builtin_fmaxf(mx, tk[k]);
+            if (ids[k] >= 0) {
+                mx = __builtin_fmaxf(mx, tk[k]);
+                nan |= tk[k] != tk[k];
+            }
         mx = wave_max(mx);
-        if (mx == kNegInf) {                // the teacher names nothing
+        nan = __builtin_amdgcn_ballot_w64(nan) != 0;
+        if (mx == kNegInf && !nan) {        // the teacher names nothing
             nothing();
             return;
         }
@@ -192,7 +197,7 @@ __global__ __launch_bounds__(NT, NV <= 4 ? 8 : NV <= 8 ? 6 : 4) void k_distill_r
         for (int k = lane; k < K; k += 64) sp += prob(k);
         sp = wave_sum(sp);
         r = sp < 1.0 ? 1.0 - sp : (sp != sp ? sp : 0.0);
-        P = sp > 1.0 ? sp : 1.0;
+        P = sp < 1.0 ? 1.0 : sp;
     }
 
     // m, s: maximum and sum of exp((z - m) / T) over the row, without the named

@@ -118,3 +118,23 @@ def test_one_call_gives_loss_statistics_and_gradient(lrc, prec, V, tail):
     assert torch.allclose(stats, want_stats, rtol=1e-5, atol=0)
     back = lrc.distill_backward(z, ids, top, stats, **kw)
     assert torch.allclose(back.float(), grad.float(), rtol=2.1 * UNIT[prec], atol=1.4e-4)
+
+
+@pytest.mark.parametrize("V", [50, 40000])
+def test_teacher_that_names_only_nan(lrc, V):
+    """A NaN among the named teacher logits makes the row's loss NaN, beside other values or alone."""
+    z = torch.randn(4, V, device="cuda")
+    ids = torch.tensor([[1, 2, 3]] * 4, device="cuda")
+    top = torch.tensor([[1.0, 0.5, 0.0]] * 4, device="cuda")
+    top[1] = float("nan")
+    top[2, 1] = float("nan")
+    top[3] = float("nan")
+    ids[3, :] = -1                                       # NaN in unused slots does not count
+    for lse in (None, torch.full((4,), 2.0, device="cuda")):
+        loss, grad = lrc.distill(z, ids, top, teacher_lse=lse)
+        floss, stats = lrc.distill_forward(z, ids, top, teacher_lse=lse)
+        back = lrc.distill_backward(z, ids, top, stats, teacher_lse=lse)
+        for x in (loss, floss):
+            assert x[[0, 3]].isfinite().all() and x[1].isnan() and x[2].isnan()
+        for x in (grad, back):
+            assert x[[0, 3]].isfinite().all() and x[1, 1:4].isnan().all() and x[2, 1:4].isnan().all()
