@@ -831,7 +831,8 @@ __global__ __launch_bounds__(256) void k_q4_mid(const T* __restrict__ X, int64_t
 
 // The same for 16-bit activations and factors, on the 16-bit matrix cores with
 // exact products: both binary16, or bfloat16 with the one of the two that is
-// binary16 as the sum of two bfloat16 values (8 + 3 bits).  Steps of 128 rows of V
+// binary16 as the sum of two bfloat16 values (8 + 3 bits; an infinity of the other
+// meets the first alone, as the second may be 0).  Steps of 128 rows of V
 // lie transposed in LDS ([rank][column], PV planes).  FV: V is binary16.
 // 4096 rows of 8192, k = 65: 53 us, k_q4_mid 86.
 template <typename T, bool FV, int F, int TW>
@@ -850,6 +851,16 @@ __global__ __launch_bounds__(256) void k_q4_mid16(const T* __restrict__ X, int64
     const int w = (int)std::min<int64_t>(k - r0, 16 * F);
     const int64_t j0 = s * chunk, j1 = std::min(n, j0 + chunk);
     const T* x = X + std::min(b0 + (TW == 4 ? 16 * wave : 0) + lr, b - 1) * ldx;
+    // x for the low plane of V: infinities and NaN, which the high plane takes, as 0
+    auto finite = [](frag f) {
+        uint4v_t v = __builtin_bit_cast(uint4v_t, f);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const unsigned top = ((v[q] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;    // a bit per special half
+            v[q] &= ~((top << 1) - (top >> 15));
+        }
+        return __builtin_bit_cast(frag, v);
+    };
     auto put = [&](int r, int j, unsigned h) {
         if (PV == 1) {
             lv[r * PITCH + j] = (unsigned short)h;
@@ -926,17 +937,18 @@ __global__ __launch_bounds__(256) void k_q4_mid16(const T* __restrict__ X, int64
         }
         __syncthreads();
 #pragma unroll
-        for (int h = 0; h < (TW == 4 ? 4 : 1); ++h)
+        for (int h = 0; h < (TW == 4 ? 4 : 1); ++h) {
+            const frag xl = PV == 2 ? finite(xa[h][0]) : xa[h][0];
 #pragma unroll
             for (int f = 0; f < F; ++f) {
                 const int at = (16 * f + lr) * PITCH + (TW == 4 ? h : wave) * 32 + lg * 8;
+                if constexpr (PV == 2)
+                    acc[f] = M::mfma(xl, *reinterpret_cast<const frag*>(lv + 16 * F * PITCH + at), acc[f]);
+                const frag vf = *reinterpret_cast<const frag*>(lv + at);
 #pragma unroll
-                for (int q = PV - 1; q >= 0; --q) {
-                    const frag vf = *reinterpret_cast<const frag*>(lv + q * 16 * F * PITCH + at);
-#pragma unroll
-                    for (int p = PX - 1; p >= 0; --p) acc[f] = M::mfma(xa[h][p], vf, acc[f]);
-                }
+                for (int p = PX - 1; p >= 0; --p) acc[f] = M::mfma(xa[h][p], vf, acc[f]);
             }
+        }
     }
     if (TW == 4) {
 #pragma unroll

@@ -1,0 +1,51 @@
+"""What the interface says of the 4-bit product and quantization beyond the common case."""
+import numpy as np
+import pytest
+
+from oracle import head as H
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+DT = {"fp32": torch.float32, "fp16": torch.float16, "bf16": torch.bfloat16}
+
+
+@pytest.fixture(scope="module")
+def lrc():
+    from paper_2607_12969_amd import lrc as mod
+    assert torch.cuda.is_available()
+    mod.lib()
+    return mod
+
+
+@pytest.mark.parametrize("prec", ["fp16", "bf16", "fp32"])
+@pytest.mark.parametrize("fprec", ["fp16", "bf16", "fp32"])
+@pytest.mark.parametrize("b", [1, 5, 20])
+@pytest.mark.parametrize("k", [1, 33, 90])
+def test_infinite_activations_through_the_compensation(lrc, prec, fprec, b, k):
+    """Weights, U and s above 0 and one sign a row of V: an infinity gives the infinity of the sums, not NaN; and the
+    other rows are those of the call without it."""
+    rng = np.random.default_rng(b + k)
+    m, n = 96, 200
+    codes = torch.from_numpy(H.pack(rng.integers(1, 8, (m, n)))).cuda()
+    scales = torch.ones(m, -(-n // 32), dtype=torch.float16, device="cuda")
+    sign = torch.ones(n, 1)
+    sign[1::2] = -1
+    mixed = torch.from_numpy(1.0 + rng.random((n, k))).float()
+    mixed[::3] = 1.0                                     # one significant bit: what a split leaves is 0
+    U, s, V = (x.to(DT[fprec]).cuda() for x in (1.0 + torch.rand(m, k), torch.ones(k), mixed * sign))
+    X = torch.from_numpy(rng.random((b, n))).to(DT[prec]).cuda()
+    clean = lrc.q4_apply(codes, scales, X, 32, (U, s, V), out_dtype=torch.float32)
+    assert clean.isfinite().all()
+    for j, want in ((0, np.inf), (3, None), (7, None), (6, np.inf), (199, None)):
+        Z = X.clone()
+        Z[b - 1, j] = float("inf")
+        Y = lrc.q4_apply(codes, scales, Z, 32, (U, s, V), out_dtype=torch.float32)
+        assert torch.equal(Y[:b - 1], clean[:b - 1])
+        if want is None:                                 # + infinity from W, - infinity from the compensation
+            assert Y[b - 1].isnan().all()
+        else:
+            assert (Y[b - 1] == want).all(), (prec, fprec, j)
+    Z[b - 1, 199] = float("nan")
+    Y = lrc.q4_apply(codes, scales, Z, 32, (U, s, V), out_dtype=torch.float32)
+    assert torch.equal(Y[:b - 1], clean[:b - 1]) and Y[b - 1].isnan().all()
