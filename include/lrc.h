@@ -35,6 +35,13 @@
  *     (device, stream), allocated on first use and released by
  *     lrc_shutdown().  Calls on the same stream are ordered; calls issued
  *     concurrently from several host threads on the SAME stream race on it.
+ *   Graph capture.  A call captured into a HIP graph works in the workspace of
+ *     the stream it was captured on.  That memory stays until lrc_shutdown(),
+ *     also when a later call on the stream needs more and gets a new one.
+ *     Graphs that were captured on one stream share its workspace: their
+ *     replays must not overlap with each other, nor with calls on that stream.
+ *     Calls that wait for a result (certificates, factorizations, counts)
+ *     cannot be captured.
  */
 #ifndef LRC_H
 #define LRC_H
@@ -571,7 +578,8 @@ int lrc_set_stream(void* hip_stream);
  * The pointer stays valid until the next call on the same thread. */
 const char* lrc_last_error(void);
 
-/* Releases every library-owned device workspace.  Later calls allocate
+/* Releases every library-owned device workspace, those of captured graphs
+ * included (such graphs must not be replayed again).  Later calls allocate
  * again.  No call may be in flight. */
 void lrc_shutdown(void);
 

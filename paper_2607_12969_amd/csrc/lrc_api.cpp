@@ -236,20 +236,43 @@ KernelTimer::~KernelTimer() {
 
 // ------------------------------------------------------------- Workspace --
 namespace lrc {
+static bool is_capturing(hipStream_t stream) {
+    hipStreamCaptureStatus s = hipStreamCaptureStatusNone;
+    if (!stream) return false;            // the null stream takes no capture
+    if (hipStreamIsCapturing(stream, &s) != hipSuccess) {
+        (void)hipGetLastError();
+        return false;
+    }
+    return s != hipStreamCaptureStatusNone;
+}
+
 hipError_t Workspace::reserve(size_t bytes, hipStream_t stream) {
     bytes = (size_t)round_up((int64_t)bytes, 256) + 256;
+    const bool capturing = is_capturing(stream);
     if (bytes > cap) {
         // grow by at least half the current size, so that a sequence of
         // slightly larger calls does not reallocate every time
         const size_t want = std::max(bytes, cap + cap / 2);
-        if (base) {
+        if (base && (captured || capturing)) {
+            // the replays of a graph go on using it; under capture there is no waiting for its last call
+            try {
+                held.push_back(base);
+            } catch (...) {
+                return hipErrorOutOfMemory;
+            }
+        } else if (base) {
             hipError_t e = hipStreamSynchronize(stream);
             if (e != hipSuccess) return e;
             (void)hipFree(base);
-            base = nullptr;
-            cap = 0;
         }
+        base = nullptr;
+        cap = 0;
+        captured = false;
+        // an allocation is no work of the stream, but is let into a capture in this mode alone
+        hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;
+        if (capturing) (void)hipThreadExchangeStreamCaptureMode(&mode);
         hipError_t e = hipMalloc(reinterpret_cast<void**>(&base), want);
+        if (capturing) (void)hipThreadExchangeStreamCaptureMode(&mode);
         if (e != hipSuccess) {
             base = nullptr;
             (void)hipGetLastError();   // reported here; a later launch check must not see it
@@ -257,6 +280,7 @@ hipError_t Workspace::reserve(size_t bytes, hipStream_t stream) {
         }
         cap = want;
     }
+    captured |= capturing;
     used = 0;
     return hipSuccess;
 }
@@ -275,7 +299,10 @@ void* Workspace::take(size_t bytes) {
 
 void Workspace::release() {
     if (base) (void)hipFree(base);
+    for (char* p : held) (void)hipFree(p);
+    held.clear();
     base = nullptr;
+    captured = false;
     cap = used = 0;
 }
 }  // namespace lrc

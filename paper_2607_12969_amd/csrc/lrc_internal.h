@@ -9,6 +9,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <vector>
 
 namespace lrc {
 
@@ -26,6 +27,8 @@ struct Workspace {
     size_t cap = 0;
     size_t used = 0;
     bool overrun = false;         // a take() exceeded the reservation
+    bool captured = false;        // a graph holds base
+    std::vector<char*> held;      // earlier buffers that graphs hold
     hipError_t reserve(size_t bytes, hipStream_t stream);
     void* take(size_t bytes);     // nullptr (and overrun = true) past the reservation
     void reset() { used = 0; overrun = false; }
