@@ -578,6 +578,7 @@ def q4_apply(codes, scales, X, group: int = 128, factors=None, out_dtype=None, Y
     V n x k, one dtype) or None.  Y (batch x m) is in out_dtype (X's unless
     given); a caller-supplied Y sets it."""
     _need(X.dim() == 2 and codes.dim() == 2 and scales.dim() == 2, "X, codes and scales must be matrices")
+    _need(group in (32, 64, 128, 256, 512), "group must be 32, 64, 128, 256 or 512")
     b, n = X.shape
     m = codes.shape[0]
     if codes.dtype != _uint8():
