@@ -450,10 +450,13 @@ int64_t lrc_q4_storage_bytes(int64_t m, int64_t n, int64_t group, int sprec);
  *           stores the number of groups that hold a NaN or an infinity or whose
  *           scale overflows `sprec`; such a group gets the scale NaN.
  * scale = max |w| of the group times 1/6 (each rounded to binary32, binary64 for
- * LRC_FP64), rounded to binary32 and then to sprec; a code is the E2M1 value nearest to the quotient w / scale (rounded to binary32;
- * binary64 for LRC_FP64), ties to the even code, magnitudes above 6 become 6.
- * A group whose scale is 0 gets codes 0.  Enqueued on the calling thread's
- * stream; without n_nonfinite it returns without synchronizing.
+ * LRC_FP64), rounded to binary32 and then to sprec; a code is the E2M1 value
+ * nearest to the quotient w / scale (rounded to binary32; binary64 for LRC_FP64),
+ * ties to the even code, magnitudes above 6 become 6, and bit 3 is the sign of w,
+ * that of -0 included.  A group whose scale is 0 (all weights 0, or too small for
+ * sprec) gets magnitude 0 and keeps its signs: codes 0 and 8, values 0 and -0.  A
+ * group whose scale is NaN gets codes 0.  Enqueued on the calling thread's stream;
+ * without n_nonfinite it returns without synchronizing.
  * Errors: LRC_EINVAL for NULL pointers, m or n < 1, ldw < n, another group,
  * unknown precisions, misaligned codes or an output that overlaps W or another
  * output; LRC_EOVERFLOW as elsewhere and for n above 2^34; LRC_ENOMEM, LRC_EHIP,

@@ -49,3 +49,22 @@ def test_infinite_activations_through_the_compensation(lrc, prec, fprec, b, k):
     Z[b - 1, 199] = float("nan")
     Y = lrc.q4_apply(codes, scales, Z, 32, (U, s, V), out_dtype=torch.float32)
     assert torch.equal(Y[:b - 1], clean[:b - 1]) and Y[b - 1].isnan().all()
+
+
+@pytest.mark.parametrize("prec", ["fp16", "bf16", "fp32", "fp64"])
+def test_groups_of_scale_zero_keep_their_signs(lrc, prec):
+    """Weights too small for the scale's type: magnitude 0, the weight's sign; a group of scale NaN: codes 0."""
+    tiny = 2.0 ** -24 if prec == "fp16" else 1e-30       # times 1 / 6 rounds to 0 in binary16
+    W = torch.zeros(3, 96, dtype=torch.float64)
+    W[0, :32:2], W[0, 1:32:2] = -tiny, tiny
+    W[1, 32:64:3] = -0.0
+    W[2, 64:] = -1.0
+    W[2, 70] = float("nan")
+    W = W.to({**DT, "fp64": torch.float64}[prec]).cuda()
+    codes, scales, values = lrc.q4_quantize(W, 32, torch.float16, values=True)
+    c = torch.stack((codes & 15, codes >> 4), 2).view(3, -1)
+    neg = torch.signbit(W)
+    neg[2, 64:] = False
+    assert torch.equal(c, 8 * neg.to(torch.uint8))
+    assert torch.equal(torch.signbit(values[:2]), neg[:2]) and not values[:2].any() and values[2, 64:].isnan().all()
+    assert not scales[:2].any() and scales[2].isnan().tolist() == [False, False, True]
