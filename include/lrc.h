@@ -479,8 +479,11 @@ int lrc_q4_quantize(const void* W, int64_t ldw, int64_t m, int64_t n, int64_t gr
  * Products of codes and activations are exact and summed in binary32 (a
  * binary32 activation as the exact sum of three bfloat16 values; below 2^-110
  * its last bits may be lost), the scale of a group enters in binary32, and so
- * does the compensation, whose (X V) diag(s) is not rounded further.  Sums are
- * split in a fixed order: bitwise reproducible.  Infinities and NaN in X reach
+ * does the compensation, whose (X V) diag(s) is not rounded further.  The scale
+ * multiplies sums of up to 128 products of a group, which pass binary32's range to
+ * an infinity sooner than the scaled weights would: with |x| below 2^118 (any
+ * binary16 activation) they do not.  Sums are split in a fixed order: bitwise
+ * reproducible.  Infinities and NaN in X reach
  * the outputs of their row as in the sums above (a zero weight times an
  * infinity is NaN).
  * Errors: LRC_EINVAL for NULL pointers, m or n < 1, batch or k < 0, k >

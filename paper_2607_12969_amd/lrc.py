@@ -8,6 +8,11 @@ module raises on first use.
 
 Precision follows the tensors' dtype: float64 -> FP64, float32 -> FP32,
 float16 -> FP16 (FP32 accumulation); the output-head calls also take bfloat16.
+
+Every call returns plain tensors and records nothing for autograd, also for
+inputs that require a gradient.  Of the output-head calls the distillation
+loss has a gradient (distill, distill_backward: by the student's logits); the
+4-bit product has no backward call.
 """
 from __future__ import annotations
 

@@ -68,3 +68,18 @@ def test_groups_of_scale_zero_keep_their_signs(lrc, prec):
     assert torch.equal(c, 8 * neg.to(torch.uint8))
     assert torch.equal(torch.signbit(values[:2]), neg[:2]) and not values[:2].any() and values[2, 64:].isnan().all()
     assert not scales[:2].any() and scales[2].isnan().tolist() == [False, False, True]
+
+
+@pytest.mark.parametrize("prec", ["bf16", "fp32"])
+@pytest.mark.parametrize("group", [32, 64, 128, 512])
+@pytest.mark.parametrize("b", [1, 20, 200])
+def test_large_activations_stay_finite(lrc, prec, group, b):
+    """|x| just below 2^118 at the largest weights of one sign: group sums before their scale stay in range.  All terms
+    are positive: a relative error of (n + n / group + 8) 2^-24."""
+    m, n = 40, 1030
+    codes = torch.from_numpy(H.pack(np.full((m, n), 7))).cuda()
+    scales = torch.full((m, -(-n // group)), 2.0 ** -14, dtype=torch.float16, device="cuda")
+    x = 2.0 ** 118 * (1 - 2.0 ** -8)
+    Y = lrc.q4_apply(codes, scales, torch.full((b, n), x, dtype=DT[prec], device="cuda"), group, out_dtype=torch.float32)
+    want = n * 6 * 2.0 ** -14 * x
+    assert ((Y.double() / want - 1).abs() <= (n + n / group + 8) * 2.0 ** -24).all()
