@@ -364,13 +364,13 @@ void launch_nv(const DistillArgs& a, float* loss, float* stats, const float* dlo
                        dloss, (T*)grad, ldg);
 }
 
-// The step takes the smallest workgroup whose registers hold the row: 4096 x 65536
-// bfloat16, K = 64, 230 us against 262 to 282 read twice.  The forward and the
-// backward pass read a row once and need no registers for it: workgroups of 256
-// run more rows at a time (4096 x 65536 forward 106 us against 143 with 1024
-// threads, 2000 x 10007 15 against 36), those of 1024 suit few rows (64 x 65536
-// 11.5 against 15.3, backward 8.8 against 13.6) and the backward pass of long ones
-// (4096 x 65536 209 against 222).
+// The step takes the smallest workgroup whose registers hold the row.  bfloat16, K =
+// 64, both sides measured in turn: 4096 x 65536 215 us against 241 read twice, 2000 x
+// 10007 30 against 45.  The forward and the backward pass read a row once and need
+// no registers for it: workgroups of 256 run more rows at a time (4096 x 65536
+// forward 97 us against 130 with 1024 threads, 2000 x 10007 16 against 37, backward
+// 23 against 29), those of 1024 suit few rows (64 x 65536 12 against 15, backward 10
+// against 15) and the backward pass of long ones (4096 x 65536 204 against 219).
 template <typename T, int MODE>
 void launch_t(const DistillArgs& a, float* loss, float* stats, const float* dloss, void* grad, int64_t ldg,
               hipStream_t st) {

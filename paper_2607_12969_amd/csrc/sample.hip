@@ -701,12 +701,16 @@ __global__ __launch_bounds__(kThreads) void k_sample_row(SampleArgs a, unsigned 
 // The passes over a row become launches, each on `parts` workgroups a row (16 L
 // logits each), joined through memory; the last one, a workgroup a row, does what
 // concerns the lists and draws inside one part.  Four launches cost more than the
-// passes save until few rows are long.  FP32, us, one workgroup a row against this,
-// no filter / top-p / top-k / both:
-//     1 x 65536     16 34 22 27    18 31 25 31
-//     1 x 131072    22 55 30 34    19 36 25 31
-//     8 x 131072    25 56 32 37    22 38 29 34
-//     48 x 131072   26 58 33 38    29 50 33 38
+// passes save until few rows are long, and from 17 rows the parts of all rows no
+// longer fit the 256 compute units at once.  FP32, us, one workgroup a row against
+// this, no filter / top-p / top-k / both / a batch of all four:
+//     1 x 65536     16 34 22 27       18 31 25 31
+//     1 x 131072    22 55 29 34       19 36 25 30
+//     8 x 131072    25 56 32 36 55    22 38 29 34 37
+//     16 x 98304    20 45 27 32 45    21 37 28 33 37
+//     16 x 131072   25 56 32 37 56    22 40 31 36 39
+//     24 x 131072   26 57 32 37 56    27 50 39 44 48
+//     48 x 131072   25 57 33 38 56    33 63 52 57 61
 namespace {
 
 struct SplitBuffers {
