@@ -138,3 +138,30 @@ def test_teacher_that_names_only_nan(lrc, V):
             assert x[[0, 3]].isfinite().all() and x[1].isnan() and x[2].isnan()
         for x in (grad, back):
             assert x[[0, 3]].isfinite().all() and x[1, 1:4].isnan().all() and x[2, 1:4].isnan().all()
+
+
+@pytest.mark.parametrize("prec", ["fp32", "fp16", "bf16"])
+@pytest.mark.parametrize("rows,V,K,T", [(9, 1000, 1, 4.0), (7, 30001, 4, 4.0), (5, 131072, 4, 4.0), (3, 131072, 200, 4.0),
+                                        (3, 300007, 3, 2.0), (6, 5000, 64, 1.0)])
+def test_loss_of_little_named_mass(lrc, prec, rows, V, K, T):
+    """Where the rest of both distributions is nearly all of them, the loss is what its terms leave: sum p log(p / q) and
+    r log(r / Q) cancel to the square of their size.  Named tokens lie within 8 / log2(e) of the maximum here, so their q is
+    right to 5e-7 and p, the logarithms to a few 2^-24: an error of 2e-6 (sum p (1 + |log p / q|) + sum q), whatever the
+    sum over the row, whose error the two terms share."""
+    rng = np.random.default_rng(V + K)
+    teacher = rng.normal(size=(rows, V))
+    z = torch.from_numpy(teacher + 0.5 * rng.normal(size=(rows, V))).to(DT[prec]).cuda()
+    ids = np.argsort(-teacher, 1)[:, :K].copy()
+    top = torch.from_numpy(np.take_along_axis(teacher, ids, 1)).float().cuda()
+    lse = torch.from_numpy(np.log(np.exp(teacher / T).sum(1)).astype(np.float32)).cuda()
+    ids = torch.from_numpy(ids).cuda()
+    L, _ = H.distill(up(z), ids.cpu().numpy(), up(top), T, up(lse))
+    x = up(z) / T
+    q = np.take_along_axis(np.exp(x - x.max(1, keepdims=True)), ids.cpu().numpy(), 1)
+    q /= np.exp(x - x.max(1, keepdims=True)).sum(1, keepdims=True)
+    p = np.exp(up(top) / T - up(lse)[:, None])
+    tol = 2e-6 * T * T * ((p * (1 + abs(np.log(p / q)))).sum(1) + q.sum(1)) + 2.0 ** -24 * abs(L)
+    loss, _ = lrc.distill(z, ids, top, temperature=T, teacher_lse=lse)
+    floss, _ = lrc.distill_forward(z, ids, top, temperature=T, teacher_lse=lse)
+    for l in (loss, floss):
+        assert (abs(up(l) - L) <= tol).all(), float((abs(up(l) - L) / tol).max())
