@@ -83,3 +83,33 @@ def test_large_activations_stay_finite(lrc, prec, group, b):
     Y = lrc.q4_apply(codes, scales, torch.full((b, n), x, dtype=DT[prec], device="cuda"), group, out_dtype=torch.float32)
     want = n * 6 * 2.0 ** -14 * x
     assert ((Y.double() / want - 1).abs() <= (n + n / group + 8) * 2.0 ** -24).all()
+
+
+@pytest.mark.parametrize("prec", ["fp16", "bf16", "fp32"])
+@pytest.mark.parametrize("b", [1, 8, 20, 300])
+def test_small_activations_and_factors_keep_their_bits(lrc, prec, b):
+    """Subnormal binary16 activations and factors, and small bfloat16 and binary32 activations: products are exact,
+    so errors stay those of the sums.  Sums of one sign: relative errors of (n + n / group + 8) 2^-24 from the weights,
+    (n + k + 8) 2^-24 from the compensation."""
+    rng = np.random.default_rng(b)
+    m, n, k, u = 70, 390, 18, 2.0 ** -24
+    low = {"fp16": 2.0 ** -24, "bf16": 2.0 ** -100, "fp32": 2.0 ** -90}[prec]
+    codes = rng.integers(1, 8, (m, n))
+    packed = torch.from_numpy(H.pack(codes)).cuda()
+    X = torch.from_numpy(low * rng.integers(1, 200, (b, n))).to(DT[prec]).cuda()
+    x = X.double().cpu().numpy()
+    for sprec in ("fp16", "fp32"):
+        scales = torch.from_numpy(2.0 ** -24 * rng.integers(1, 900, (m, -(-n // 32)))).to(DT[sprec])
+        W = H.weights(codes, scales.double().numpy(), 32)
+        Y = lrc.q4_apply(packed, (scales * 2 ** 10).cuda(), X, 32, out_dtype=torch.float32)
+        want = (x @ W.T) * 2.0 ** 10
+        assert (abs(Y.double().cpu().numpy() - want) <= (n + n / 32 + 8) * u * want + 2.0 ** -149).all()
+    zero = torch.zeros(m, -(-n // 32), dtype=torch.float32, device="cuda")
+    for fprec in ("fp16", "bf16", "fp32"):
+        small = 2.0 ** -24 if fprec == "fp16" else 2.0 ** -30
+        U, V = (torch.from_numpy(small * rng.integers(1, 250, s)).to(DT[fprec]) for s in ((m, k), (n, k)))
+        s = torch.full((k,), 2.0 ** 15, dtype=DT[fprec])
+        Y = lrc.q4_apply(packed, zero, X, 32, (U.cuda(), s.cuda(), V.cuda()), out_dtype=torch.float32)
+        want = ((x @ V.double().numpy()) * s.double().numpy()) @ U.double().numpy().T
+        tiny = 2.0 ** -126 * k                           # results below binary32's normal range are not held to it
+        assert (abs(Y.double().cpu().numpy() - want) <= (2 * n + 2 * k + 16) * u * want + tiny).all(), (fprec, sprec)
