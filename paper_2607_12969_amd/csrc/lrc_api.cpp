@@ -860,9 +860,13 @@ int lrc_certify(const lrc_cert_args* args, lrc_cert_result* res) {
 namespace {
 
 // The entry points below let no exception out (allocation of host memory).
-#define LRC_NO_EXCEPTION \
-    catch (...) {        \
-        return LRC_ENOMEM; \
+int fail_exception() noexcept {
+    g_err.assign("out of memory");          // short enough to be stored without an allocation
+    return LRC_ENOMEM;
+}
+#define LRC_NO_EXCEPTION         \
+    catch (...) {                \
+        return fail_exception(); \
     }
 
 bool head_prec(int p) { return p == LRC_FP32 || p == LRC_FP16 || p == LRC_BF16; }
