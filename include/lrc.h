@@ -58,7 +58,10 @@ extern "C" {
 #define LRC_FP64 0
 #define LRC_FP32 1
 #define LRC_FP16 2
-#define LRC_BF16 3          /* output-head calls only (lrc_q4_*, lrc_sample, lrc_distill*) */
+#define LRC_BF16 3          /* output-head and step calls only (lrc_q4_*, lrc_sample, lrc_distill*, lrc_rms_norm*,
+                             * lrc_adapter_*, lrc_verify) */
+#define LRC_E4M3 4          /* 8 bits (sign, 4 exponent bits, 3 of significand; largest 448, no infinity): y of
+                             * lrc_rms_norm, X of lrc_q4_apply_e4m3 */
 
 /* return codes */
 #define LRC_OK 0
@@ -567,6 +570,144 @@ int lrc_distill(const void* logits, int64_t ld, int64_t rows, int64_t vocab, int
 int lrc_distill_backward(const void* logits, int64_t ld, int64_t rows, int64_t vocab, int prec, const int64_t* ids,
                          const void* top, int64_t K, int tprec, const float* teacher_lse, const float* weight,
                          double temperature, const float* stats, const float* dloss, void* grad, int64_t ldg);
+
+/* ---- Around the compressed projections of a step: the norm in front of them,
+ * low-rank adapters beside them, the check of drafted tokens behind them.  Pitches
+ * and zero rows as in the output-head calls; types LRC_FP32, LRC_FP16 and LRC_BF16. */
+
+/*
+ * lrc_q4_apply_e4m3 -- lrc_q4_apply of 8-bit activations
+ *   X       device, batch rows of n e4m3 values, pitch ldx
+ *   xscale  device, batch factors (binary32): row b of Y is
+ *           xscale_b (X_b W^T + [(X_b V) diag(s)] U^T)
+ * The rest as lrc_q4_apply.  Products of codes and activations are exact; the
+ * row's factor enters last, in binary32.  An e4m3 NaN makes its row NaN.
+ */
+int lrc_q4_apply_e4m3(const void* codes, const void* scales, int sprec, int64_t group, const void* U, const void* s,
+                      const void* V, int64_t k, int fprec, const void* X, int64_t ldx, const float* xscale, void* Y,
+                      int64_t ldy, int64_t m, int64_t n, int64_t batch, int yprec);
+
+/*
+ * lrc_rms_norm -- root-mean-square norm of rows, after the residual's addition
+ *   h = x + residual (rounded once to prec), y = h (mean h^2 + eps)^(-1/2) weight
+ *   x, residual   device, rows x n (pitches ldx, ldr) in `prec`; residual may be
+ *           NULL: h = x
+ *   weight  device, n values in `wprec`, or NULL (1)
+ *   sum     device, rows x n (pitch lds) in `prec`, or NULL: h; may be `residual` or
+ *           `x` itself (equal pitch).  Not written without residual
+ *   y       device, rows x n (pitch ldy) in `yprec`: prec, or LRC_E4M3
+ *   scales  device, rows, for LRC_E4M3: t = max |y| / 448 of the row, and y holds the
+ *           e4m3 values nearest to y / t (ties to even; 0 where t is 0).  A row with a
+ *           NaN or an infinity among its y gets the scale NaN and codes NaN
+ *   rstd    device, rows, or NULL: (mean h^2 + eps)^(-1/2), for the gradient
+ * Sums are in binary32: squares pass its range for |h| above 1.8e19, and such rows give 0.
+ * With eps = 0 a row of zeros gives NaN.
+ * Errors: LRC_EINVAL for NULL pointers, rows < 0, n < 1, pitches below n, eps not
+ * a finite number >= 0, unknown precisions (yprec other than prec or LRC_E4M3,
+ * scales given or missing against it) or an output that overlaps an input (other than
+ * sum as above) or another output; LRC_EOVERFLOW, LRC_EHIP, LRC_ENODEV as elsewhere.
+ */
+int lrc_rms_norm(const void* x, int64_t ldx, const void* residual, int64_t ldr, int64_t rows, int64_t n, int prec,
+                 const void* weight, int wprec, double eps, void* sum, int64_t lds, void* y, int64_t ldy, int yprec,
+                 float* scales, float* rstd);
+
+/*
+ * lrc_rms_norm_backward -- gradient of lrc_rms_norm (y in prec)
+ *   dy, h   device, rows x n (pitches lddy, ldh) in `prec`: the gradient of y, and the
+ *           h that the norm was taken of
+ *   rstd    device, rows, as lrc_rms_norm wrote it
+ *   dsum    device, rows x n (pitch ldd) in `prec`, or NULL: gradient that reaches h
+ *           by other ways, added to dx
+ *   dx      device, rows x n (pitch ldx) in `prec`: gradient of h, that is of x and of the
+ *           residual; may be dy or dsum itself (equal pitch)
+ *   dweight device, n values in `wprec`, or NULL
+ * Sums in binary32, in a fixed order: bitwise reproducible.
+ * Errors: as lrc_rms_norm, and LRC_ENOMEM.
+ */
+int lrc_rms_norm_backward(const void* dy, int64_t lddy, const void* h, int64_t ldh, const float* rstd, int64_t rows,
+                          int64_t n, int prec, const void* weight, int wprec, const void* dsum, int64_t ldd, void* dx,
+                          int64_t ldx, void* dweight);
+
+/*
+ * lrc_adapter_apply -- low-rank adapters of many requests beside a shared projection
+ *   Y_i = base_i + scale_a (X_i A_a^T) B_a^T,  a = ids_i
+ *   X       device, rows x n (pitch ldx) in `prec`
+ *   A, B    device, count x k x n and count x m x k in `prec`, without pitch; an
+ *           adapter of smaller rank is filled up with zeros
+ *   ids     device, rows: the adapter of each row; one outside [0, count): none, Y_i =
+ *           base_i
+ *   scale   device, count factors (binary32), or NULL (1)
+ *   base    device, rows x m (pitch ldb) in `prec`, or NULL (0): what the shared
+ *           projection gave; may be Y itself (equal pitch)
+ *   Y       device, rows x m (pitch ldy) in `prec`, rounded once
+ *   hidden  device, rows x k binary32 without pitch, or NULL: X_i A_a^T (0 without an
+ *           adapter), for the gradient
+ * Sums are in binary32; X_i A_a^T enters the second product with at least 16 bits
+ * (24 in LRC_FP32).  Sums are split in a fixed order: bitwise reproducible.
+ * Errors: LRC_EINVAL for NULL pointers, rows < 0, m, n or count < 1, k outside
+ * [1, LRC_ADAPTER_MAX_RANK], pitches below the rows, unknown precisions or an output
+ * that overlaps an input (other than base = Y) or another output; LRC_EOVERFLOW as
+ * elsewhere and for rows above 2^28 or count, m or n above 2^30; LRC_ENOMEM, LRC_EHIP,
+ * LRC_ENODEV as elsewhere.
+ */
+#define LRC_ADAPTER_MAX_RANK 256
+int lrc_adapter_apply(const void* X, int64_t ldx, const void* A, const void* B, const int64_t* ids, const float* scale,
+                      int64_t rows, int64_t m, int64_t n, int64_t k, int64_t count, int prec, const void* base,
+                      int64_t ldb, void* Y, int64_t ldy, float* hidden);
+
+/*
+ * lrc_adapter_backward -- gradient of lrc_adapter_apply
+ *   dH_i = scale_a dY_i B_a,  dX_i = base_i + dH_i A_a,  dA_a = sum dH_i^T X_i,
+ *   dB_a = scale_a sum dY_i^T hidden_i  over the rows i of adapter a
+ *   dY      device, rows x m (pitch lddy) in `prec`
+ *   hidden  device, as lrc_adapter_apply wrote it
+ *   base    device, rows x n (pitch ldb) in `prec`, or NULL (0): the shared projection's
+ *           part of dX; may be dX itself (equal pitch)
+ *   dX      device, rows x n (pitch lddx) in `prec`, or NULL
+ *   dA, dB  device, as A and B, or NULL; 0 for an adapter without rows
+ * (base's own gradient is dY.)  Sums and errors as lrc_adapter_apply; hidden and X
+ * may be NULL where neither dA nor dB needs them (dB needs hidden, dA needs X).
+ */
+int lrc_adapter_backward(const void* dY, int64_t lddy, const void* X, int64_t ldx, const void* A, const void* B,
+                         const int64_t* ids, const float* scale, const float* hidden, int64_t rows, int64_t m, int64_t n,
+                         int64_t k, int64_t count, int prec, const void* base, int64_t ldb, void* dX, int64_t lddx,
+                         void* dA, void* dB);
+
+/*
+ * lrc_verify -- drafted tokens checked against the target's logits
+ *   logits  device, requests x (drafts + 1) rows of vocab, pitch ld of a row and lr of
+ *           a request, in `prec`: row j holds the target's logits behind the first j drafts.
+ *           A pitch of 0 takes the same row, or the same request's rows, for all
+ *   draft   device, requests x drafts token indices; one outside [0, vocab) ends its
+ *           request's drafts
+ *   draft_logits  device, requests x drafts rows (pitches ldq, lrq) in `prec`: what the
+ *           drafts were drawn from, by lrc_sample under the same parameters; or NULL:
+ *           every draft was certain
+ *   u       device, requests x (drafts + 1) uniform numbers in [0, 1): one to accept each
+ *           draft, the last to draw a token (others are moved to the nearer end, NaN to 0)
+ *   temperature, top_k, top_p, min_p   device, one value per request, or NULL, as in
+ *           lrc_sample
+ *   tokens  device, requests x (drafts + 1): the accepted drafts, one drawn token, then -1
+ *   accepted  device, requests, or NULL: how many drafts were accepted
+ * With W the whole-number weights that lrc_sample gives the tokens it keeps (2^31 for
+ * the one token of a temperature that is not above 0) and S their sum, p of the target
+ * and q of the draft: draft t is accepted if (u Wq(t)) Sp < Wp(t) Sq, each product rounded
+ * once to binary64.  At the first draft that is not, the token is drawn from
+ * max(P - Q, 0), P = floor(Wp (2^52 / Sp)), Q = floor(Wq (2^52 / Sq)), or from Wp where that
+ * is 0 throughout; behind the last accepted draft from Wp, as lrc_sample does.  So the
+ * tokens follow the target's distribution.  A row whose logits are all -infinity accepts
+ * nothing and gives -1.  Sums are of whole numbers: the result does not depend on
+ * how the work is split.  Rows behind a request's last draft are not read.
+ * Errors: LRC_EINVAL for NULL logits, draft (with drafts > 0), u or tokens, requests or
+ * drafts < 0, drafts above LRC_VERIFY_MAX_DRAFTS, vocab < 1 or >= 2^31, pitches other
+ * than 0 below vocab, an unknown precision or an output that overlaps an input or another output;
+ * LRC_EOVERFLOW, LRC_ENOMEM, LRC_EHIP, LRC_ENODEV as elsewhere.
+ */
+#define LRC_VERIFY_MAX_DRAFTS 65536
+int lrc_verify(const void* logits, int64_t ld, int64_t lr, const void* draft_logits, int64_t ldq, int64_t lrq,
+               int64_t requests, int64_t drafts, int64_t vocab, int prec, const int64_t* draft, const float* u,
+               const float* temperature, const int64_t* top_k, const float* top_p, const float* min_p, int64_t* tokens,
+               int64_t* accepted);
 
 /* Stored bytes of rank-k factors in `prec`: (b/8) k (m+n+1)  (Sec. 4.2).
  * Returns LRC_EINVAL for bad arguments or LRC_EOVERFLOW on overflow. */

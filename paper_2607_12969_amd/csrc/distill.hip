@@ -33,41 +33,6 @@ constexpr float kNegInf = -__builtin_inff();
 
 enum { FORWARD = 0, BOTH = 1, BACKWARD = 2 };
 
-__device__ __forceinline__ float wave_max(float x) {
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) x = __builtin_fmaxf(x, __shfl_xor(x, off, 64));
-    return x;
-}
-// Over the workgroup's NT / 64 waves, in a fixed order; one barrier, so each use
-// has a `red` of its own.
-template <int NT> __device__ __forceinline__ float block_add(float x, float* red) {
-    x = wave_sum(x);
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
-    __syncthreads();
-    float t = 0.0f;
-#pragma unroll
-    for (int w = 0; w < NT / 64; ++w) t += red[w];
-    return t;
-}
-template <int NT> __device__ __forceinline__ float block_max(float x, float* red) {
-    x = wave_max(x);
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
-    __syncthreads();
-    float t = kNegInf;
-#pragma unroll
-    for (int w = 0; w < NT / 64; ++w) t = __builtin_fmaxf(t, red[w]);
-    return t;
-}
-
-// Keeps the packed form in the registers: without it the widened values of one
-// pass over the row are kept for the next (210 against 114 registers).
-template <int N> __device__ __forceinline__ void stay(uint4v_t (&v)[N]) {
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) asm volatile("" : "+v"(v[i][q]));
-}
-
 // log x, to a few 2^-26: the logarithm of the significand alone is binary32 (one of x
 // would carry half an ulp of its size, 2.4e-7 for sums of a few hundred).
 __device__ __forceinline__ double log_of(double x) {

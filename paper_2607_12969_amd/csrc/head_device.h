@@ -1,6 +1,7 @@
-// Storage types of the output-head kernels (4-bit product, sampling,
-// distillation): loads and stores of binary32, binary16 and bfloat16 values
-// as binary32, one at a time or eight (16 or 32 bytes) at a time.
+// Storage types of the output-head kernels (4-bit product, sampling, distillation,
+// norm, adapters, verification): loads and stores of binary32, binary16 and bfloat16
+// values as binary32, one at a time or eight (16 or 32 bytes) at a time, and sums and
+// maxima over a workgroup.
 #pragma once
 
 #include "lrc_device.h"
@@ -105,6 +106,41 @@ template <typename T> __device__ __forceinline__ uint4v_t pack16(const float (&g
         else v[q] = pack2<T>(g[2 * q], g[2 * q + 1]);
     }
     return v;
+}
+
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) x = __builtin_fmaxf(x, __shfl_xor(x, off, 64));
+    return x;
+}
+// Over the workgroup's NT / 64 waves, in a fixed order; one barrier, so each use
+// has a `red` of its own.
+template <int NT> __device__ __forceinline__ float block_add(float x, float* red) {
+    x = wave_sum(x);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
+    __syncthreads();
+    float t = 0.0f;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) t += red[w];
+    return t;
+}
+template <int NT> __device__ __forceinline__ float block_max(float x, float* red) {
+    x = wave_max(x);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
+    __syncthreads();
+    float t = -__builtin_inff();
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) t = __builtin_fmaxf(t, red[w]);
+    return t;
+}
+
+// Keeps the packed form in the registers: without it the widened values of one
+// pass over the row are kept for the next (210 against 114 registers).
+template <int N> __device__ __forceinline__ void stay(uint4v_t (&v)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) asm volatile("" : "+v"(v[i][q]));
 }
 
 }  // namespace lrc

@@ -974,20 +974,21 @@ int lrc_q4_quantize(const void* W, int64_t ldw, int64_t m, int64_t n, int64_t gr
     return LRC_OK;
 } LRC_NO_EXCEPTION
 
-int lrc_q4_apply(const void* codes, const void* scales, int sprec, int64_t group, const void* U, const void* s,
-                 const void* V, int64_t k, int fprec, const void* X, int64_t ldx, void* Y, int64_t ldy, int64_t m,
-                 int64_t n, int64_t batch, int prec, int yprec) try {
+// xscale: with prec = PE4M3, else NULL.
+static int q4_apply(const void* codes, const void* scales, int sprec, int64_t group, const void* U, const void* s,
+                    const void* V, int64_t k, int fprec, const void* X, int64_t ldx, const float* xscale, void* Y,
+                    int64_t ldy, int64_t m, int64_t n, int64_t batch, int prec, int yprec) {
     size_t cb, sb, xb, yb;
     int rc = check_q4(m, n, group, sprec, &cb, &sb);
     if (rc) return rc;
-    if (!head_prec(prec) || !head_prec(yprec))
-        return fail(LRC_EINVAL, "unknown precision code %d", head_prec(prec) ? yprec : prec);
+    const bool e4m3 = xscale != nullptr || prec == PE4M3, xprec = e4m3 || head_prec(prec);
+    if (!xprec || !head_prec(yprec)) return fail(LRC_EINVAL, "unknown precision code %d", xprec ? yprec : prec);
     if (batch < 0 || k < 0) return fail(LRC_EINVAL, "batch = %lld or k = %lld < 0", (long long)batch, (long long)k);
     if (k > std::min(m, n)) return fail(LRC_EINVAL, "k = %lld exceeds min(m, n)", (long long)k);
     if (k > 0 && !head_prec(fprec)) return fail(LRC_EINVAL, "unknown precision code %d of the factors", fprec);
     if (ldx < n || ldy < m) return fail(LRC_EINVAL, "pitches %lld, %lld below n = %lld, m = %lld", (long long)ldx,
                                         (long long)ldy, (long long)n, (long long)m);
-    if (!codes || !scales || (k > 0 && (!U || !s || !V)) || (batch > 0 && (!X || !Y)))
+    if (!codes || !scales || (k > 0 && (!U || !s || !V)) || (batch > 0 && (!X || !Y || (e4m3 && !xscale))))
         return fail(LRC_EINVAL, "NULL array argument");
     if (reinterpret_cast<uintptr_t>(codes) % 16) return fail(LRC_EINVAL, "codes must be 16-byte aligned");
     int64_t t, fe = k > 0 ? elem_bytes(fprec) : 0, need;
@@ -998,7 +999,8 @@ int lrc_q4_apply(const void* codes, const void* scales, int sprec, int64_t group
         return fail(LRC_EOVERFLOW, "array sizes overflow int64");
     if ((rc = check_out({Y, yb, "Y"}, {{codes, cb, "codes"}, {scales, sb, "scales"}, {X, xb, "X"},
                                        {k ? U : nullptr, (size_t)(m * k * fe), "U"}, {k ? s : nullptr, (size_t)(k * fe), "s"},
-                                       {k ? V : nullptr, (size_t)(n * k * fe), "V"}})))
+                                       {k ? V : nullptr, (size_t)(n * k * fe), "V"},
+                                       {xscale, (size_t)batch * 4, "xscale"}})))
         return rc;
     if (batch == 0) return LRC_OK;
     int dev;
@@ -1011,8 +1013,21 @@ int lrc_q4_apply(const void* codes, const void* scales, int sprec, int64_t group
     const size_t bytes = q4_apply_workspace_bytes(w, X, ldx, batch, prec);
     hipError_t e = bytes ? ws.reserve(bytes, st) : hipSuccess;
     if (e != hipSuccess) return fail_hip(e, "workspace");
-    e = launch_q4_apply(w, X, ldx, Y, ldy, batch, prec, yprec, ws, st);
+    e = launch_q4_apply(w, X, ldx, xscale, Y, ldy, batch, prec, yprec, ws, st);
     return e == hipSuccess ? LRC_OK : fail_hip(e, "4-bit apply launch");
+}
+
+int lrc_q4_apply(const void* codes, const void* scales, int sprec, int64_t group, const void* U, const void* s,
+                 const void* V, int64_t k, int fprec, const void* X, int64_t ldx, void* Y, int64_t ldy, int64_t m,
+                 int64_t n, int64_t batch, int prec, int yprec) try {
+    if (prec == PE4M3) return fail(LRC_EINVAL, "unknown precision code %d", prec);      // lrc_q4_apply_e4m3
+    return q4_apply(codes, scales, sprec, group, U, s, V, k, fprec, X, ldx, nullptr, Y, ldy, m, n, batch, prec, yprec);
+} LRC_NO_EXCEPTION
+
+int lrc_q4_apply_e4m3(const void* codes, const void* scales, int sprec, int64_t group, const void* U, const void* s,
+                      const void* V, int64_t k, int fprec, const void* X, int64_t ldx, const float* xscale, void* Y,
+                      int64_t ldy, int64_t m, int64_t n, int64_t batch, int yprec) try {
+    return q4_apply(codes, scales, sprec, group, U, s, V, k, fprec, X, ldx, xscale, Y, ldy, m, n, batch, PE4M3, yprec);
 } LRC_NO_EXCEPTION
 
 int lrc_sample(const void* logits, int64_t ld, int64_t rows, int64_t vocab, int prec, const float* u,
@@ -1116,6 +1131,217 @@ int lrc_distill_backward(const void* logits, int64_t ld, int64_t rows, int64_t v
     const DistillArgs a{logits, rows, vocab, ld, prec, ids, top, K, tprec, teacher_lse, weight, (float)temperature};
     hipError_t e = launch_distill_backward(a, stats, dloss, grad, ldg, g_stream);
     return e == hipSuccess ? LRC_OK : fail_hip(e, "distillation gradient launch");
+} LRC_NO_EXCEPTION
+
+// ---- around the projections
+// Workspace of a call, reserved; its launch follows.
+static int reserve(size_t bytes, Workspace** out) {
+    int dev;
+    const int rc = current_device(&dev, nullptr);
+    if (rc) return rc;
+    Workspace& ws = workspace_for(dev, g_stream);
+    ws.reset();
+    const hipError_t e = bytes ? ws.reserve(bytes, g_stream) : hipSuccess;
+    if (e != hipSuccess) return fail_hip(e, "workspace");
+    *out = &ws;
+    return LRC_OK;
+}
+
+static int check_norm(int64_t rows, int64_t n, int prec, bool weight, int wprec) {
+    if (rows < 0) return fail(LRC_EINVAL, "rows = %lld < 0", (long long)rows);
+    if (n < 1) return fail(LRC_EINVAL, "n = %lld < 1", (long long)n);
+    if (!head_prec(prec)) return fail(LRC_EINVAL, "unknown precision code %d", prec);
+    if (weight && !head_prec(wprec)) return fail(LRC_EINVAL, "unknown precision code %d of the weight", wprec);
+    return LRC_OK;
+}
+// Bytes of a rows x n array, 0 for a NULL one.
+static int check_pitch(const void* p, const char* name, int64_t rows, int64_t ld, int64_t n, int64_t e, size_t* bytes) {
+    *bytes = 0;
+    if (!p) return LRC_OK;
+    if (ld < n) return fail(LRC_EINVAL, "pitch %lld of %s below %lld", (long long)ld, name, (long long)n);
+    if (!span_bytes(rows, ld, n, e, bytes)) return fail(LRC_EOVERFLOW, "array sizes overflow int64");
+    return LRC_OK;
+}
+
+int lrc_rms_norm(const void* x, int64_t ldx, const void* residual, int64_t ldr, int64_t rows, int64_t n, int prec,
+                 const void* weight, int wprec, double eps, void* sum, int64_t lds, void* y, int64_t ldy, int yprec,
+                 float* scales, float* rstd) try {
+    int rc = check_norm(rows, n, prec, weight, wprec);
+    if (rc) return rc;
+    if (yprec != prec && yprec != LRC_E4M3) return fail(LRC_EINVAL, "unknown precision code %d of y", yprec);
+    if (!(eps >= 0 && eps <= 3.4028234663852886e38)) return fail(LRC_EINVAL, "eps = %g is not a finite number >= 0", eps);
+    if (rows > 0 && (!x || !y || (yprec == LRC_E4M3 && !scales))) return fail(LRC_EINVAL, "NULL array argument");
+    if (yprec != LRC_E4M3 && scales) return fail(LRC_EINVAL, "scales belong to y in e4m3");
+    const int e = elem_bytes(prec), ye = elem_bytes(yprec);
+    size_t xb, rb, sb, yb;
+    if (!residual) sum = nullptr;
+    if ((rc = check_pitch(x, "x", rows, ldx, n, e, &xb)) || (rc = check_pitch(residual, "residual", rows, ldr, n, e, &rb)) ||
+        (rc = check_pitch(sum, "sum", rows, lds, n, e, &sb)) || (rc = check_pitch(y, "y", rows, ldy, n, ye, &yb)))
+        return rc;
+    const Span in[3] = {{x, xb, "x"}, {residual, rb, "residual"}, {weight, (size_t)n * elem_bytes(wprec), "weight"}};
+    const Span s{sum, sb, "sum"}, o{y, yb, "y"}, t{scales, (size_t)rows * 4, "scales"}, d{rstd, (size_t)rows * 4, "rstd"};
+    const Span none{nullptr, 0, ""};
+    if ((rc = check_out(s, {sum == x && lds == ldx ? none : in[0], sum == residual && lds == ldr ? none : in[1], in[2]})) ||
+        (rc = check_out(o, {in[0], in[1], in[2], s})) || (rc = check_out(t, {in[0], in[1], in[2], s, o})) ||
+        (rc = check_out(d, {in[0], in[1], in[2], s, o, t})))
+        return rc;
+    if (rows == 0) return LRC_OK;
+    int dev;
+    if ((rc = current_device(&dev, nullptr))) return rc;
+    const NormArgs a{x, residual, ldx, ldr, rows, n, prec, weight, wprec, (float)eps, sum, lds, y, ldy, scales, rstd};
+    const hipError_t he = launch_rms_norm(a, g_stream);
+    return he == hipSuccess ? LRC_OK : fail_hip(he, "norm launch");
+} LRC_NO_EXCEPTION
+
+int lrc_rms_norm_backward(const void* dy, int64_t lddy, const void* h, int64_t ldh, const float* rstd, int64_t rows,
+                          int64_t n, int prec, const void* weight, int wprec, const void* dsum, int64_t ldd, void* dx,
+                          int64_t ldx, void* dweight) try {
+    int rc = check_norm(rows, n, prec, weight || dweight, wprec);
+    if (rc) return rc;
+    if (rows > 0 && (!dy || !h || !rstd || !dx)) return fail(LRC_EINVAL, "NULL array argument");
+    const int e = elem_bytes(prec);
+    size_t yb, hb, db, xb;
+    int64_t t;
+    if ((rc = check_pitch(dy, "dy", rows, lddy, n, e, &yb)) || (rc = check_pitch(h, "h", rows, ldh, n, e, &hb)) ||
+        (rc = check_pitch(dsum, "dsum", rows, ldd, n, e, &db)) || (rc = check_pitch(dx, "dx", rows, ldx, n, e, &xb)))
+        return rc;
+    if (!mul_ok(n, 4 * 4096, &t)) return fail(LRC_EOVERFLOW, "array sizes overflow int64");
+    const Span sy{dy, yb, "dy"}, sh{h, hb, "h"}, sr{rstd, (size_t)rows * 4, "rstd"}, sd{dsum, db, "dsum"}, sx{dx, xb, "dx"};
+    const Span sw{weight, (size_t)n * elem_bytes(wprec), "weight"}, gw{dweight, (size_t)n * elem_bytes(wprec), "dweight"};
+    const Span none{nullptr, 0, ""};
+    if ((rc = check_out(sx, {dx == dy && ldx == lddy ? none : sy, sh, sr, dx == dsum && ldx == ldd ? none : sd, sw})) ||
+        (rc = check_out(gw, {sy, sh, sr, sd, sw, sx})))
+        return rc;
+    if (rows == 0 && !dweight) return LRC_OK;
+    const NormGradArgs a{dy, h, dsum, lddy, ldh, ldd, rows, n, prec, rstd, weight, wprec, dx, ldx, dweight};
+    Workspace* ws;
+    if ((rc = reserve(norm_grad_workspace_bytes(a), &ws))) return rc;
+    const hipError_t he = launch_rms_norm_backward(a, *ws, g_stream);
+    return he == hipSuccess ? LRC_OK : fail_hip(he, "norm gradient launch");
+} LRC_NO_EXCEPTION
+
+static_assert(kAdapterMaxRank == LRC_ADAPTER_MAX_RANK, "rank limit of the adapters");
+
+// Sizes; bytes of one of A, B.
+static int check_adapter(int64_t rows, int64_t m, int64_t n, int64_t k, int64_t count, int prec, size_t* ab, size_t* bb) {
+    if (rows < 0) return fail(LRC_EINVAL, "rows = %lld < 0", (long long)rows);
+    if (m < 1 || n < 1 || count < 1)
+        return fail(LRC_EINVAL, "sizes must be >= 1 (m=%lld n=%lld count=%lld)", (long long)m, (long long)n, (long long)count);
+    if (k < 1 || k > LRC_ADAPTER_MAX_RANK)
+        return fail(LRC_EINVAL, "k = %lld outside [1, %d]", (long long)k, LRC_ADAPTER_MAX_RANK);
+    if (!head_prec(prec)) return fail(LRC_EINVAL, "unknown precision code %d", prec);
+    const int64_t most = (int64_t)1 << 30;
+    if (rows > (int64_t)1 << 28 || m > most || n > most || count > most)
+        return fail(LRC_EOVERFLOW, "rows = %lld above 2^28, or m, n or count above 2^30", (long long)rows);
+    int64_t t;
+    if (!mul_ok(count * k, std::max(m, n), &t) || !mul_ok(t, 8, &t) || !mul_ok(rows + 1, std::max(m, n), &t) || !mul_ok(t, 2048, &t))
+        return fail(LRC_EOVERFLOW, "array sizes overflow int64");
+    *ab = (size_t)(count * k * n) * elem_bytes(prec);
+    *bb = (size_t)(count * k * m) * elem_bytes(prec);
+    return LRC_OK;
+}
+
+int lrc_adapter_apply(const void* X, int64_t ldx, const void* A, const void* B, const int64_t* ids, const float* scale,
+                      int64_t rows, int64_t m, int64_t n, int64_t k, int64_t count, int prec, const void* base,
+                      int64_t ldb, void* Y, int64_t ldy, float* hidden) try {
+    size_t ab, bb, xb, sb, yb;
+    int rc = check_adapter(rows, m, n, k, count, prec, &ab, &bb);
+    if (rc) return rc;
+    if (rows > 0 && (!X || !A || !B || !ids || !Y)) return fail(LRC_EINVAL, "NULL array argument");
+    const int e = elem_bytes(prec);
+    if ((rc = check_pitch(X, "X", rows, ldx, n, e, &xb)) || (rc = check_pitch(base, "base", rows, ldb, m, e, &sb)) ||
+        (rc = check_pitch(Y, "Y", rows, ldy, m, e, &yb)))
+        return rc;
+    const Span sX{X, xb, "X"}, sA{A, ab, "A"}, sB{B, bb, "B"}, si{ids, (size_t)rows * 8, "ids"},
+        sc{scale, (size_t)count * 4, "scale"}, sb_{base, sb, "base"}, sY{Y, yb, "Y"}, sH{hidden, (size_t)(rows * k) * 4, "hidden"};
+    if ((rc = check_out(sY, {sX, sA, sB, si, sc, base == Y && ldb == ldy ? Span{nullptr, 0, ""} : sb_})) ||
+        (rc = check_out(sH, {sX, sA, sB, si, sc, sb_, sY})))
+        return rc;
+    if (rows == 0) return LRC_OK;
+    const AdapterArgs a{X, A, B, ids, scale, rows, m, n, k, count, ldx, prec, base, ldb, Y, ldy, hidden};
+    Workspace* ws;
+    if ((rc = reserve(adapter_workspace_bytes(a), &ws))) return rc;
+    const hipError_t he = launch_adapter(a, *ws, g_stream);
+    return he == hipSuccess ? LRC_OK : fail_hip(he, "adapter launch");
+} LRC_NO_EXCEPTION
+
+int lrc_adapter_backward(const void* dY, int64_t lddy, const void* X, int64_t ldx, const void* A, const void* B,
+                         const int64_t* ids, const float* scale, const float* hidden, int64_t rows, int64_t m, int64_t n,
+                         int64_t k, int64_t count, int prec, const void* base, int64_t ldb, void* dX, int64_t lddx,
+                         void* dA, void* dB) try {
+    size_t ab, bb, yb, xb, sb, db;
+    int rc = check_adapter(rows, m, n, k, count, prec, &ab, &bb);
+    if (rc) return rc;
+    if (rows > 0 && (!dY || !B || !ids || (dX && !A) || (dA && !X) || (dB && !hidden)))
+        return fail(LRC_EINVAL, "NULL array argument");
+    if (!dX) base = nullptr;
+    if (!dA) X = nullptr;
+    const int e = elem_bytes(prec);
+    if ((rc = check_pitch(dY, "dY", rows, lddy, m, e, &yb)) || (rc = check_pitch(X, "X", rows, ldx, n, e, &xb)) ||
+        (rc = check_pitch(base, "base", rows, ldb, n, e, &sb)) || (rc = check_pitch(dX, "dX", rows, lddx, n, e, &db)))
+        return rc;
+    const Span sY{dY, yb, "dY"}, sX{X, xb, "X"}, sA{A, ab, "A"}, sB{B, bb, "B"}, si{ids, (size_t)rows * 8, "ids"},
+        sc{scale, (size_t)count * 4, "scale"}, sb_{base, sb, "base"}, sH{hidden, (size_t)(rows * k) * 4, "hidden"};
+    const Span gX{dX, db, "dX"}, gA{dA, ab, "dA"}, gB{dB, bb, "dB"};
+    if ((rc = check_out(gX, {sY, sX, sA, sB, si, sc, sH, base == dX && ldb == lddx ? Span{nullptr, 0, ""} : sb_})) ||
+        (rc = check_out(gA, {sY, sX, sA, sB, si, sc, sH, sb_, gX})) ||
+        (rc = check_out(gB, {sY, sX, sA, sB, si, sc, sH, sb_, gX, gA})))
+        return rc;
+    if (rows == 0 && !dA && !dB) return LRC_OK;
+    if (!dX && !dA && !dB) return LRC_OK;
+    const AdapterGradArgs a{dY, X, A, B, ids, scale, hidden, rows, m, n, k, count, lddy, ldx, prec, base, ldb, dX, lddx, dA, dB};
+    Workspace* ws;
+    if ((rc = reserve(adapter_grad_workspace_bytes(a), &ws))) return rc;
+    const hipError_t he = launch_adapter_backward(a, *ws, g_stream);
+    return he == hipSuccess ? LRC_OK : fail_hip(he, "adapter gradient launch");
+} LRC_NO_EXCEPTION
+
+int lrc_verify(const void* logits, int64_t ld, int64_t lr, const void* draft_logits, int64_t ldq, int64_t lrq,
+               int64_t requests, int64_t drafts, int64_t vocab, int prec, const int64_t* draft, const float* u,
+               const float* temperature, const int64_t* top_k, const float* top_p, const float* min_p, int64_t* tokens,
+               int64_t* accepted) try {
+    if (requests < 0) return fail(LRC_EINVAL, "requests = %lld < 0", (long long)requests);
+    if (drafts < 0 || drafts > LRC_VERIFY_MAX_DRAFTS)
+        return fail(LRC_EINVAL, "drafts = %lld outside [0, %d]", (long long)drafts, LRC_VERIFY_MAX_DRAFTS);
+    if (drafts == 0) draft_logits = nullptr;
+    // pitches of 0: one row, or one request's rows, for all
+    int rc = check_logits(logits, ld ? ld : vocab, requests, vocab, prec);
+    if (!rc && draft_logits) rc = check_logits(draft_logits, ldq ? ldq : vocab, requests, vocab, prec);
+    if (rc) return rc;
+    if ((lr && lr < vocab) || (draft_logits && lrq && lrq < vocab))
+        return fail(LRC_EINVAL, "pitches %lld, %lld of requests below vocab = %lld", (long long)lr, (long long)lrq,
+                    (long long)vocab);
+    if (requests > 0 && (!u || !tokens || (drafts > 0 && !draft))) return fail(LRC_EINVAL, "NULL array argument");
+    // bytes from the first to past the last logit
+    auto span = [&](int64_t rows, int64_t row, int64_t request, size_t* out) {
+        int64_t a, b, c;
+        if (!mul_ok(rows, row, &a) || !mul_ok(requests, request, &b) || a > INT64_MAX / 2 || b > INT64_MAX / 2 ||
+            !mul_ok(a + b, 8, &c))
+            return false;
+        *out = requests < 1 || rows < 1
+                   ? 0 : (size_t)((requests - 1) * request + (rows - 1) * row + vocab) * elem_bytes(prec);
+        return true;
+    };
+    size_t pb, qb = 0;
+    int64_t rows;
+    if (!span(drafts + 1, ld, lr, &pb) || (draft_logits && !span(drafts, ldq, lrq, &qb)) ||
+        !mul_ok(requests, 2 * drafts + 1, &rows) || !mul_ok(rows, 64, &rows))
+        return fail(LRC_EOVERFLOW, "array sizes overflow int64");
+    const size_t fb = (size_t)requests * 4;
+    const std::initializer_list<Span> in = {{logits, pb, "logits"}, {draft_logits, qb, "draft_logits"},
+                                            {draft, (size_t)(requests * drafts) * 8, "draft"},
+                                            {u, (size_t)(requests * (drafts + 1)) * 4, "u"},
+                                            {temperature, fb, "temperature"}, {top_k, 2 * fb, "top_k"},
+                                            {top_p, fb, "top_p"}, {min_p, fb, "min_p"}};
+    const Span to{tokens, (size_t)(requests * (drafts + 1)) * 8, "tokens"}, ac{accepted, 2 * fb, "accepted"};
+    if ((rc = check_out(to, in)) || (rc = check_out(ac, in)) || (rc = check_out(ac, {to}))) return rc;
+    if (requests == 0) return LRC_OK;
+    const VerifyArgs a{logits, draft_logits, requests, drafts, vocab, ld, lr, ldq, lrq, prec, draft, u, temperature,
+                       top_p, min_p, top_k, tokens, accepted};
+    Workspace* ws;
+    if ((rc = reserve(verify_workspace_bytes(a), &ws))) return rc;
+    const hipError_t he = launch_verify(a, *ws, g_stream);
+    return he == hipSuccess ? LRC_OK : fail_hip(he, "verification launch");
 } LRC_NO_EXCEPTION
 
 }  // extern "C"

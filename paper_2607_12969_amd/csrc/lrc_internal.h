@@ -13,9 +13,9 @@
 
 namespace lrc {
 
-enum Prec { P64 = 0, P32 = 1, P16 = 2, PB16 = 3 };
+enum Prec { P64 = 0, P32 = 1, P16 = 2, PB16 = 3, PE4M3 = 4 };
 
-inline int elem_bytes(int prec) { return prec == P64 ? 8 : (prec == P32 ? 4 : 2); }
+inline int elem_bytes(int prec) { return prec == P64 ? 8 : prec == P32 ? 4 : prec == PE4M3 ? 1 : 2; }
 inline int mfma_kb(int prec) { return prec == P16 ? 32 : 4; }
 inline int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
@@ -238,9 +238,10 @@ struct Q4Weights {
 // values (prec, m x n with pitch n) and nbad (zeroed first) may be null
 hipError_t launch_q4_quantize(const void* W, int64_t ldw, int prec, int64_t m, int64_t n, int64_t group, void* codes,
                               void* scales, int sprec, void* values, unsigned long long* nbad, hipStream_t stream);
+// xscale: with prec = PE4M3 the factor of each row of X, else null.
 size_t q4_apply_workspace_bytes(const Q4Weights& w, const void* X, int64_t ldx, int64_t batch, int prec);
-hipError_t launch_q4_apply(const Q4Weights& w, const void* X, int64_t ldx, void* Y, int64_t ldy, int64_t batch,
-                           int prec, int yprec, Workspace& ws, hipStream_t stream);
+hipError_t launch_q4_apply(const Q4Weights& w, const void* X, int64_t ldx, const float* xscale, void* Y, int64_t ldy,
+                           int64_t batch, int prec, int yprec, Workspace& ws, hipStream_t stream);
 
 // Sampling: per-row parameters on the device, each may be null (off).
 struct SampleArgs {
@@ -270,6 +271,83 @@ hipError_t launch_distill(const DistillArgs& a, float* loss, float* stats, void*
                           hipStream_t stream);
 hipError_t launch_distill_backward(const DistillArgs& a, const float* stats, const float* dloss, void* grad,
                                    int64_t ldg, hipStream_t stream);
+
+// Verification of drafted tokens: logits requests x (drafts + 1) rows, pitch ld of a
+// row and lr of a request; draft_logits (pitches ldq, lrq), the per-request
+// parameters and accepted may be null.
+struct VerifyArgs {
+    const void *logits, *draft_logits;
+    int64_t requests, drafts, vocab, ld, lr, ldq, lrq;
+    int prec;
+    const int64_t* draft;
+    const float *u, *temperature, *top_p, *min_p;
+    const int64_t* top_k;
+    int64_t *tokens, *accepted;
+};
+size_t verify_workspace_bytes(const VerifyArgs& a);
+hipError_t launch_verify(const VerifyArgs& a, Workspace& ws, hipStream_t stream);
+
+// Adapters: scale, base, hidden (rows x k) may be null; base may be Y.
+constexpr int kAdapterMaxRank = 256;
+struct AdapterArgs {
+    const void *X, *A, *B;
+    const int64_t* ids;
+    const float* scale;
+    int64_t rows, m, n, k, count, ldx;
+    int prec;
+    const void* base;
+    int64_t ldb;
+    void* Y;
+    int64_t ldy;
+    float* hidden;
+};
+size_t adapter_workspace_bytes(const AdapterArgs& a);
+hipError_t launch_adapter(const AdapterArgs& a, Workspace& ws, hipStream_t stream);
+// Their gradient: base (added to dX; may be dX), dX, dA and dB may be null.
+struct AdapterGradArgs {
+    const void *dY, *X, *A, *B;
+    const int64_t* ids;
+    const float *scale, *hidden;
+    int64_t rows, m, n, k, count, lddy, ldx;
+    int prec;
+    const void* base;
+    int64_t ldb;
+    void* dX;
+    int64_t lddx;
+    void *dA, *dB;
+};
+size_t adapter_grad_workspace_bytes(const AdapterGradArgs& a);
+hipError_t launch_adapter_backward(const AdapterGradArgs& a, Workspace& ws, hipStream_t stream);
+
+// Norm of rows: residual, weight, sum, scales (given: y in e4m3) and rstd may be null.
+struct NormArgs {
+    const void *x, *residual;
+    int64_t ldx, ldr, rows, n;
+    int prec;
+    const void* weight;
+    int wprec;
+    float eps;
+    void* sum;
+    int64_t lds;
+    void* y;
+    int64_t ldy;
+    float *scales, *rstd;
+};
+hipError_t launch_rms_norm(const NormArgs& a, hipStream_t stream);
+// Its gradient: weight, dsum and dw (in wprec) may be null.
+struct NormGradArgs {
+    const void *dy, *h, *dsum;
+    int64_t lddy, ldh, ldd, rows, n;
+    int prec;
+    const float* rstd;
+    const void* weight;
+    int wprec;
+    void* dx;
+    int64_t ldx;
+    void* dw;
+};
+size_t norm_grad_workspace_bytes(const NormGradArgs& a);
+hipError_t launch_rms_norm_backward(const NormGradArgs& a, Workspace& ws, hipStream_t stream);
 
 // ------------------------------------------------------------------- TT ---
 constexpr int kMaxD = 16;

@@ -179,6 +179,7 @@ struct Q4Args {
     int fprec;
     const void* X;
     int64_t ldx, plane;   // k_q4_tile: 16-bit planes, `plane` elements apart
+    const float* xscale;  // factor of each row of Y (8-bit activations), or null
     void* Y;
     int64_t ldy;
     int yprec;
@@ -513,6 +514,7 @@ __global__ __launch_bounds__(64 * NW) void k_q4_rows(Q4Args a, int KC) {
             float y = red[t * RP + i];
 #pragma unroll
             for (int q = 1; q < NW; ++q) y += red[(q * 16 + t) * RP + i];
+            if (a.xscale) y *= a.xscale[t];
             store_from_f32(a.Y, t * a.ldy + i0 + i, a.yprec, y);
         }
     }
@@ -700,18 +702,20 @@ __global__ __launch_bounds__(64 * WX * WR, (TileCfg<T, WX, NX, WR>::EU)) void k_
                 const int64_t i = i0 + wr * 16 * NR + 16 * r + lr, b = b0 + wx * 16 * NX + 16 * f + 4 * lg + v;
                 if (i < a.m && b < a.b) {
                     if (a.part) a.part[(split * a.b + b) * a.m + i] = acc[r][f][v];
-                    else store_from_f32(a.Y, b * a.ldy + i, a.yprec, acc[r][f][v]);
+                    else store_from_f32(a.Y, b * a.ldy + i, a.yprec, a.xscale ? acc[r][f][v] * a.xscale[b] : acc[r][f][v]);
                 }
             }
 }
 
 // Y = the sum of the splits, in their order.
 __global__ __launch_bounds__(256) void k_q4_join(const float* __restrict__ part, int splits, int64_t m, int64_t b,
-                                                 void* __restrict__ Y, int64_t ldy, int yprec) {
+                                                 const float* __restrict__ xscale, void* __restrict__ Y, int64_t ldy,
+                                                 int yprec) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, t = blockIdx.y;
     if (i >= m) return;
     float y = 0.0f;
     for (int q = 0; q < splits; ++q) y += part[(q * b + t) * m + i];
+    if (xscale) y *= xscale[t];
     store_from_f32(Y, t * ldy + i, yprec, y);
 }
 
@@ -726,6 +730,35 @@ __global__ __launch_bounds__(256) void k_q4_pack(const T* __restrict__ X, int64_
 #pragma unroll
         for (int p = 0; p < ActTraits<T>::P; ++p)
             *reinterpret_cast<typename ActTraits<T>::frag*>(out + p * b * ldp + c * 8) = f[p];
+    }
+}
+
+// e4m3 activations as binary16, which holds them exactly, in rows of the same padding.
+__global__ __launch_bounds__(256) void k_q4_unpack8(const unsigned char* __restrict__ X, int64_t ldx, int64_t n, int64_t b,
+                                                    half_t* __restrict__ out, int64_t ldp) {
+    const int64_t per = ldp / 8, step = (int64_t)gridDim.x * 256;
+    for (int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x; c < b * per; c += step) {
+        const unsigned char* x = X + c / per * ldx;
+        const int64_t j = c % per * 8;
+        uint2v_t v = {0, 0};
+        if (j + 8 <= n) {
+            __builtin_memcpy(&v, x + j, 8);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (j + e < n) v[e >> 2] |= (unsigned)x[j + e] << (8 * (e & 3));
+        }
+        half8_t h;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const half2_t lo = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v[e], 1.0f, false);
+            const half2_t hi = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v[e], 1.0f, true);
+            h[4 * e] = lo[0];
+            h[4 * e + 1] = lo[1];
+            h[4 * e + 2] = hi[0];
+            h[4 * e + 3] = hi[1];
+        }
+        *reinterpret_cast<half8_t*>(out + c * 8) = h;
     }
 }
 
@@ -1033,7 +1066,8 @@ bool plan_rows(Q4Plan& p, const Q4Weights& w, int64_t b, int prec) {
     return true;
 }
 
-Q4Plan plan_q4(const Q4Weights& w, const void* X, int64_t ldx, int64_t b, int prec) {
+// unpacked: rows of X are zero from n to the next multiple of 128.
+Q4Plan plan_q4(const Q4Weights& w, const void* X, int64_t ldx, int64_t b, int prec, bool unpacked = false) {
     Q4Plan p{};
     const int64_t blocks = (w.n + 127) / 128;
     p.tile = !plan_rows(p, w, b, prec);
@@ -1046,7 +1080,7 @@ Q4Plan plan_q4(const Q4Weights& w, const void* X, int64_t ldx, int64_t b, int pr
         p.splits = (int)std::min<int64_t>(std::max<int64_t>(1, 512 / tiles), std::max<int64_t>(1, blocks / 4));
         const int e = elem_bytes(prec);
         p.ldp = blocks * 128;
-        p.pack = prec == P32 || w.n % 128 || reinterpret_cast<uintptr_t>(X) % 16 || ldx * e % 16;
+        p.pack = prec == P32 || (w.n % 128 && !unpacked) || reinterpret_cast<uintptr_t>(X) % 16 || ldx * e % 16;
         if (p.pack) p.planes = (size_t)(prec == P32 ? 3 : 1) * b * p.ldp * 2;
         if (p.splits > 1) p.part = (size_t)p.splits * b * w.m * 4;
     }
@@ -1140,7 +1174,7 @@ void mid_f(const Q4Plan& p, const Q4Weights& w, const Q4Args& a, float* part, hi
 
 template <typename T>
 hipError_t apply_t(const Q4Weights& w, Q4Args& a, int prec, Workspace& ws, hipStream_t st) {
-    const Q4Plan p = plan_q4(w, a.X, a.ldx, a.b, prec);
+    const Q4Plan p = plan_q4(w, a.X, a.ldx, a.b, prec, a.xscale != nullptr);
     float* Tm = static_cast<float*>(ws.take(p.tm));
     float* mid = static_cast<float*>(ws.take(p.mid_part));
     unsigned short* planes = static_cast<unsigned short*>(ws.take(p.planes));
@@ -1180,7 +1214,7 @@ hipError_t apply_t(const Q4Weights& w, Q4Args& a, int prec, Workspace& ws, hipSt
     if (p.splits > 1) {
         KernelTimer t("q4_join", st);
         hipLaunchKernelGGL(k_q4_join, dim3((unsigned)((w.m + 255) / 256), (unsigned)a.b), dim3(256), 0, st, a.part, p.splits,
-                           w.m, a.b, a.Y, a.ldy, a.yprec);
+                           w.m, a.b, a.xscale, a.Y, a.ldy, a.yprec);
     }
     return hipGetLastError();
 }
@@ -1193,12 +1227,19 @@ hipError_t apply_t(const Q4Weights& w, Q4Args& a, int prec, Workspace& ws, hipSt
 constexpr int64_t kQ4Panel = 1 << 20;
 int64_t weight_panel(int64_t batch) { return std::min<int64_t>(1 << 28, ((int64_t)1 << 36) / batch); }
 
+// 8-bit activations widened: rows of whole 128 columns, zero from n on.
+static int64_t unpacked_pitch(int64_t n) { return round_up(n, 128); }
+static size_t unpacked_bytes(int64_t n, int64_t b) { return (size_t)round_up(b * unpacked_pitch(n) * 2, 256); }
+
 size_t q4_apply_workspace_bytes(const Q4Weights& w, const void* X, int64_t ldx, int64_t batch, int prec) {
     size_t bytes = 0;
+    const bool e4m3 = prec == PE4M3;                       // as binary16 in rows of their own
     auto panel = [&](int64_t m, int64_t b) {
         Q4Weights part = w;
         part.m = m;
-        if (m && b) bytes = std::max(bytes, plan_bytes(plan_q4(part, X, ldx, b, prec)));
+        if (m && b)
+            bytes = std::max(bytes, e4m3 ? plan_bytes(plan_q4(part, nullptr, unpacked_pitch(w.n), b, P16, true)) + unpacked_bytes(w.n, b)
+                                         : plan_bytes(plan_q4(part, X, ldx, b, prec)));
     };
     const int64_t b = std::min(batch, kQ4Panel), m = std::min(w.m, weight_panel(b));
     for (int64_t rows : {b, batch % b}) {
@@ -1208,8 +1249,8 @@ size_t q4_apply_workspace_bytes(const Q4Weights& w, const void* X, int64_t ldx, 
     return bytes;
 }
 
-hipError_t launch_q4_apply(const Q4Weights& w, const void* X, int64_t ldx, void* Y, int64_t ldy, int64_t batch,
-                           int prec, int yprec, Workspace& ws, hipStream_t st) {
+hipError_t launch_q4_apply(const Q4Weights& w, const void* X, int64_t ldx, const float* xscale, void* Y, int64_t ldy,
+                           int64_t batch, int prec, int yprec, Workspace& ws, hipStream_t st) {
     const int64_t rb = q4_row_bytes(w.n), G = (w.n + w.group - 1) / w.group;
     auto panel = [&](int64_t i0, int64_t rows, int64_t b0, int64_t b) {
         Q4Weights part = w;
@@ -1228,6 +1269,7 @@ hipError_t launch_q4_apply(const Q4Weights& w, const void* X, int64_t ldx, void*
         a.fprec = w.fprec;
         a.X = static_cast<const char*>(X) + b0 * ldx * elem_bytes(prec);
         a.ldx = ldx;
+        a.xscale = xscale ? xscale + b0 : nullptr;
         a.Y = static_cast<char*>(Y) + (b0 * ldy + i0) * elem_bytes(yprec);
         a.ldy = ldy;
         a.yprec = yprec;
@@ -1235,6 +1277,19 @@ hipError_t launch_q4_apply(const Q4Weights& w, const void* X, int64_t ldx, void*
         a.n = w.n;
         a.b = b;
         ws.reset();
+        if (prec == PE4M3) {
+            half_t* x16 = static_cast<half_t*>(ws.take(unpacked_bytes(w.n, b)));
+            if (ws.overrun) return hipErrorOutOfMemory;
+            const int64_t ldp = unpacked_pitch(w.n);
+            {
+                KernelTimer t("q4_unpack8", st);
+                hipLaunchKernelGGL(k_q4_unpack8, dim3(strided_grid(b * (ldp / 8))), dim3(256), 0, st,
+                                   static_cast<const unsigned char*>(a.X), ldx, w.n, b, x16, ldp);
+            }
+            a.X = x16;
+            a.ldx = ldp;
+            return apply_t<half_t>(part, a, P16, ws, st);
+        }
         return prec == P32   ? apply_t<float>(part, a, prec, ws, st)
                : prec == P16 ? apply_t<half_t>(part, a, prec, ws, st)
                              : apply_t<bhalf_t>(part, a, prec, ws, st);

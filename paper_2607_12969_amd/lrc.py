@@ -10,9 +10,10 @@ Precision follows the tensors' dtype: float64 -> FP64, float32 -> FP32,
 float16 -> FP16 (FP32 accumulation); the output-head calls also take bfloat16.
 
 Every call returns plain tensors and records nothing for autograd, also for
-inputs that require a gradient.  Of the output-head calls the distillation
-loss has a gradient (distill, distill_backward: by the student's logits); the
-4-bit product has no backward call.
+inputs that require a gradient.  The distillation loss (distill,
+distill_backward: by the student's logits), the norm (rms_norm_backward) and
+the adapters (adapter_backward) have a gradient; the 4-bit product and the
+8-bit norm have no backward call.
 """
 from __future__ import annotations
 
@@ -26,7 +27,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("LRC_LIBRARY") or os.path.join(HERE, "liblrc.so")
 HEADER = os.path.join(os.path.dirname(HERE), "include", "lrc.h")
 
-FP64, FP32, FP16, BF16 = 0, 1, 2, 3
+FP64, FP32, FP16, BF16, E4M3 = 0, 1, 2, 3, 4
 PATH_AUTO, PATH_STREAM, PATH_MFMA = 0, 1, 2
 CERT_MATRIX, CERT_TT = 0, 1
 ERRORS = {-1: "EINVAL", -2: "EOVERFLOW", -3: "EHIP", -4: "ENOMEM", -5: "ENODEV", -6: "ENUMERIC"}
@@ -136,6 +137,24 @@ def lib():
     L.lrc_distill.restype = ctypes.c_int
     L.lrc_distill_backward.argtypes = distill + [_vp, _vp, _vp, _i64]
     L.lrc_distill_backward.restype = ctypes.c_int
+    L.lrc_q4_apply_e4m3.argtypes = [_vp, _vp, ctypes.c_int, _i64, _vp, _vp, _vp, _i64, ctypes.c_int, _vp, _i64, _vp, _vp,
+                                    _i64, _i64, _i64, _i64, ctypes.c_int]
+    L.lrc_q4_apply_e4m3.restype = ctypes.c_int
+    L.lrc_rms_norm.argtypes = [_vp, _i64, _vp, _i64, _i64, _i64, ctypes.c_int, _vp, ctypes.c_int, ctypes.c_double, _vp,
+                               _i64, _vp, _i64, ctypes.c_int, _vp, _vp]
+    L.lrc_rms_norm.restype = ctypes.c_int
+    L.lrc_rms_norm_backward.argtypes = [_vp, _i64, _vp, _i64, _vp, _i64, _i64, ctypes.c_int, _vp, ctypes.c_int, _vp, _i64,
+                                        _vp, _i64, _vp]
+    L.lrc_rms_norm_backward.restype = ctypes.c_int
+    L.lrc_adapter_apply.argtypes = [_vp, _i64, _vp, _vp, _vp, _vp, _i64, _i64, _i64, _i64, _i64, ctypes.c_int, _vp, _i64,
+                                    _vp, _i64, _vp]
+    L.lrc_adapter_apply.restype = ctypes.c_int
+    L.lrc_adapter_backward.argtypes = [_vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _i64, _i64, _i64, _i64, _i64,
+                                       ctypes.c_int, _vp, _i64, _vp, _i64, _vp, _vp]
+    L.lrc_adapter_backward.restype = ctypes.c_int
+    L.lrc_verify.argtypes = [_vp, _i64, _i64, _vp, _i64, _i64, _i64, _i64, _i64, ctypes.c_int, _vp, _vp, _vp, _vp, _vp, _vp,
+                             _vp, _vp]
+    L.lrc_verify.restype = ctypes.c_int
     L.lrc_storage_bytes.argtypes = [_i64, _i64, _i64, ctypes.c_int]
     L.lrc_storage_bytes.restype = _i64
     L.lrc_tt_storage_bytes.argtypes = [ctypes.POINTER(_i64), ctypes.POINTER(_i64), ctypes.c_int, ctypes.c_int]
@@ -576,12 +595,14 @@ def q4_quantize(W, group: int = 128, scale_dtype=None, values: bool = False, cou
     return out
 
 
-def q4_apply(codes, scales, X, group: int = 128, factors=None, out_dtype=None, Y=None):
+def q4_apply(codes, scales, X, group: int = 128, factors=None, out_dtype=None, Y=None, x_scales=None):
     """Y = X W^T + [(X V) diag(s)] U^T: X (batch x n, float32, float16 or
     bfloat16, contiguous rows), W the m x n weights of `codes` and `scales`
     (q4_quantize), factors = (U, s, V) a rank-k compensation (U m x k, s k,
     V n x k, one dtype) or None.  Y (batch x m) is in out_dtype (X's unless
-    given); a caller-supplied Y sets it."""
+    given); a caller-supplied Y sets it.  X may be float8_e4m3fn with
+    x_scales (float32, one factor per row, as rms_norm_e4m3 gives them): row b
+    of the whole is times x_scales[b], and out_dtype is bfloat16 unless given."""
     _need(X.dim() == 2 and codes.dim() == 2 and scales.dim() == 2, "X, codes and scales must be matrices")
     _need(group in (32, 64, 128, 256, 512), "group must be 32, 64, 128, 256 or 512")
     b, n = X.shape
@@ -591,8 +612,13 @@ def q4_apply(codes, scales, X, group: int = 128, factors=None, out_dtype=None, Y
     if codes.shape[1] != (n + 31) // 32 * 16 or scales.shape != (m, -(-n // group)):
         raise ValueError(f"shape mismatch: codes {tuple(codes.shape)} (want {(m, (n + 31) // 32 * 16)}), "
                          f"scales {tuple(scales.shape)} (want {(m, -(-n // group))})")
-    prec, sprec = _head_prec(X.dtype), _head_prec(scales.dtype)
+    e4m3 = X.dtype == _e4m3_dtype()
+    _need(e4m3 == (x_scales is not None), "x_scales belong to activations in float8_e4m3fn")
+    if e4m3 and out_dtype is None:
+        out_dtype = Y.dtype if Y is not None else _e4m3[1]
+    prec, sprec = None if e4m3 else _head_prec(X.dtype), _head_prec(scales.dtype)
     ldx = _rows(X, "X")
+    xs = _row_values(x_scales, "x_scales", b, _whole_dtypes()[2])
     k, fprec, ptrs = 0, 0, (None, None, None)
     dev = X.device
     if factors is not None:
@@ -617,6 +643,11 @@ def q4_apply(codes, scales, X, group: int = 128, factors=None, out_dtype=None, Y
     _on(dev, codes=codes, scales=scales, Y=Y)
     if Y is None:
         Y, ldy = _empty((b, m), out_dtype or X.dtype, dev), m
+    if e4m3:
+        _on(dev, x_scales=x_scales)
+        _launch(dev, "lrc_q4_apply_e4m3", codes.data_ptr(), scales.data_ptr(), sprec, group, *ptrs, k, fprec,
+                X.data_ptr(), ldx, xs, Y.data_ptr(), ldy, m, n, b, yprec)
+        return Y
     _bind_stream(dev)
     rc = lib().lrc_q4_apply(codes.data_ptr(), scales.data_ptr(), sprec, group, *ptrs, k, fprec, X.data_ptr(), ldx,
                             Y.data_ptr(), ldy, m, n, b, prec, yprec)
@@ -628,6 +659,40 @@ def q4_apply(codes, scales, X, group: int = 128, factors=None, out_dtype=None, Y
 def _empty(shape, dtype, device):
     import torch
     return torch.empty(shape, dtype=dtype, device=device)
+
+
+_e4m3 = None
+
+
+def _e4m3_dtype():
+    """float8_e4m3fn, looked up once (with bfloat16 beside it)."""
+    global _e4m3
+    if _e4m3 is None:
+        import torch
+        _e4m3 = (torch.float8_e4m3fn, torch.bfloat16)
+    return _e4m3[0]
+
+
+_current = None
+
+
+def _launch(dev, name, *args):
+    """One call on torch's current stream of the tensors' device, which need
+    not be the current one."""
+    global _current
+    if _current is None:
+        import torch
+        _current = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    if _current() == dev.index:
+        _bind_stream(dev)
+        rc = getattr(lib(), name)(*args)
+    else:
+        import torch
+        with torch.cuda.device(dev):
+            _bind_stream(dev)
+            rc = getattr(lib(), name)(*args)
+    if rc < 0:
+        _check(rc)
 
 
 _whole = None
@@ -755,6 +820,218 @@ def distill_backward(logits, ids, top_logits, stats, dloss=None, temperature: fl
     _bind_stream(logits.device)
     _check(lib().lrc_distill_backward(*args, stats.data_ptr(), up, g.data_ptr(), _rows(g, "grad")))
     return g
+
+
+# ---- around the compressed projections ----
+
+def _like(t, name, shape, dtype, dev):
+    """A caller's output, or a new one: (tensor, pitch)."""
+    if t is None:
+        return _empty(shape, dtype, dev), shape[1]
+    _need(tuple(t.shape) == tuple(shape) and t.dtype == dtype, f"{name} must be {tuple(shape)} of {dtype}")
+    _on(dev, **{name: t})
+    return t, _rows(t, name)
+
+
+def _norm_args(x, weight, residual, eps, sum_out):
+    _need(x.dim() == 2, "x must be a matrix")
+    rows, n = x.shape
+    prec = _head_prec(x.dtype)
+    ldx = _rows(x, "x")
+    dev = x.device
+    _on(dev, weight=weight, residual=residual)
+    wprec = 0
+    if weight is not None:
+        wprec = _head_prec(weight.dtype)
+        _need(weight.shape == (n,) and weight.is_contiguous(), f"weight must hold {n} contiguous values")
+    if residual is None:
+        _need(sum_out is None, "sum belongs to a residual")
+        return (x.data_ptr(), ldx, None, 0, rows, n, prec, weight.data_ptr() if weight is not None else None, wprec,
+                float(eps), None, 0), x, dev
+    _need(residual.shape == x.shape and residual.dtype == x.dtype, "residual must have x's shape and dtype")
+    h, ldh = _like(sum_out, "sum", (rows, n), x.dtype, dev)
+    return (x.data_ptr(), ldx, residual.data_ptr(), _rows(residual, "residual"), rows, n, prec,
+            weight.data_ptr() if weight is not None else None, wprec, float(eps), h.data_ptr(), ldh), h, dev
+
+
+def rms_norm(x, weight=None, residual=None, eps: float = 1e-6, stats: bool = False, out=None, sum=None):
+    """Root-mean-square norm of the rows of h = x + residual (rounded to x's
+    dtype; h = x without one): y = h (mean h^2 + eps)^(-1/2) weight.  x and
+    residual rows x n (float32, float16 or bfloat16, contiguous rows), weight
+    (n, any of the three) or None.  Returns (y, h), with stats=True also the
+    inverse roots (rows, float32) that rms_norm_backward takes.  h without a
+    residual is x itself; a caller-supplied `sum` receives it else, and may be
+    the residual or x."""
+    args, h, dev = _norm_args(x, weight, residual, eps, sum)
+    rows, n, prec = args[4], args[5], args[6]
+    y, ldy = _like(out, "out", (rows, n), x.dtype, dev)
+    rstd = _empty((rows,), _whole_dtypes()[2], dev) if stats else None
+    _launch(dev, "lrc_rms_norm", *args, y.data_ptr(), ldy, prec, None, rstd.data_ptr() if stats else None)
+    return (y, h, rstd) if stats else (y, h)
+
+
+def rms_norm_e4m3(x, weight=None, residual=None, eps: float = 1e-6, out=None, sum=None):
+    """rms_norm with y in 8 bits: returns (codes, scales, h), codes (rows x n,
+    float8_e4m3fn) the values nearest to y / scale and scales (rows, float32)
+    max |y| / 448 of each row, as q4_apply takes them."""
+    args, h, dev = _norm_args(x, weight, residual, eps, sum)
+    rows, n = args[4], args[5]
+    y, ldy = _like(out, "out", (rows, n), _e4m3_dtype(), dev)
+    scales = _empty((rows,), _whole_dtypes()[2], dev)
+    _launch(dev, "lrc_rms_norm", *args, y.data_ptr(), ldy, E4M3, scales.data_ptr(), None)
+    return y, scales, h
+
+
+def rms_norm_backward(dy, h, weight, rstd, dsum=None, dx=None):
+    """Gradient of rms_norm from dy (the gradient of y), h and rstd as it
+    returned them: (dx, dweight), dx that of h (of x and of the residual
+    alike) with dsum added, the gradient that reaches h by other ways, and
+    dweight in weight's dtype (None without a weight).  dx may be dy or dsum."""
+    _need(dy.dim() == 2 and h.shape == dy.shape and h.dtype == dy.dtype, "dy and h must be matrices of one shape and dtype")
+    rows, n = dy.shape
+    prec = _head_prec(dy.dtype)
+    dev = dy.device
+    lddy, ldh = _rows(dy, "dy"), _rows(h, "h")
+    pr = _row_values(rstd, "rstd", rows, _whole_dtypes()[2])
+    _need(pr is not None, "rstd must be given")
+    _on(dev, h=h, weight=weight, rstd=rstd, dsum=dsum)
+    pd, ldd = None, 0
+    if dsum is not None:
+        _need(dsum.shape == dy.shape and dsum.dtype == dy.dtype, "dsum must have dy's shape and dtype")
+        pd, ldd = dsum.data_ptr(), _rows(dsum, "dsum")
+    pw, wprec, dw = None, 0, None
+    if weight is not None:
+        wprec = _head_prec(weight.dtype)
+        _need(weight.shape == (n,) and weight.is_contiguous(), f"weight must hold {n} contiguous values")
+        pw, dw = weight.data_ptr(), _empty((n,), weight.dtype, dev)
+    dx, ldx = _like(dx, "dx", (rows, n), dy.dtype, dev)
+    _launch(dev, "lrc_rms_norm_backward", dy.data_ptr(), lddy, h.data_ptr(), ldh, pr, rows, n, prec, pw, wprec, pd, ldd,
+            dx.data_ptr(), ldx, dw.data_ptr() if dw is not None else None)
+    return dx, dw
+
+
+def _adapter_args(A, B, ids, scale, rows, dtype, dev):
+    """(m, n, k, count, prec, pointers of A, B, ids and scale)"""
+    _need(A.dim() == 3 and B.dim() == 3, "A and B must be count x k x n and count x m x k")
+    count, k, n = A.shape
+    m = B.shape[1]
+    if B.shape != (count, m, k):
+        raise ValueError(f"shape mismatch: A {tuple(A.shape)}, B {tuple(B.shape)}")
+    _, i64, f32 = _whole_dtypes()
+    if A.dtype != dtype or B.dtype != dtype:
+        raise TypeError(f"A and B have dtype {A.dtype} and {B.dtype}, want {dtype}")
+    pi = _row_values(ids, "ids", rows, i64)
+    _need(pi is not None, "ids must be given")
+    if scale is not None:
+        if scale.dtype != f32:
+            raise TypeError(f"scale has dtype {scale.dtype}, want {f32}")
+        _need(scale.shape == (count,) and scale.is_contiguous(), f"scale must hold {count} contiguous values")
+    _on(dev, A=A, B=B, ids=ids, scale=scale)
+    _need(A.is_contiguous() and B.is_contiguous(), "tensors must be contiguous (row-major)")
+    return m, n, k, count, _head_prec(dtype), A.data_ptr(), B.data_ptr(), pi, scale.data_ptr() if scale is not None else None
+
+
+def adapter_apply(X, A, B, ids, scale=None, base=None, hidden: bool = False, Y=None):
+    """Low-rank adapters of many requests beside a shared projection:
+    Y_i = base_i + scale_a (X_i A_a^T) B_a^T with a = ids_i (int64, one per
+    row); rows whose id is outside [0, count) have none.  X rows x n (float32,
+    float16 or bfloat16, contiguous rows), A count x k x n, B count x m x k,
+    base (rows x m, what the shared projection gave) or None: 0, all of X's
+    dtype, scale (count, float32) or None: 1.  Y may be base.  With
+    hidden=True also X_i A_a^T (rows x k, float32), which adapter_backward
+    takes."""
+    _need(X.dim() == 2, "X must be a matrix")
+    rows = X.shape[0]
+    dev = X.device
+    m, n, k, count, prec, pA, pB, pi, ps = _adapter_args(A, B, ids, scale, rows, X.dtype, dev)
+    _need(X.shape[1] == n, f"X has {X.shape[1]} columns, A {n}")
+    ldx = _rows(X, "X")
+    pb, ldb = None, 0
+    if base is not None:
+        _need(base.shape == (rows, m) and base.dtype == X.dtype, f"base must be {(rows, m)} of {X.dtype}")
+        _on(dev, base=base)
+        pb, ldb = base.data_ptr(), _rows(base, "base")
+    Y, ldy = _like(Y, "Y", (rows, m), X.dtype, dev)
+    H = _empty((rows, k), _whole_dtypes()[2], dev) if hidden else None
+    _launch(dev, "lrc_adapter_apply", X.data_ptr(), ldx, pA, pB, pi, ps, rows, m, n, k, count, prec, pb, ldb,
+            Y.data_ptr(), ldy, H.data_ptr() if hidden else None)
+    return (Y, H) if hidden else Y
+
+
+def adapter_backward(dY, X, A, B, ids, hidden, scale=None, base=None, dX=None):
+    """Gradients (dX, dA, dB) of adapter_apply from dY (rows x m) and the
+    hidden values that it returned; base (rows x n, X's dtype) is added to dX,
+    the shared projection's part of it (dX may be base).  base's own gradient
+    is dY; adapters without rows get zeros."""
+    _need(X.dim() == 2 and dY.dim() == 2, "X and dY must be matrices")
+    rows = X.shape[0]
+    dev = X.device
+    m, n, k, count, prec, pA, pB, pi, ps = _adapter_args(A, B, ids, scale, rows, X.dtype, dev)
+    _need(X.shape[1] == n, f"X has {X.shape[1]} columns, A {n}")
+    _need(dY.shape == (rows, m) and dY.dtype == X.dtype, f"dY must be {(rows, m)} of {X.dtype}")
+    _need(hidden.shape == (rows, k) and hidden.dtype == _whole_dtypes()[2] and hidden.is_contiguous(),
+          f"hidden must be {(rows, k)} of float32, contiguous")
+    ldx, lddy = _rows(X, "X"), _rows(dY, "dY")
+    _on(dev, dY=dY, hidden=hidden, base=base)
+    pb, ldb = None, 0
+    if base is not None:
+        _need(base.shape == (rows, n) and base.dtype == X.dtype, f"base must be {(rows, n)} of {X.dtype}")
+        pb, ldb = base.data_ptr(), _rows(base, "base")
+    dX, lddx = _like(dX, "dX", (rows, n), X.dtype, dev)
+    dA, dB = _empty((count, k, n), X.dtype, dev), _empty((count, m, k), X.dtype, dev)
+    _launch(dev, "lrc_adapter_backward", dY.data_ptr(), lddy, X.data_ptr(), ldx, pA, pB, pi, ps, hidden.data_ptr(), rows,
+            m, n, k, count, prec, pb, ldb, dX.data_ptr(), lddx, dA.data_ptr(), dB.data_ptr())
+    return dX, dA, dB
+
+
+def _request_rows(t, name, requests, rows, vocab):
+    """Pitches (of a row, of a request) of requests x rows x vocab logits."""
+    _need(t.shape == (requests, rows, vocab), f"{name} has shape {tuple(t.shape)}, want {(requests, rows, vocab)}")
+    lr, ld, step = t.stride()
+    if step != 1 and vocab > 1:
+        raise ValueError(f"the rows of {name} must be contiguous")
+    ld = ld if rows > 1 else vocab
+    return ld, lr if requests > 1 else max(ld, vocab)
+
+
+def verify(logits, drafts, u, draft_logits=None, temperature=None, top_k=None, top_p=None, min_p=None):
+    """Drafted tokens checked against the target's logits so that the tokens
+    follow the distribution that sample draws from: (tokens, accepted), tokens
+    requests x (D + 1) (int64: the accepted drafts, one drawn token, then -1)
+    and accepted (requests, int64).  logits requests x (D + 1) x vocab
+    (float32, float16 or bfloat16, contiguous rows): row j behind the first j
+    drafts; drafts requests x D (int64), one outside the vocabulary ends its
+    request's; draft_logits requests x D x vocab what sample drew them from
+    under the same parameters, or None: drafts that were certain; u requests x
+    (D + 1) (float32) uniform numbers, the last for the drawn token;
+    temperature, top_p, min_p (float32) and top_k (int64) one value per
+    request, or None, as in sample."""
+    _need(logits.dim() == 3 and drafts.dim() == 2, "logits must have three dimensions, drafts two")
+    R, D = drafts.shape
+    vocab = logits.shape[2]
+    prec = _head_prec(logits.dtype)
+    _, i64, f32 = _whole_dtypes()
+    if drafts.dtype != i64 or u.dtype != f32:
+        raise TypeError(f"drafts and u have dtype {drafts.dtype} and {u.dtype}, want {i64} and {f32}")
+    ld, lr = _request_rows(logits, "logits", R, D + 1, vocab)
+    _need(u.shape == (R, D + 1), f"u has shape {tuple(u.shape)}, want {(R, D + 1)}")
+    _need(drafts.is_contiguous() and u.is_contiguous(), "drafts and u must be contiguous (row-major)")
+    pq, ldq, lrq = None, 0, 0
+    if draft_logits is not None:
+        if draft_logits.dtype != logits.dtype:
+            raise TypeError(f"draft_logits have dtype {draft_logits.dtype}, want {logits.dtype}")
+        ldq, lrq = _request_rows(draft_logits, "draft_logits", R, D, vocab)
+        pq = draft_logits.data_ptr()
+    pt = _row_values(temperature, "temperature", R, f32)
+    pk = _row_values(top_k, "top_k", R, i64)
+    pp = _row_values(top_p, "top_p", R, f32)
+    pm = _row_values(min_p, "min_p", R, f32)
+    dev = logits.device
+    _on(dev, drafts=drafts, u=u, draft_logits=draft_logits, temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p)
+    tokens, accepted = _empty((R, D + 1), i64, dev), _empty((R,), i64, dev)
+    _launch(dev, "lrc_verify", logits.data_ptr(), ld, lr, pq, ldq, lrq, R, D, vocab, prec, drafts.data_ptr(), u.data_ptr(),
+            pt, pk, pp, pm, tokens.data_ptr(), accepted.data_ptr())
+    return tokens, accepted
 
 
 def _result(res: CertResult) -> dict:
