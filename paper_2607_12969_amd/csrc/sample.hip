@@ -139,7 +139,7 @@ __global__ __launch_bounds__(kThreads) void k_sample_row(SampleArgs a, unsigned 
     __syncthreads();
     find_bin(s, true, (u64)k, bin, before, beforec);
     const int last = bin < 0 ? kBins : bin;          // fewer than k tokens weigh anything: all of them
-    const int n = gather_down_to(s, row, wt, last);
+    const int n = gather_down_to<T>(s, row, wt, last);
     if (lane == 0) s.ln[wave] = n;
     __syncthreads();
     bool fits = true;
@@ -317,7 +317,7 @@ __global__ __launch_bounds__(kThreads) void k_sample_gather(SampleArgs a, SplitB
     if (q.topk || q.topp) find_cut_bin(s, q, b.hist + r * kBins, target, bin, before, beforec);
     if (q.topk) {
         // in index order: the waves' lists one after another
-        const int n = gather_down_to(s, row, wt, bin < 0 ? kBins : bin);
+        const int n = gather_down_to<T>(s, row, wt, bin < 0 ? kBins : bin);
         if (lane == 0) s.ln[wave] = n;
         __syncthreads();
         int from = 0, total = 0;

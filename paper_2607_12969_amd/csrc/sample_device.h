@@ -69,6 +69,7 @@ struct Shared {
     unsigned beforec;
     unsigned kmin, kmax;
     int nb;                              // values in the bin of the cut
+    unsigned eq;                         // values equal to the cut
 };
 
 __device__ __forceinline__ void clear_bins(Shared& s) {
@@ -126,6 +127,7 @@ struct Cut {
     float v;             // all logits above v ...
     u64 above;           // ... their mass ...
     unsigned count;      // ... and number
+    unsigned eq;         // logits equal to v; 0: not counted
 };
 
 // A row in memory, or the 16 L logits of it from `base` on: wave w takes the
@@ -153,10 +155,13 @@ template <typename T> struct Row {
     __device__ __forceinline__ unsigned begin(int wave) const {
         return (unsigned)std::min<uint64_t>(V, (uint64_t)base + (uint64_t)wave * L);
     }
-    // every logit of this wave's part
-    template <typename F> __device__ __forceinline__ void each(F&& f) const {
+    // the blocks of this wave's part, and every logit of it
+    template <typename F> __device__ __forceinline__ void part(F&& f) const {
         const int wave = threadIdx.x >> 6;
-        visit(begin(wave), begin(wave + 1), [&](unsigned, const uint4v_t& v) {
+        visit(begin(wave), begin(wave + 1), f);
+    }
+    template <typename F> __device__ __forceinline__ void each(F&& f) const {
+        part([&](unsigned, const uint4v_t& v) {
 #pragma unroll
             for (int e = 0; e < E; ++e) f(elem<T>(v, e));
         });
@@ -182,6 +187,7 @@ __device__ __noinline__ Cut refine(Shared& s, W wt, bool by_count, u64 target, i
     if (t == 0) {
         s.kmin = ~0u;
         s.kmax = 0u;
+        s.eq = 0u;
         s.nb = 0;
         s.before = before;
         s.beforec = beforec;
@@ -223,10 +229,11 @@ __device__ __noinline__ Cut refine(Shared& s, W wt, bool by_count, u64 target, i
                 s.kmin = key;
                 s.before = above;
                 s.beforec = c;
+                s.eq = eq;
             }
         }
         __syncthreads();
-        const Cut cut{of_key(s.kmin), s.before, s.beforec};
+        const Cut cut{of_key(s.kmin), s.before, s.beforec, s.eq};
         __syncthreads();
         return cut;
     }
@@ -259,7 +266,7 @@ __device__ __noinline__ Cut refine(Shared& s, W wt, bool by_count, u64 target, i
         hi = top;
     }
     __syncthreads();
-    return Cut{of_key(hi), before, beforec};
+    return Cut{of_key(hi), before, beforec, 0u};
 }
 
 // Kept tokens: logits above v and the first `ties` equal to v, of weight at least
@@ -478,12 +485,12 @@ __device__ __noinline__ void sample_any(Shared& s, Row<T> row, W wt, int64_t k, 
 
 // The tokens of this wave's part down to bin `last`, in index order, to its list in
 // LDS; their number, which may pass the list's kPart entries.
-template <typename T>
-__device__ __forceinline__ int gather_down_to(Shared& s, const Row<T>& row, const Weigh& wt, int last) {
+template <typename T, typename R>
+__device__ __forceinline__ int gather_down_to(Shared& s, const R& row, const Weigh& wt, int last) {
     constexpr int E = kVec<T>;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int n = 0;
-    row.visit(row.begin(wave), row.begin(wave + 1), [&](unsigned i, const uint4v_t& v) {
+    row.part([&](unsigned i, const uint4v_t& v) {
         unsigned mask = 0;
 #pragma unroll
         for (int e = 0; e < E; ++e) {

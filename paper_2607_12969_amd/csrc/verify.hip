@@ -11,10 +11,11 @@
 // of sample.hip.  All sums are of whole numbers: the result does not depend on how
 // the work is split.
 //
-// Two launches.  The first, one workgroup a row, passes each row as often as its
+// Three launches.  The first, one workgroup a row, passes each row as often as its
 // filters need (maximum; bins, cut; sum) and leaves which tokens it keeps, their sum
-// and the draft's weight; the vector units bound it, as they do the draw.  The second,
-// one workgroup a request, decides and draws from one row or two.
+// and the draft's weight.  The others decide and draw: sums over parts of the row (or two)
+// that a request draws from, then the part that holds the token (by one workgroup a
+// request in one launch 48 requests of 65536 took 60 us, 8 + 6 in two).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -25,6 +26,7 @@ namespace lrc {
 
 namespace {
 
+constexpr int kHeld = 8;                 // vectors of a thread that stay in registers
 enum : unsigned { NOTHING = 0, FINITE = 1, INFINITE = 2, GREEDY = 3 };
 
 // What a row keeps: logits above v, and those equal to v up to index `last`, of weight
@@ -53,6 +55,26 @@ __device__ __forceinline__ int drafts_of(const VerifyArgs& a, int64_t r) {
     return D;
 }
 
+// How many of the first `limit` drafts of request r are taken; 64 at a time, a lane each,
+// alike in every wave.
+__device__ __forceinline__ int taken_of(const VerifyArgs& a, const RowLaw* lp, const RowLaw* lq, int64_t r, int limit) {
+    const int lane = threadIdx.x & 63;
+    const bool sure = !a.draft_logits;
+    const float* u = a.u + r * (a.drafts + 1);
+    for (int n = 0; n < limit; n += 64) {
+        const int j = n + lane;
+        bool no = false;
+        if (j < limit) {
+            const float x = u[j] > 0.0f ? std::min(u[j], 0.99999994f) : 0.0f;
+            const double wq = sure ? 1.0 : (double)lq[j].wt, Sq = sure ? 1.0 : (double)lq[j].S;
+            no = !(((double)x * wq) * (double)lp[j].S < (double)lp[j].wt * Sq);
+        }
+        const u64 m = __builtin_amdgcn_ballot_w64(no);
+        if (m) return n + __builtin_ctzll(m);
+    }
+    return limit;
+}
+
 // Index of the entry with which the running number of ties reaches `ties` (>= 1), E
 // entries a lane; moves `seen` past a block that does not reach it and returns false.
 template <int E>
@@ -78,6 +100,37 @@ __device__ __forceinline__ bool find_tie(u64 ties, u64& seen, const bool (&tied)
         if (tied[e] && ++n == ties) *out = (int)at[e];
     return true;
 }
+
+// A row whose first NV blocks of each wave stay in registers between the passes (what
+// 256 compute units pass at once does not fit L2: each further pass met the memory's rate).
+template <typename T, int NV> struct HeldRow : Row<T> {
+    using Base = Row<T>;
+    static constexpr int E = Base::E, B = Base::B;
+    uint4v_t v[NV];
+    __device__ __forceinline__ HeldRow(const T* row, unsigned V, unsigned L) : Base{row, V, L, 0} {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const unsigned lane = (threadIdx.x & 63) * E, from = this->begin(wave), to = this->begin(wave + 1);
+#pragma unroll
+        for (int q = 0; q < NV; ++q) {
+            v[q] = uint4v_t{kNegInfPair<T>, kNegInfPair<T>, kNegInfPair<T>, kNegInfPair<T>};
+            if (from + q * B < to) v[q] = load_row16(row, (int64_t)from + q * B + lane, (int64_t)V);
+        }
+    }
+    template <typename F> __device__ __forceinline__ void part(F&& f) const {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const unsigned lane = (threadIdx.x & 63) * E, from = this->begin(wave), to = this->begin(wave + 1);
+#pragma unroll
+        for (int q = 0; q < NV; ++q)
+            if (from + q * B < to) f(from + q * B + lane, v[q]);
+        if (from + NV * B < to) this->visit(from + NV * B, to, f);
+    }
+    template <typename F> __device__ __forceinline__ void each(F&& f) const {
+        part([&](unsigned, const uint4v_t& x) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) f(elem<T>(x, e));
+        });
+    }
+};
 
 // Kept mass of the waves' sums, and the last tie that is kept.  `walk(f)` calls
 // f(tied, at), for each block of this wave's part in order, until it returns true.
@@ -113,8 +166,8 @@ __device__ __forceinline__ void finish_law(Shared& s, const Kept<W>& k, u64 sum,
     }
 }
 
-template <typename T, typename W>
-__device__ __forceinline__ void law_of_row(Shared& s, const Row<T>& row, const Kept<W>& k, RowLaw& law) {
+template <typename T, typename R, typename W>
+__device__ __forceinline__ void law_of_row(Shared& s, const R& row, const Kept<W>& k, RowLaw& law) {
     constexpr int E = kVec<T>;
     u64 sum = 0;
     unsigned eq = 0;
@@ -141,16 +194,24 @@ __device__ __forceinline__ void law_of_row(Shared& s, const Row<T>& row, const K
 }
 
 // Rows whose cut the fast paths do not hold: every pass over the row.
+// A cut with ties that are not all kept.
+template <typename T>
+__device__ __noinline__ void law_ties(Shared& s, Row<T> row, Kept<Weigh> kept, RowLaw* law) {
+    RowLaw o = *law;
+    law_of_row<T>(s, row, kept, o);
+    *law = o;
+}
+
 template <typename T, typename W>
 __device__ __noinline__ void law_any(Shared& s, Row<T> row, W wt, int64_t k, float p, float floor_w, RowLaw* law) {
     RowLaw o = *law;
     const Kept<W> kept = cut_any(s, row, wt, k, p, floor_w);
-    law_of_row(s, row, kept, o);
+    law_of_row<T>(s, row, kept, o);
     *law = o;
 }
 
-template <typename T>
-__device__ __forceinline__ RowLaw row_law(Shared& s, const Row<T>& row, float temp, int64_t k, float p, float mp) {
+template <typename T, int NV>
+__device__ __forceinline__ RowLaw row_law(Shared& s, HeldRow<T, NV>& row, float temp, int64_t k, float p, float mp) {
     constexpr int E = kVec<T>;
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
     RowLaw law{kNegInf, 0.0f, kNegInf, 0.0f, ~0u, NOTHING, 0, 0};
@@ -161,6 +222,7 @@ __device__ __forceinline__ RowLaw row_law(Shared& s, const Row<T>& row, float te
     if (t == 0) s.n = 0;
     float M = kNegInf;
     row.each([&](float l) { M = __builtin_fmaxf(M, l); });
+    stay(row.v);
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) M = __builtin_fmaxf(M, __shfl_xor(M, off, 64));
     if (lane == 0) s.redf[wave] = M;
@@ -171,7 +233,7 @@ __device__ __forceinline__ RowLaw row_law(Shared& s, const Row<T>& row, float te
     if (M == kNegInf) return law;
     if (!(temp > 0.0f)) {        // the first logit equal to the maximum
         unsigned at = row.V;
-        row.visit(row.begin(wave), row.begin(wave + 1), [&](unsigned i, const uint4v_t& v) {
+        row.part([&](unsigned i, const uint4v_t& v) {
 #pragma unroll
             for (int e = E - 1; e >= 0; --e)
                 if (elem<T>(v, e) == M) at = std::min(at, i + e);
@@ -189,7 +251,7 @@ __device__ __forceinline__ RowLaw row_law(Shared& s, const Row<T>& row, float te
     law.floor_w = mp > 0.0f ? std::min(mp, 1.0f) : 0.0f;
     if (M == __builtin_inff()) {
         law.mode = INFINITE;
-        law_any(s, row, WeighInf{}, k, p, law.floor_w, &law);
+        law_any(s, static_cast<const Row<T>&>(row), WeighInf{}, k, p, law.floor_w, &law);
         return law;
     }
     law.mode = FINITE;
@@ -215,24 +277,56 @@ __device__ __forceinline__ RowLaw row_law(Shared& s, const Row<T>& row, float te
             __syncthreads();
             const u64 target = mass_target(p, mass);
             find_bin(s, false, target, bin, before, beforec);
-            // the values in that bin, in any order
-            row.each([&](float l) {
-                const float z = wt.z(l);
+            stay(row.v);
+            // the values in that bin, in any order, and the mass that min-p alone keeps
+            auto take = [&](float l, float z) {
                 if (z >= -31.0f && bin_of(z) == bin) {
                     const int at = atomicAdd(&s.n, 1);
                     if (at < kWaves * kPart) s.lv[at] = l;
                 }
-            });
+            };
+            u64 least = 0;
+            if (law.floor_w > 0.0f) {
+                row.each([&](float l) {
+                    const float z = wt.z(l), w = __builtin_amdgcn_exp2f(z);
+                    take(l, z);
+                    least += w >= law.floor_w ? Weigh::q(w) : 0u;
+                });
+                least = wave_add(least);
+            } else {
+                row.each([&](float l) { take(l, wt.z(l)); });
+            }
             __syncthreads();
             const int n = s.n;
             if (bin < 0 || n > kWaves * kPart) {
-                law_any(s, row, wt, 0, p, law.floor_w, &law);
+                law_any(s, static_cast<const Row<T>&>(row), wt, 0, p, law.floor_w, &law);
                 return law;
             }
             const Cut cut = refine(s, wt, false, target, bin, before, 0u, List{s.lv, t, n, kThreads});
             kept.cut(cut.v, ties_to(target, cut.above, Weigh::q(wt.w(cut.v))));
+            if (cut.eq == 0 || cut.eq > kept.ties) {
+                law_ties(s, static_cast<const Row<T>&>(row), kept, &law);
+                return law;
+            }
+            law.v = cut.v;
+            if (kept.qv) {                   // min-p keeps the cut, and so all above it
+                law.S = cut.above + cut.eq * kept.qv;
+                return law;
+            }
+            if (lane == 0) s.red[wave] = least;
+            __syncthreads();
+            for (int w = 0; w < kWaves; ++w) law.S += s.red[w];
+            return law;
         }
-        law_of_row(s, row, kept, law);
+        u64 sum = 0;                         // all, or what min-p keeps
+        row.each([&](float l) {
+            const float w = wt.w(l);
+            sum += w >= law.floor_w ? Weigh::q(w) : 0u;
+        });
+        sum = wave_add(sum);
+        if (lane == 0) s.red[wave] = sum;
+        __syncthreads();
+        for (int w = 0; w < kWaves; ++w) law.S += s.red[w];
         return law;
     }
     // top-k: counts, then the tokens down to the bin of the k-th, in index order
@@ -242,13 +336,14 @@ __device__ __forceinline__ RowLaw row_law(Shared& s, const Row<T>& row, float te
     });
     __syncthreads();
     find_bin(s, true, (u64)k, bin, before, beforec);
-    const int n = gather_down_to(s, row, wt, bin < 0 ? kBins : bin);
+    stay(row.v);
+    const int n = gather_down_to<T>(s, row, wt, bin < 0 ? kBins : bin);
     if (lane == 0) s.ln[wave] = n;
     __syncthreads();
     bool fits = true;
     for (int w = 0; w < kWaves; ++w) fits &= s.ln[w] <= kPart;
     if (!fits) {
-        law_any(s, row, wt, k, p, law.floor_w, &law);
+        law_any(s, static_cast<const Row<T>&>(row), wt, k, p, law.floor_w, &law);
         return law;
     }
     const List list{s.lv, wave * kPart + lane, wave * kPart + n, 64};
@@ -272,21 +367,24 @@ __device__ __forceinline__ RowLaw row_law(Shared& s, const Row<T>& row, float te
 
 }  // namespace
 
-// One workgroup a row: request r's rows are the target's 0 .. drafts, then the draft
-// model's 0 .. drafts - 1.  Rows that its drafts do not reach are left out.
+// One workgroup a row, for the places [j0, j1): the target's rows of a request, then the
+// draft model's.  Rows that its drafts do not reach are left out, and so are all of a request
+// that an earlier launch saw reject a draft.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void k_verify_rows(VerifyArgs a, RowLaw* __restrict__ laws, unsigned L) {
+__global__ __launch_bounds__(kThreads) void k_verify_rows(VerifyArgs a, RowLaw* __restrict__ laws, unsigned L, int j0, int j1) {
     __shared__ Shared s;
-    const int per = (int)a.drafts + 1 + (a.draft_logits ? (int)a.drafts : 0);
-    const int64_t r = blockIdx.x / per;
-    const int at = (int)(blockIdx.x % per);
-    const bool target = at <= a.drafts;
-    const int j = target ? at : at - (int)a.drafts - 1;
+    const int D = (int)a.drafts, n = j1 - j0 + (a.draft_logits ? std::min(j1, D) - j0 : 0);
+    const int64_t r = blockIdx.x / n;
+    const int at = (int)(blockIdx.x % n);
+    const bool target = at < j1 - j0;
+    const int j = j0 + (target ? at : at - (j1 - j0));
     const int have = drafts_of(a, r);
     if (j > have || (!target && j == have)) return;
+    RowLaw* mine = laws + r * (D + 1 + (a.draft_logits ? D : 0));
+    if (j0 > 0 && taken_of(a, mine, mine + D + 1, r, j0) < j0) return;
     const T* logits = target ? static_cast<const T*>(a.logits) + r * a.lr + j * a.ld
                              : static_cast<const T*>(a.draft_logits) + r * a.lrq + j * a.ldq;
-    const Row<T> row{logits, (unsigned)a.vocab, L, 0};
+    HeldRow<T, kHeld> row(logits, (unsigned)a.vocab, L);
     RowLaw law = row_law(s, row, a.temperature ? a.temperature[r] : 1.0f, a.top_k ? a.top_k[r] : 0,
                          a.top_p ? a.top_p[r] : 1.0f, a.min_p ? a.min_p[r] : 0.0f);
     if (threadIdx.x == 0) {
@@ -294,145 +392,175 @@ __global__ __launch_bounds__(kThreads) void k_verify_rows(VerifyArgs a, RowLaw* 
             const int64_t d = a.draft[r * a.drafts + j];
             law.wt = law.weight((float)logits[d], (unsigned)d);
         }
-        laws[blockIdx.x] = law;
+        mine[target ? j : D + 1 + j] = law;
     }
 }
 
-// One workgroup a request: how many drafts are taken, and the token behind them.
+namespace {
+
+// What a request draws its token from: the row behind its accepted drafts, or what that
+// row has above the draft model's.
+template <typename T> struct Source {
+    RowLaw p, q;
+    const T *prow, *qrow;
+    double ap, aq;
+    unsigned drafted, V;
+    int taken;
+    bool rest, sure;
+    // weight in the row itself, and above the draft's
+    __device__ __forceinline__ void weights(float lp, float lq, unsigned i, u64& plain, u64& above) const {
+        const unsigned w = p.weight(lp, i);
+        plain = w;
+        above = 0;
+        if (rest) {
+            const u64 P = (u64)((double)w * ap);
+            const u64 Q = sure ? (i == drafted ? 1ull << 52 : 0ull) : (u64)((double)q.weight(lq, i) * aq);
+            above = P > Q ? P - Q : 0ull;
+        }
+    }
+    __device__ __forceinline__ uint4v_t load_p(unsigned at) const { return load_row16(prow, (int64_t)at, (int64_t)V); }
+    __device__ __forceinline__ uint4v_t load_q(unsigned at) const {
+        return rest && !sure ? load_row16(qrow, (int64_t)at, (int64_t)V) : uint4v_t{0, 0, 0, 0};
+    }
+    __device__ __forceinline__ Source(const VerifyArgs& a, const RowLaw* laws, int64_t r) {
+        const int64_t D = a.drafts;
+        sure = !a.draft_logits;
+        const RowLaw* lp = laws + r * (D + 1 + (sure ? 0 : D));
+        const RowLaw* lq = lp + D + 1;
+        const int have = drafts_of(a, r);
+        taken = taken_of(a, lp, lq, r, have);
+        rest = taken < have;
+        p = lp[taken];
+        q = rest && !sure ? lq[taken] : RowLaw{0.0f, 0.0f, 0.0f, 0.0f, 0u, NOTHING, 0, 0};
+        drafted = rest ? (unsigned)a.draft[r * D + taken] : 0u;
+        ap = 4503599627370496.0 / (double)p.S;
+        aq = q.S ? 4503599627370496.0 / (double)q.S : 0.0;
+        V = (unsigned)a.vocab;
+        prow = static_cast<const T*>(a.logits) + r * a.lr + taken * a.ld;
+        qrow = rest && !sure ? static_cast<const T*>(a.draft_logits) + r * a.lrq + taken * a.ldq : prow;
+    }
+};
+
+}  // namespace
+
+// Sums of a request's weights over its parts of `size` tokens: [request][part][2], of the row
+// itself and of what it has above the draft model's.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void k_verify_draw(VerifyArgs a, const RowLaw* __restrict__ laws, unsigned L) {
-    constexpr int E = kVec<T>, B = 64 * E;
-    __shared__ u64 red[kWaves];
-    __shared__ int taken;
+__global__ __launch_bounds__(256) void k_verify_sums(VerifyArgs a, const RowLaw* __restrict__ laws, u64* __restrict__ sums,
+                                                     unsigned size) {
+    constexpr int E = kVec<T>, B = 256 * E;
+    __shared__ u64 red[4][2];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t r = blockIdx.x, D = a.drafts;
-    const int per = (int)D + 1 + (a.draft_logits ? (int)D : 0);
-    const RowLaw* lp = laws + r * per;
-    const RowLaw* lq = lp + D + 1;
-    const int have = drafts_of(a, r);
-    const float* u = a.u + r * (D + 1);
-    if (wave == 0) {
-        int n = 0;
-        for (; n < have; n += 64) {
-            const int j = n + lane;
-            bool no = false;
-            if (j < have) {
-                const float x = u[j] > 0.0f ? std::min(u[j], 0.99999994f) : 0.0f;
-                const double q = a.draft_logits ? (double)lq[j].wt : 1.0, Sq = a.draft_logits ? (double)lq[j].S : 1.0;
-                no = !(((double)x * q) * (double)lp[j].S < (double)lp[j].wt * Sq);
-            }
-            const u64 m = __builtin_amdgcn_ballot_w64(no);
-            if (m) {
-                n += __builtin_ctzll(m);
-                break;
+    const int64_t r = blockIdx.y;
+    const Source<T> s(a, laws, r);
+    u64 plain = 0, above = 0;
+    if (s.p.mode != NOTHING) {
+        const unsigned from = blockIdx.x * size, to = (unsigned)std::min<uint64_t>(s.V, (uint64_t)from + size);
+#pragma unroll 2
+        for (unsigned i = from; i < to; i += B) {
+            const unsigned at = i + threadIdx.x * E;
+            const uint4v_t v = s.load_p(at), w = s.load_q(at);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                u64 x, y;
+                s.weights(elem<T>(v, e), elem<T>(w, e), at + e, x, y);
+                plain += x;
+                above += y;
             }
         }
-        if (lane == 0) taken = std::min(n, have);
+    }
+    plain = wave_add(plain);
+    above = wave_add(above);
+    if (lane == 0) {
+        red[wave][0] = plain;
+        red[wave][1] = above;
     }
     __syncthreads();
-    const int c = taken;
+    if (threadIdx.x < 2) {
+        u64 t = 0;
+        for (int w = 0; w < 4; ++w) t += red[w][threadIdx.x];
+        sums[(r * gridDim.x + blockIdx.x) * 2 + threadIdx.x] = t;
+    }
+}
+
+// One workgroup a request: its accepted drafts, and the token from the part that holds it.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_verify_draw(VerifyArgs a, const RowLaw* __restrict__ laws, const u64* __restrict__ sums,
+                                                          int parts, unsigned size) {
+    constexpr int E = kVec<T>, B = 64 * E;
+    __shared__ u64 red[kWaves];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t r = blockIdx.x, D = a.drafts;
+    const Source<T> s(a, laws, r);
+    const int c = s.taken;
     int64_t* out = a.tokens + r * (D + 1);
     for (int64_t j = threadIdx.x; j <= D; j += kThreads)
         if (j != c) out[j] = j < c ? a.draft[r * D + j] : -1;
     if (threadIdx.x == 0 && a.accepted) a.accepted[r] = c;
-    const RowLaw p = lp[c];
-    if (p.mode == NOTHING) {
-        if (threadIdx.x == 0) out[c] = -1;
-        return;
-    }
-    bool rest = c < have;
-    const bool sure = !a.draft_logits;
-    const RowLaw q = rest && !sure ? lq[c] : RowLaw{0.0f, 0.0f, 0.0f, 0.0f, 0u, NOTHING, 0, 0};
-    const unsigned drafted = rest ? (unsigned)a.draft[r * D + c] : 0u;
-    const double ap = 4503599627370496.0 / (double)p.S, aq = q.S ? 4503599627370496.0 / (double)q.S : 0.0;
-    const T* prow = static_cast<const T*>(a.logits) + r * a.lr + c * a.ld;
-    const T* qrow = rest && !sure ? static_cast<const T*>(a.draft_logits) + r * a.lrq + c * a.ldq : prow;
-    auto share = [&](float l, float lq_, unsigned i) -> u64 {
-        const unsigned w = p.weight(l, i);
-        if (!rest) return w;
-        const u64 P = (u64)((double)w * ap);
-        const u64 Q = sure ? (i == drafted ? 1ull << 52 : 0ull) : (u64)((double)q.weight(lq_, i) * aq);
-        return P > Q ? P - Q : 0ull;
-    };
-    const unsigned V = (unsigned)a.vocab;
-    // this lane's sum over the blocks of [begin, end)
-    auto sum_of = [&](unsigned begin, unsigned end) {
-        u64 sum = 0;
-#pragma unroll 1
-        for (unsigned i = begin; i < end; i += B) {
-            const unsigned at = i + lane * E;
-            const uint4v_t v = load_row16(prow, (int64_t)at, (int64_t)V), w = load_row16(qrow, (int64_t)at, (int64_t)V);
-#pragma unroll
-            for (int e = 0; e < E; ++e) sum += share(elem<T>(v, e), elem<T>(w, e), at + e);
-        }
-        return wave_add(sum);
-    };
-    auto bound = [&](unsigned from, unsigned step, int w, unsigned to) {
-        return (unsigned)std::min<uint64_t>(to, (uint64_t)from + (uint64_t)w * step);
-    };
-    // which of the waves' sums holds `target`; run: what lies before it
-    auto find = [&](u64 target, u64& run) {
-        for (int w = 0; w < kWaves; ++w) {
-            if (target < run + red[w]) return w;
-            run += red[w];
-        }
-        return -1;
-    };
-    u64 S = 0;
-    for (;;) {
-        const u64 sum = sum_of(bound(0, L, wave, V), bound(0, L, wave + 1, V));
-        if (lane == 0) red[wave] = sum;
-        __syncthreads();
-        for (int w = 0; w < kWaves; ++w) S += red[w];
-        if (S || !rest) break;
-        rest = false;                  // nothing of the target above the draft: the target itself
-        __syncthreads();
-    }
+    // 64 parts at most: a lane each
+    const u64* mine = sums + r * parts * 2;
+    const u64 plain = lane < parts ? mine[2 * lane] : 0, above = lane < parts ? mine[2 * lane + 1] : 0;
+    const u64 all = wave_add(above);
+    const bool rest = all != 0;        // nothing above the draft model's: the target's own
+    u64 run = rest ? above : plain;
+    const u64 S = rest ? all : wave_add(plain);
     if (!S) {
         if (threadIdx.x == 0) out[c] = -1;
         return;
     }
-    const float x = u[D];
+    const float x = a.u[r * (D + 1) + D];
     const double td = (double)(x > 0.0f ? x : 0.0f) * (double)S;
     const u64 target = td >= (double)S ? S - 1 : (u64)td;
-    u64 run = 0;
-    const int part = find(target, run);
-    if (part < 0) return;
-    // the same inside that part
-    const unsigned from = bound(0, L, part, V), to = bound(0, L, part + 1, V);
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const u64 o = __shfl_up(run, off, 64);
+        if (lane >= off) run += o;
+    }
+    const int part = __builtin_ctzll(__builtin_amdgcn_ballot_w64(target < run));
+    u64 before = part ? __shfl(run, part - 1, 64) : 0;
+    // inside the part: the sum of each wave's share, then the share that holds the token
+    const unsigned from = part * size, to = (unsigned)std::min<uint64_t>(s.V, (uint64_t)from + size);
     const unsigned sub = ((to - from + kWaves * B - 1) / (kWaves * B)) * B;
-    __syncthreads();
-    const u64 sum = sum_of(bound(from, sub, wave, to), bound(from, sub, wave + 1, to));
+    auto bound = [&](int w) { return (unsigned)std::min<uint64_t>(to, (uint64_t)from + (uint64_t)w * sub); };
+    auto share = [&](unsigned at, u64 (&h)[E]) {
+        const uint4v_t v = s.load_p(at), w = s.load_q(at);
+        u64 t = 0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            u64 x, y;
+            s.weights(elem<T>(v, e), elem<T>(w, e), at + e, x, y);
+            h[e] = rest ? y : x;
+            t += h[e];
+        }
+        return t;
+    };
+    u64 sum = 0, h[E];
+#pragma unroll 1
+    for (unsigned i = bound(wave); i < bound(wave + 1); i += B) sum += share(i + lane * E, h);
+    sum = wave_add(sum);
     if (lane == 0) red[wave] = sum;
     __syncthreads();
-    const int w = find(target, run);
+    int w = 0;
+    for (; w < kWaves - 1 && target >= before + red[w]; ++w) before += red[w];
     if (wave != w) return;
-    const unsigned end = bound(from, sub, w + 1, to);
 #pragma unroll 1
-    for (unsigned i = bound(from, sub, w, to); i < end; i += B) {
-        const unsigned at = i + lane * E;
-        const uint4v_t v = load_row16(prow, (int64_t)at, (int64_t)V), o = load_row16(qrow, (int64_t)at, (int64_t)V);
-        u64 h[E], mine = 0;
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            h[e] = share(elem<T>(v, e), elem<T>(o, e), at + e);
-            mine += h[e];
-        }
-        u64 scan = mine;
+    for (unsigned i = bound(w); i < bound(w + 1); i += B) {
+        const u64 own = share(i + lane * E, h);
+        u64 scan = own;
 #pragma unroll
         for (int off = 1; off < 64; off <<= 1) {
-            const u64 b = __shfl_up(scan, off, 64);
-            if (lane >= off) scan += b;
+            const u64 o = __shfl_up(scan, off, 64);
+            if (lane >= off) scan += o;
         }
         const u64 block = __shfl(scan, 63, 64);
-        if (target >= run + block) {
-            run += block;
+        if (target >= before + block) {
+            before += block;
             continue;
         }
-        u64 here = run + scan - mine;
+        u64 here = before + scan - own;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            if (target >= here && target < here + h[e]) out[c] = at + e;
+            if (target >= here && target < here + h[e]) out[c] = i + lane * E + e;
             here += h[e];
         }
         return;
@@ -444,9 +572,18 @@ namespace {
 int64_t rows_per(const VerifyArgs& a) { return a.drafts + 1 + (a.draft_logits ? a.drafts : 0); }
 int64_t requests_panel(const VerifyArgs& a) { return std::max<int64_t>(1, kRowPanel / rows_per(a)); }
 
+// Parts of a row that the sums are taken of: about 1024 workgroups, 64 a row at most (a
+// lane each of the next launch), whole steps of 256 vectors.
+unsigned part_size(const VerifyArgs& a, int64_t requests, int e) {
+    const int64_t step = 256 * (16 / e), steps = (a.vocab + step - 1) / step;
+    const int64_t parts = std::min<int64_t>({64, steps, std::max<int64_t>(1, 1024 / requests)});
+    return (unsigned)((steps + parts - 1) / parts * step);
+}
+
 template <typename T> hipError_t verify_t(const VerifyArgs& a, Workspace& ws, hipStream_t st) {
-    const int64_t panel = requests_panel(a);
-    RowLaw* laws = static_cast<RowLaw*>(ws.take((size_t)std::min(a.requests, panel) * rows_per(a) * sizeof(RowLaw)));
+    const int64_t panel = requests_panel(a), most = std::min(a.requests, panel);
+    RowLaw* laws = static_cast<RowLaw*>(ws.take((size_t)most * rows_per(a) * sizeof(RowLaw)));
+    u64* sums = static_cast<u64*>(ws.take((size_t)most * 64 * 2 * sizeof(u64)));
     if (ws.overrun) return hipErrorOutOfMemory;
     const unsigned L = (unsigned)round_up((a.vocab + kWaves - 1) / kWaves, 64 * kVec<T>);
     return in_panels(a.requests, panel, [&](int64_t r, int64_t count) {
@@ -463,20 +600,43 @@ template <typename T> hipError_t verify_t(const VerifyArgs& a, Workspace& ws, hi
         q.min_p = from(a.min_p, 1);
         q.tokens = a.tokens + r * (a.drafts + 1);
         q.accepted = from(a.accepted, 1);
-        {
+        // A round of one row a compute unit first, then twice as many places each time: rows
+        // behind a rejected draft need not be looked at.  48 requests, 5 drafts, 65536
+        // tokens, top-p: 122 us in one launch of three rounds, TWO in two.
+        for (int64_t j0 = 0, some = std::max<int64_t>(1, 128 / count); j0 <= a.drafts; j0 += some, some *= 2) {
+            if (j0) some = std::min(some, a.drafts + 1 - j0);
+            const int64_t j1 = std::min(a.drafts + 1, j0 + some), n = j1 - j0 + (a.draft_logits ? std::min(j1, a.drafts) - j0 : 0);
             KernelTimer t("verify_rows", st);
-            hipLaunchKernelGGL(k_verify_rows<T>, dim3((unsigned)(count * rows_per(a))), dim3(kThreads), 0, st, q, laws, L);
+            hipLaunchKernelGGL(k_verify_rows<T>, dim3((unsigned)(count * n)), dim3(kThreads), 0, st, q, laws, L, (int)j0, (int)j1);
         }
-        KernelTimer t("verify_draw", st);
-        hipLaunchKernelGGL(k_verify_draw<T>, dim3((unsigned)count), dim3(kThreads), 0, st, q, laws, L);
-        return hipGetLastError();
+        const unsigned size = part_size(a, count, sizeof(T));
+        const int parts = (int)((a.vocab + size - 1) / size);
+        // the grid's second dimension ends at 65535
+        return in_panels(count, 65535, [&](int64_t first, int64_t some) {
+            VerifyArgs v = q;
+            v.requests = some;
+            v.logits = static_cast<const T*>(q.logits) + first * a.lr;
+            v.draft_logits = a.draft_logits ? static_cast<const T*>(q.draft_logits) + first * a.lrq : nullptr;
+            v.draft = q.draft ? q.draft + first * a.drafts : nullptr;
+            v.u = q.u + first * (a.drafts + 1);
+            v.tokens = q.tokens + first * (a.drafts + 1);
+            v.accepted = q.accepted ? q.accepted + first : nullptr;
+            const RowLaw* l = laws + first * rows_per(a);
+            {
+                KernelTimer t("verify_sums", st);
+                hipLaunchKernelGGL(k_verify_sums<T>, dim3(parts, (unsigned)some), dim3(256), 0, st, v, l, sums, size);
+            }
+            KernelTimer t("verify_draw", st);
+            hipLaunchKernelGGL(k_verify_draw<T>, dim3((unsigned)some), dim3(kThreads), 0, st, v, l, sums, parts, size);
+            return hipGetLastError();
+        });
     });
 }
 
 }  // namespace
 
 size_t verify_workspace_bytes(const VerifyArgs& a) {
-    return (size_t)std::min(a.requests, requests_panel(a)) * rows_per(a) * sizeof(RowLaw) + 256;
+    return (size_t)std::min(a.requests, requests_panel(a)) * (rows_per(a) * sizeof(RowLaw) + 64 * 2 * sizeof(u64)) + 512;
 }
 
 hipError_t launch_verify(const VerifyArgs& a, Workspace& ws, hipStream_t st) {
