@@ -224,6 +224,25 @@ template <> struct ActTraits<float> : ActTraits<bhalf_t> {
     static constexpr int P = 3;
 };
 
+// e4m3 activations: binary16 holds every one of them.
+struct e4m3_t {
+    unsigned char bits;
+};
+template <> struct ActTraits<e4m3_t> : ActTraits<half_t> {};
+__device__ __forceinline__ half8_t widen_e4m3(uint2v_t v) {
+    half8_t h;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const half2_t lo = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v[e], 1.0f, false);
+        const half2_t hi = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v[e], 1.0f, true);
+        h[4 * e] = lo[0];
+        h[4 * e + 1] = lo[1];
+        h[4 * e + 2] = hi[0];
+        h[4 * e + 3] = hi[1];
+    }
+    return h;
+}
+
 // x = h + m + l exactly, each with 8 significant bits, as bits of bfloat16; an
 // infinity keeps its sign in h alone, NaN stays NaN.
 __device__ __forceinline__ void split3(float x, unsigned (&p)[3]) {
@@ -275,6 +294,19 @@ __device__ __forceinline__ void load_act(const T* x, int64_t j, int64_t n,
     } else {
         f[0] = __builtin_bit_cast(typename ActTraits<T>::frag, v[0]);
     }
+}
+
+template <>
+__device__ __forceinline__ void load_act<e4m3_t>(const e4m3_t* x, int64_t j, int64_t n, half8_t (&f)[1]) {
+    uint2v_t v = {0, 0};
+    if (j + 8 <= n) {
+        __builtin_memcpy(&v, x + j, 8);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (j + e < n) v[e >> 2] |= (unsigned)x[j + e].bits << (8 * (e & 3));
+    }
+    f[0] = widen_e4m3(v);
 }
 
 // Transposes the 4 x 4 words (lane group, register): register t of lane group
@@ -707,6 +739,218 @@ __global__ __launch_bounds__(64 * WX * WR, (TileCfg<T, WX, NX, WR>::EU)) void k_
             }
 }
 
+// ---- many rows of e4m3 activations: tiles on the scaled matrix instructions ------
+// v_mfma_f32_16x16x128_f8f6f4 takes e4m3 and E2M1 operands as they are stored, 128 columns
+// at twice the 16-bit rate, so nothing is widened and a step of 128 columns is one
+// instruction for each 16 x 16 results.  Groups of 32 and 64 take it four times or twice a
+// step, with the other columns' codes as zeros.  Layout as k_q4_tile: WX x WR waves, a wave 16 NR
+// rows of W and 16 NX of X, D LDS buffers filled D - 1 steps ahead; the 16-byte chunks of
+// X's rows (128 bytes a step) and of the codes' (64) are XOR-swizzled by the row on the global
+// side, so that operand reads meet every bank once.  Of a step's columns a lane of group g
+// (lane / 16) supplies the codes 32 g .. 32 g + 31 and the activations 16 g .. 16 g + 15 and 64 + 16 g ..
+// (measured with an in-bounds probe).  Results cross LDS, 32 rows of X at a
+// time, so that a store covers whole rows.
+template <int WX, int NX, int WR> struct Tile8Cfg {
+    static constexpr int NW = WX * WR, NR = WR == 4 && WX == 1 ? 2 : 4;
+    static constexpr int BM = 16 * NR * WR, BT = 16 * NX * WX;                   // rows of W and of X
+    static constexpr int XB = BT * 128, BUF = XB + BM * 64, D = 4;               // bytes of a step, buffers
+    static constexpr int XR = BT / 8, WR16 = BM / 16;                            // 1 KB loads of a step: X, codes
+    static constexpr int XL = (XR + NW - 1) / NW, WL = (WR16 + NW - 1) / NW, LOADS = XL + WL;      // of a wave
+    static constexpr int TR = NX == 1 ? 16 : 32, OP = 16 * NR + 4;               // rows that cross LDS at a time, pitch
+    static constexpr int OUT = NW * TR * OP * 4, LDS = D * BUF > OUT ? D * BUF : OUT;
+};
+
+typedef int int8v_t __attribute__((ext_vector_type(8)));
+
+template <int WX, int NX, int WR, int FL, int SB>
+__global__ __launch_bounds__(64 * WX * WR, 2) void k_q4_tile8(Q4Args a, int tiles_m, int tiles_b) {
+    using C = Tile8Cfg<WX, NX, WR>;
+    constexpr int NR = C::NR, BT = C::BT, BM = C::BM, D = C::D, XL = C::XL, WL = C::WL;
+    __shared__ alignas(16) char S[C::LDS];
+    const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wx = wave % WX, wr = wave / WX;
+    // an XCD's consecutive workgroups take 8 row tiles for one tile of X after another
+    const int64_t lt = xcd_tile((int64_t)tiles_m * tiles_b * a.splits);
+    if (lt >= (int64_t)tiles_m * tiles_b * a.splits) return;
+    const int64_t split = lt / ((int64_t)tiles_m * tiles_b), q = lt % ((int64_t)tiles_m * tiles_b);
+    const int64_t g = q / (8 * tiles_b), gs = std::min<int64_t>(8, tiles_m - 8 * g), in = q - g * 8 * tiles_b;
+    const int64_t i0 = (8 * g + in % gs) * BM, b0 = in / gs * BT;
+
+    float4_t acc[NR][NX];
+#pragma unroll
+    for (int r = 0; r < NR; ++r)
+#pragma unroll
+        for (int f = 0; f < NX; ++f) acc[r][f] = zero_accv<float4_t>();
+    const int64_t blocks = (a.n + 127) / 128;
+    const int64_t k0 = blocks * split / a.splits, k1 = blocks * (split + 1) / a.splits;
+    // a wave moves 8 rows of X a load and 16 rows of codes; where a step has fewer loads than
+    // waves, some repeat another's
+    const char* xs[XL];
+    int xo[XL], co[WL];
+#pragma unroll
+    for (int h = 0; h < XL; ++h) {
+        const int load = (wave * XL + h) % C::XR, r = load * 8 + (lane >> 3);
+        xs[h] = static_cast<const char*>(a.X) + std::min(b0 + r, a.b - 1) * a.ldx + ((lane & 7) ^ (r >> 1 & 7)) * 16;
+        xo[h] = load * 1024;
+    }
+    const unsigned char* cs[WL];
+    int cc[WL];
+#pragma unroll
+    for (int h = 0; h < WL; ++h) {
+        const int load = (wave * WL + h) % C::WR16, r = load * 16 + (lane >> 2);
+        cs[h] = a.codes + std::min(i0 + r, a.m - 1) * a.rb;
+        cc[h] = ((lane & 3) ^ (r >> 2 & 3)) * 16;
+        co[h] = C::XB + load * 1024;
+    }
+    auto move = [&](int64_t kb, int buf) {
+        char* to = S + buf * C::BUF;
+#pragma unroll
+        for (int h = 0; h < XL; ++h)
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(xs[h] + kb * 128),
+                                             (__attribute__((address_space(3))) void*)(to + xo[h]), 16, 0, 0);
+#pragma unroll
+        for (int h = 0; h < WL; ++h)
+            __builtin_amdgcn_global_load_lds(
+                (const __attribute__((address_space(1))) void*)(cs[h] + std::min(kb * 64 + cc[h], a.rb - 16)),
+                (__attribute__((address_space(3))) void*)(to + co[h]), 16, 0, 0);
+    };
+    int64_t srow[NR];                                   // where a row's scales begin
+#pragma unroll
+    for (int r = 0; r < NR; ++r) srow[r] = std::min(i0 + wr * 16 * NR + 16 * r + lr, a.m - 1) * a.G;
+    unsigned sn[NR][4 / FL];
+    auto fetch = [&](int64_t kb) {                      // bits only: converting here would wait for the load
+        int64_t at[4 / FL];
+#pragma unroll
+        for (int t = 0; t < 4 / FL; ++t) at[t] = std::min(kb * 128 + t * 32 * FL, a.n - 1) >> a.gshift;
+#pragma unroll
+        for (int r = 0; r < NR; ++r)
+#pragma unroll
+            for (int t = 0; t < 4 / FL; ++t)
+                sn[r][t] = SB == 4 ? static_cast<const unsigned*>(a.scales)[srow[r] + at[t]]
+                                   : static_cast<const unsigned short*>(a.scales)[srow[r] + at[t]];
+    };
+    const unsigned bf16_mask = a.sprec == PB16 ? ~0u : 0u;
+    if (k0 < k1) fetch(k0);
+#pragma unroll
+    for (int d = 0; d < D - 1; ++d)
+        if (k0 + d < k1) move(k0 + d, d);
+    // products of a row block, which join acc with their scale one block later
+    float4_t d[2][NX];
+    auto flush = [&](int r, int which, float scale) {
+#pragma unroll
+        for (int f = 0; f < NX; ++f)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) acc[r][f][v] += scale * d[which][f][v];
+    };
+#pragma unroll
+    for (int f = 0; f < NX; ++f) d[1][f] = zero_accv<float4_t>();
+    float carry = 0.0f;
+    int buf = 0;
+    for (int64_t kb = k0; kb < k1; ++kb) {
+        // this step has landed when no more than the loads of the D - 2 later ones are on their way
+        if (kb + D - 2 < k1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((D - 2) * C::LOADS) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        float sc[NR][4 / FL];
+#pragma unroll
+        for (int r = 0; r < NR; ++r)
+#pragma unroll
+            for (int t = 0; t < 4 / FL; ++t) sc[r][t] = scale_of_bits<SB>(sn[r][t], bf16_mask);
+        if (kb + 1 < k1) fetch(kb + 1);
+        if (kb + D - 1 < k1) move(kb + D - 1, buf == 0 ? D - 1 : buf - 1);
+        const char* from = S + buf * C::BUF;
+        int8v_t x[NX];
+#pragma unroll
+        for (int f = 0; f < NX; ++f) {
+            const int r = wx * 16 * NX + 16 * f + lr;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint4v_t v = *reinterpret_cast<const uint4v_t*>(from + r * 128 + ((lg + 4 * h) ^ (r >> 1 & 7)) * 16);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[f][4 * h + e] = (int)v[e];
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+            const int row = wr * 16 * NR + 16 * r + lr;
+            const uint4v_t w = *reinterpret_cast<const uint4v_t*>(from + C::XB + row * 64 + (lg ^ (row >> 2 & 3)) * 16);
+#pragma unroll
+            for (int t = 0; t < 4 / FL; ++t) {
+                constexpr int PER = 4 / FL;
+                const int n = r * PER + t, which = n & 1;
+                int8v_t wf = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) wf[e] = FL == 4 || lg / FL == t ? (int)w[e] : 0;
+#pragma unroll
+                for (int f = 0; f < NX; ++f)
+                    d[which][f] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x[f], wf, zero_accv<float4_t>(), 0, 4, 0,
+                                                                                  0x7F7F7F7F, 0, 0x7F7F7F7F);
+                // the block before this one, whose products are done by now
+                const int pr = t ? r : r == 0 ? NR - 1 : r - 1, pt = t ? t - 1 : PER - 1;
+                flush(pr, which ^ 1, n == 0 ? carry : sc[pr][pt]);
+            }
+        }
+        static_assert(NR * (4 / FL) % 2 == 0, "the step's last block lies in the second half of d");
+        carry = sc[NR - 1][4 / FL - 1];
+        buf = buf == D - 1 ? 0 : buf + 1;
+    }
+    flush(NR - 1, 1, carry);
+    if (split == 0 && a.k) {
+        int64_t row[NR];
+        const float* tm[NX];
+#pragma unroll
+        for (int r = 0; r < NR; ++r) row[r] = std::min(i0 + wr * 16 * NR + 16 * r + lr, a.m - 1);
+#pragma unroll
+        for (int f = 0; f < NX; ++f) tm[f] = a.Tm + std::min(b0 + wx * 16 * NX + 16 * f + lr, a.b - 1) * a.kp;
+        add_ranks(a, tm, row, 0, 16, acc);
+    }
+    __syncthreads();
+    float* out = reinterpret_cast<float*>(S) + wave * C::TR * C::OP;
+    constexpr int FB = C::TR / 16, LANES = 16 * NR / 4, ROWS = 64 / LANES;        // lanes of a row, 4 values each
+    const int c4 = lane % LANES * 4, r0 = lane / LANES;
+#pragma unroll
+    for (int f0 = 0; f0 < NX; f0 += FB) {
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int f = 0; f < FB; ++f)
+#pragma unroll
+            for (int r = 0; r < NR; ++r)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) out[(16 * f + 4 * lg + v) * C::OP + 16 * r + lr] = acc[r][f0 + f][v];
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int t = 0; t < C::TR; t += ROWS) {
+            const int64_t b = b0 + wx * 16 * NX + 16 * f0 + t + r0, i = i0 + wr * 16 * NR + c4;
+            float4_t y = *reinterpret_cast<const float4_t*>(out + (t + r0) * C::OP + c4);
+            if (b >= a.b || i >= a.m) continue;
+            if (a.part) {
+                float* p = a.part + (split * a.b + b) * a.m + i;
+                if (i + 4 <= a.m) __builtin_memcpy(p, &y, 16);
+                else
+                    for (int e = 0; e < 4; ++e)
+                        if (i + e < a.m) p[e] = y[e];
+                continue;
+            }
+            const float s = a.xscale[b];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] *= s;
+            const int64_t at = b * a.ldy + i;
+            if (i + 4 > a.m) {
+                for (int e = 0; e < 4; ++e)
+                    if (i + e < a.m) store_from_f32(a.Y, at + e, a.yprec, y[e]);
+            } else if (a.yprec == P32) {
+                __builtin_memcpy(static_cast<float*>(a.Y) + at, &y, 16);
+            } else {
+                const uint2v_t h = a.yprec == P16 ? uint2v_t{pack2<half_t>(y[0], y[1]), pack2<half_t>(y[2], y[3])}
+                                                  : uint2v_t{pack2<bhalf_t>(y[0], y[1]), pack2<bhalf_t>(y[2], y[3])};
+                __builtin_memcpy(static_cast<unsigned short*>(a.Y) + at, &h, 8);
+            }
+        }
+    }
+}
+
 // Y = the sum of the splits, in their order.
 __global__ __launch_bounds__(256) void k_q4_join(const float* __restrict__ part, int splits, int64_t m, int64_t b,
                                                  const float* __restrict__ xscale, void* __restrict__ Y, int64_t ldy,
@@ -733,32 +977,22 @@ __global__ __launch_bounds__(256) void k_q4_pack(const T* __restrict__ X, int64_
     }
 }
 
-// e4m3 activations as binary16, which holds them exactly, in rows of the same padding.
-__global__ __launch_bounds__(256) void k_q4_unpack8(const unsigned char* __restrict__ X, int64_t ldx, int64_t n, int64_t b,
-                                                    half_t* __restrict__ out, int64_t ldp) {
-    const int64_t per = ldp / 8, step = (int64_t)gridDim.x * 256;
+// e4m3 activations in padded rows (pitch ldp, zero from n on).
+__global__ __launch_bounds__(256) void k_q4_pack8(const unsigned char* __restrict__ X, int64_t ldx, int64_t n, int64_t b,
+                                                  unsigned char* __restrict__ out, int64_t ldp) {
+    const int64_t per = ldp / 16, step = (int64_t)gridDim.x * 256;
     for (int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x; c < b * per; c += step) {
         const unsigned char* x = X + c / per * ldx;
-        const int64_t j = c % per * 8;
-        uint2v_t v = {0, 0};
-        if (j + 8 <= n) {
-            __builtin_memcpy(&v, x + j, 8);
+        const int64_t j = c % per * 16;
+        uint4v_t v = {0, 0, 0, 0};
+        if (j + 16 <= n) {
+            v = load16(x + j);
         } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
+            for (int e = 0; e < 16; ++e)
                 if (j + e < n) v[e >> 2] |= (unsigned)x[j + e] << (8 * (e & 3));
         }
-        half8_t h;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const half2_t lo = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v[e], 1.0f, false);
-            const half2_t hi = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v[e], 1.0f, true);
-            h[4 * e] = lo[0];
-            h[4 * e + 1] = lo[1];
-            h[4 * e + 2] = hi[0];
-            h[4 * e + 3] = hi[1];
-        }
-        *reinterpret_cast<half8_t*>(out + c * 8) = h;
+        *reinterpret_cast<uint4v_t*>(out + c * 16) = v;
     }
 }
 
@@ -816,7 +1050,12 @@ __global__ __launch_bounds__(256) void k_q4_mid(const T* __restrict__ X, int64_t
             if (TW == 4 || h == 0) {
                 const int64_t c = j + hh * 32 + lg * 8;
                 float xv[8];
-                if (c + 8 <= j1) {
+                if constexpr (std::is_same_v<T, e4m3_t>) {
+                    half8_t h[1];
+                    load_act<T>(x, c, j1, h);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) xv[e] = (float)h[0][e];
+                } else if (c + 8 <= j1) {
 #pragma unroll
                     for (int q = 0; q < (int)sizeof(T) / 2; ++q) {
                         const uint4v_t v = load16(x + c + q * kVec<T>);
@@ -862,7 +1101,7 @@ __global__ __launch_bounds__(256) void k_q4_mid(const T* __restrict__ X, int64_t
     }
 }
 
-// The same for 16-bit activations and factors, on the 16-bit matrix cores with
+// The same for 16-bit (or e4m3) activations and 16-bit factors, on the 16-bit matrix cores with
 // exact products: both binary16, or bfloat16 with the one of the two that is
 // binary16 as the sum of two bfloat16 values (8 + 3 bits; an infinity of the other
 // meets the first alone, as the second may be 0).  Steps of 128 rows of V
@@ -872,7 +1111,7 @@ template <typename T, bool FV, int F, int TW>
 __global__ __launch_bounds__(256) void k_q4_mid16(const T* __restrict__ X, int64_t ldx,
                                                   const unsigned short* __restrict__ V, int64_t n, int64_t k, int64_t b,
                                                   int64_t chunk, float* __restrict__ part) {
-    constexpr bool XH = std::is_same_v<T, half_t>;
+    constexpr bool XH = !std::is_same_v<T, bhalf_t>;      // binary16, or e4m3 widened to it
     constexpr bool HALF = XH && FV;                       // else bfloat16 products
     constexpr int PX = XH && !FV ? 2 : 1, PV = !XH && FV ? 2 : 1, PITCH = 136;
     using M = ActTraits<std::conditional_t<HALF, half_t, bhalf_t>>;
@@ -1066,8 +1305,7 @@ bool plan_rows(Q4Plan& p, const Q4Weights& w, int64_t b, int prec) {
     return true;
 }
 
-// unpacked: rows of X are zero from n to the next multiple of 128.
-Q4Plan plan_q4(const Q4Weights& w, const void* X, int64_t ldx, int64_t b, int prec, bool unpacked = false) {
+Q4Plan plan_q4(const Q4Weights& w, const void* X, int64_t ldx, int64_t b, int prec) {
     Q4Plan p{};
     const int64_t blocks = (w.n + 127) / 128;
     p.tile = !plan_rows(p, w, b, prec);
@@ -1080,8 +1318,8 @@ Q4Plan plan_q4(const Q4Weights& w, const void* X, int64_t ldx, int64_t b, int pr
         p.splits = (int)std::min<int64_t>(std::max<int64_t>(1, 512 / tiles), std::max<int64_t>(1, blocks / 4));
         const int e = elem_bytes(prec);
         p.ldp = blocks * 128;
-        p.pack = prec == P32 || (w.n % 128 && !unpacked) || reinterpret_cast<uintptr_t>(X) % 16 || ldx * e % 16;
-        if (p.pack) p.planes = (size_t)(prec == P32 ? 3 : 1) * b * p.ldp * 2;
+        p.pack = prec == P32 || w.n % 128 || reinterpret_cast<uintptr_t>(X) % 16 || ldx * e % 16;
+        if (p.pack) p.planes = (size_t)(prec == P32 ? 3 : 1) * b * p.ldp * std::min(e, 2);
         if (p.splits > 1) p.part = (size_t)p.splits * b * w.m * 4;
     }
     if (w.k) {
@@ -1148,6 +1386,28 @@ void tile_t(const Q4Plan& p, const Q4Args& a, hipStream_t st) {
     else tile_sb<T, FL, 2>(p, a, st);
 }
 
+template <int WX, int NX, int WR, int FL, int SB>
+void launch_tile8(const Q4Args& a, hipStream_t st) {
+    using C = Tile8Cfg<WX, NX, WR>;
+    const int tm = (int)((a.m + C::BM - 1) / C::BM), tb = (int)((a.b + C::BT - 1) / C::BT);
+    KernelTimer t("q4_tile8", st);
+    hipLaunchKernelGGL((k_q4_tile8<WX, NX, WR, FL, SB>), dim3(xcd_grid((int64_t)tm * tb * a.splits)), dim3(64 * C::NW), 0, st, a,
+                       tm, tb);
+}
+template <int FL, int SB>
+void tile8_sb(const Q4Plan& p, const Q4Args& a, hipStream_t st) {
+    if (p.wx == 2 && p.wr == 4) return launch_tile8<2, 4, 4, FL, SB>(a, st);
+    if (p.wx == 2) return launch_tile8<2, 4, 2, FL, SB>(a, st);
+    if (p.nx == 1) return launch_tile8<1, 1, 4, FL, SB>(a, st);
+    if (p.nx == 2) return launch_tile8<1, 2, 4, FL, SB>(a, st);
+    launch_tile8<1, 4, 4, FL, SB>(a, st);
+}
+template <int FL>
+void tile8_t(const Q4Plan& p, const Q4Args& a, hipStream_t st) {
+    if (a.sprec == P32) tile8_sb<FL, 4>(p, a, st);
+    else tile8_sb<FL, 2>(p, a, st);
+}
+
 template <typename T, int F>
 void mid_f(const Q4Plan& p, const Q4Weights& w, const Q4Args& a, float* part, hipStream_t st) {
     KernelTimer t("q4_mid", st);
@@ -1155,10 +1415,10 @@ void mid_f(const Q4Plan& p, const Q4Weights& w, const Q4Args& a, float* part, hi
                     (unsigned)((a.b + 16 * p.mid_tw - 1) / (16 * p.mid_tw)));
     const T* x = static_cast<const T*>(a.X);
     const size_t red = (size_t)4 * 16 * 16 * F * 4;
-    if constexpr (sizeof(T) == 2) {
+    if constexpr (sizeof(T) <= 2) {
         if (w.fprec != P32) {
             const bool fv = w.fprec == P16;
-            const size_t lds = std::max<size_t>((size_t)(fv && !std::is_same_v<T, half_t> ? 2 : 1) * 16 * F * 136 * 2, red);
+            const size_t lds = std::max<size_t>((size_t)(fv && std::is_same_v<T, bhalf_t> ? 2 : 1) * 16 * F * 136 * 2, red);
             auto* kern = p.mid_tw == 4 ? (fv ? k_q4_mid16<T, true, F, 4> : k_q4_mid16<T, false, F, 4>)
                                        : (fv ? k_q4_mid16<T, true, F, 1> : k_q4_mid16<T, false, F, 1>);
             hipLaunchKernelGGL(kern, grid, dim3(256), lds, st, x, a.ldx, static_cast<const unsigned short*>(w.V), w.n, w.k,
@@ -1174,7 +1434,7 @@ void mid_f(const Q4Plan& p, const Q4Weights& w, const Q4Args& a, float* part, hi
 
 template <typename T>
 hipError_t apply_t(const Q4Weights& w, Q4Args& a, int prec, Workspace& ws, hipStream_t st) {
-    const Q4Plan p = plan_q4(w, a.X, a.ldx, a.b, prec, a.xscale != nullptr);
+    const Q4Plan p = plan_q4(w, a.X, a.ldx, a.b, prec);
     float* Tm = static_cast<float*>(ws.take(p.tm));
     float* mid = static_cast<float*>(ws.take(p.mid_part));
     unsigned short* planes = static_cast<unsigned short*>(ws.take(p.planes));
@@ -1200,17 +1460,31 @@ hipError_t apply_t(const Q4Weights& w, Q4Args& a, int prec, Workspace& ws, hipSt
         return rows_t<T, 4>(p, a, st);
     }
     a.splits = p.splits;
-    if (p.pack) {
-        KernelTimer t("q4_pack", st);
-        hipLaunchKernelGGL(k_q4_pack<T>, dim3(strided_grid(a.b * (p.ldp / 8))), dim3(256), 0, st,
-                           static_cast<const T*>(a.X), a.ldx, w.n, a.b, planes, p.ldp);
-        a.X = planes;
-        a.ldx = p.ldp;
-        a.plane = a.b * p.ldp;
+    if constexpr (std::is_same_v<T, e4m3_t>) {
+        if (p.pack) {
+            KernelTimer t("q4_pack", st);
+            hipLaunchKernelGGL(k_q4_pack8, dim3(strided_grid(a.b * (p.ldp / 16))), dim3(256), 0, st,
+                               static_cast<const unsigned char*>(a.X), a.ldx, w.n, a.b, reinterpret_cast<unsigned char*>(planes),
+                               p.ldp);
+            a.X = planes;
+            a.ldx = p.ldp;
+        }
+        if (a.gshift == 5) tile8_t<1>(p, a, st);
+        else if (a.gshift == 6) tile8_t<2>(p, a, st);
+        else tile8_t<4>(p, a, st);
+    } else {
+        if (p.pack) {
+            KernelTimer t("q4_pack", st);
+            hipLaunchKernelGGL(k_q4_pack<T>, dim3(strided_grid(a.b * (p.ldp / 8))), dim3(256), 0, st,
+                               static_cast<const T*>(a.X), a.ldx, w.n, a.b, planes, p.ldp);
+            a.X = planes;
+            a.ldx = p.ldp;
+            a.plane = a.b * p.ldp;
+        }
+        if (a.gshift == 5) tile_t<T, 1>(p, a, st);
+        else if (a.gshift == 6) tile_t<T, 2>(p, a, st);
+        else tile_t<T, 4>(p, a, st);
     }
-    if (a.gshift == 5) tile_t<T, 1>(p, a, st);
-    else if (a.gshift == 6) tile_t<T, 2>(p, a, st);
-    else tile_t<T, 4>(p, a, st);
     if (p.splits > 1) {
         KernelTimer t("q4_join", st);
         hipLaunchKernelGGL(k_q4_join, dim3((unsigned)((w.m + 255) / 256), (unsigned)a.b), dim3(256), 0, st, a.part, p.splits,
@@ -1227,19 +1501,12 @@ hipError_t apply_t(const Q4Weights& w, Q4Args& a, int prec, Workspace& ws, hipSt
 constexpr int64_t kQ4Panel = 1 << 20;
 int64_t weight_panel(int64_t batch) { return std::min<int64_t>(1 << 28, ((int64_t)1 << 36) / batch); }
 
-// 8-bit activations widened: rows of whole 128 columns, zero from n on.
-static int64_t unpacked_pitch(int64_t n) { return round_up(n, 128); }
-static size_t unpacked_bytes(int64_t n, int64_t b) { return (size_t)round_up(b * unpacked_pitch(n) * 2, 256); }
-
 size_t q4_apply_workspace_bytes(const Q4Weights& w, const void* X, int64_t ldx, int64_t batch, int prec) {
     size_t bytes = 0;
-    const bool e4m3 = prec == PE4M3;                       // as binary16 in rows of their own
     auto panel = [&](int64_t m, int64_t b) {
         Q4Weights part = w;
         part.m = m;
-        if (m && b)
-            bytes = std::max(bytes, e4m3 ? plan_bytes(plan_q4(part, nullptr, unpacked_pitch(w.n), b, P16, true)) + unpacked_bytes(w.n, b)
-                                         : plan_bytes(plan_q4(part, X, ldx, b, prec)));
+        if (m && b) bytes = std::max(bytes, plan_bytes(plan_q4(part, X, ldx, b, prec)));
     };
     const int64_t b = std::min(batch, kQ4Panel), m = std::min(w.m, weight_panel(b));
     for (int64_t rows : {b, batch % b}) {
@@ -1277,19 +1544,7 @@ hipError_t launch_q4_apply(const Q4Weights& w, const void* X, int64_t ldx, const
         a.n = w.n;
         a.b = b;
         ws.reset();
-        if (prec == PE4M3) {
-            half_t* x16 = static_cast<half_t*>(ws.take(unpacked_bytes(w.n, b)));
-            if (ws.overrun) return hipErrorOutOfMemory;
-            const int64_t ldp = unpacked_pitch(w.n);
-            {
-                KernelTimer t("q4_unpack8", st);
-                hipLaunchKernelGGL(k_q4_unpack8, dim3(strided_grid(b * (ldp / 8))), dim3(256), 0, st,
-                                   static_cast<const unsigned char*>(a.X), ldx, w.n, b, x16, ldp);
-            }
-            a.X = x16;
-            a.ldx = ldp;
-            return apply_t<half_t>(part, a, P16, ws, st);
-        }
+        if (prec == PE4M3) return apply_t<e4m3_t>(part, a, prec, ws, st);
         return prec == P32   ? apply_t<float>(part, a, prec, ws, st)
                : prec == P16 ? apply_t<half_t>(part, a, prec, ws, st)
                              : apply_t<bhalf_t>(part, a, prec, ws, st);
