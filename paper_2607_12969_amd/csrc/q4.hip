@@ -750,12 +750,14 @@ __global__ __launch_bounds__(64 * WX * WR, (TileCfg<T, WX, NX, WR>::EU)) void k_
 // (lane / 16) supplies the codes 32 g .. 32 g + 31 and the activations 16 g .. 16 g + 15 and 64 + 16 g ..
 // (measured with an in-bounds probe).  Results cross LDS, 32 rows of X at a
 // time, so that a store covers whole rows.
-template <int WX, int NX, int WR> struct Tile8Cfg {
+template <int WX, int NX, int WR, int FL> struct Tile8Cfg {
     static constexpr int NW = WX * WR, NR = WR == 4 && WX == 1 ? 2 : 4;
     static constexpr int BM = 16 * NR * WR, BT = 16 * NX * WX;                   // rows of W and of X
-    static constexpr int XB = BT * 128, BUF = XB + BM * 64, D = 4;               // bytes of a step, buffers
-    static constexpr int XR = BT / 8, WR16 = BM / 16;                            // 1 KB loads of a step: X, codes
-    static constexpr int XL = (XR + NW - 1) / NW, WL = (WR16 + NW - 1) / NW, LOADS = XL + WL;      // of a wave
+    static constexpr int PER = 4 / FL;                                           // scales of a row in a step
+    static constexpr int XB = BT * 128, SB0 = XB + BM * 64, BUF = SB0 + BM * PER * 4, D = 4;       // bytes of a step, buffers
+    static constexpr int XR = BT / 8, WR16 = BM / 16, SR = BM * PER / 64;        // loads of a step: X, codes, scales
+    static constexpr int XL = (XR + NW - 1) / NW, WL = (WR16 + NW - 1) / NW, SL = (SR + NW - 1) / NW;
+    static constexpr int LOADS = XL + WL + SL;                                   // of a wave
     static constexpr int TR = NX == 1 ? 16 : 32, OP = 16 * NR + 4;               // rows that cross LDS at a time, pitch
     static constexpr int OUT = NW * TR * OP * 4, LDS = D * BUF > OUT ? D * BUF : OUT;
 };
@@ -764,8 +766,8 @@ typedef int int8v_t __attribute__((ext_vector_type(8)));
 
 template <int WX, int NX, int WR, int FL, int SB>
 __global__ __launch_bounds__(64 * WX * WR, 2) void k_q4_tile8(Q4Args a, int tiles_m, int tiles_b) {
-    using C = Tile8Cfg<WX, NX, WR>;
-    constexpr int NR = C::NR, BT = C::BT, BM = C::BM, D = C::D, XL = C::XL, WL = C::WL;
+    using C = Tile8Cfg<WX, NX, WR, FL>;
+    constexpr int PER = C::PER, NR = C::NR, BT = C::BT, BM = C::BM, D = C::D, XL = C::XL, WL = C::WL, SL = C::SL;
     __shared__ alignas(16) char S[C::LDS];
     const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -803,6 +805,16 @@ __global__ __launch_bounds__(64 * WX * WR, 2) void k_q4_tile8(Q4Args a, int tile
         cc[h] = ((lane & 3) ^ (r >> 2 & 3)) * 16;
         co[h] = C::XB + load * 1024;
     }
+    // scales: the aligned word that holds each, a word for each row and group
+    const char* ss[SL];
+    int so[SL], sg[SL];
+#pragma unroll
+    for (int h = 0; h < SL; ++h) {
+        const int load = (wave * SL + h) % C::SR, r = load * 64 % BM + lane;
+        sg[h] = load * 64 / BM * 32 * FL;
+        ss[h] = static_cast<const char*>(a.scales) + std::min(i0 + r, a.m - 1) * a.G * SB;
+        so[h] = C::SB0 + load * 256;
+    }
     auto move = [&](int64_t kb, int buf) {
         char* to = S + buf * C::BUF;
 #pragma unroll
@@ -814,24 +826,21 @@ __global__ __launch_bounds__(64 * WX * WR, 2) void k_q4_tile8(Q4Args a, int tile
             __builtin_amdgcn_global_load_lds(
                 (const __attribute__((address_space(1))) void*)(cs[h] + std::min(kb * 64 + cc[h], a.rb - 16)),
                 (__attribute__((address_space(3))) void*)(to + co[h]), 16, 0, 0);
+#pragma unroll
+        for (int h = 0; h < SL; ++h) {
+            const int64_t at = std::min(kb * 128 + sg[h], a.n - 1) >> a.gshift;
+            __builtin_amdgcn_global_load_lds(
+                (const __attribute__((address_space(1))) void*)(reinterpret_cast<uintptr_t>(ss[h] + at * SB) & ~(uintptr_t)3),
+                (__attribute__((address_space(3))) void*)(to + so[h]), 4, 0, 0);
+        }
     };
-    int64_t srow[NR];                                   // where a row's scales begin
+    // which half of its word a 16-bit scale is: the parity of its place
+    unsigned odd[NR];
 #pragma unroll
-    for (int r = 0; r < NR; ++r) srow[r] = std::min(i0 + wr * 16 * NR + 16 * r + lr, a.m - 1) * a.G;
-    unsigned sn[NR][4 / FL];
-    auto fetch = [&](int64_t kb) {                      // bits only: converting here would wait for the load
-        int64_t at[4 / FL];
-#pragma unroll
-        for (int t = 0; t < 4 / FL; ++t) at[t] = std::min(kb * 128 + t * 32 * FL, a.n - 1) >> a.gshift;
-#pragma unroll
-        for (int r = 0; r < NR; ++r)
-#pragma unroll
-            for (int t = 0; t < 4 / FL; ++t)
-                sn[r][t] = SB == 4 ? static_cast<const unsigned*>(a.scales)[srow[r] + at[t]]
-                                   : static_cast<const unsigned short*>(a.scales)[srow[r] + at[t]];
-    };
+    for (int r = 0; r < NR; ++r)
+        odd[r] = (unsigned)(std::min(i0 + wr * 16 * NR + 16 * r + lr, a.m - 1) * a.G) +
+                 (unsigned)(reinterpret_cast<uintptr_t>(a.scales) >> 1);
     const unsigned bf16_mask = a.sprec == PB16 ? ~0u : 0u;
-    if (k0 < k1) fetch(k0);
 #pragma unroll
     for (int d = 0; d < D - 1; ++d)
         if (k0 + d < k1) move(k0 + d, d);
@@ -853,14 +862,18 @@ __global__ __launch_bounds__(64 * WX * WR, 2) void k_q4_tile8(Q4Args a, int tile
         else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        float sc[NR][4 / FL];
-#pragma unroll
-        for (int r = 0; r < NR; ++r)
-#pragma unroll
-            for (int t = 0; t < 4 / FL; ++t) sc[r][t] = scale_of_bits<SB>(sn[r][t], bf16_mask);
-        if (kb + 1 < k1) fetch(kb + 1);
         if (kb + D - 1 < k1) move(kb + D - 1, buf == 0 ? D - 1 : buf - 1);
         const char* from = S + buf * C::BUF;
+        float sc[NR][PER];
+#pragma unroll
+        for (int t = 0; t < PER; ++t) {
+            const unsigned at = (unsigned)(std::min(kb * 128 + t * 32 * FL, a.n - 1) >> a.gshift);
+#pragma unroll
+            for (int r = 0; r < NR; ++r) {
+                const unsigned u = *reinterpret_cast<const unsigned*>(from + C::SB0 + (t * BM + wr * 16 * NR + 16 * r + lr) * 4);
+                sc[r][t] = scale_of_bits<SB>(SB == 4 ? u : (odd[r] + at) & 1 ? u >> 16 : u & 0xFFFFu, bf16_mask);
+            }
+        }
         int8v_t x[NX];
 #pragma unroll
         for (int f = 0; f < NX; ++f) {
@@ -877,8 +890,7 @@ __global__ __launch_bounds__(64 * WX * WR, 2) void k_q4_tile8(Q4Args a, int tile
             const int row = wr * 16 * NR + 16 * r + lr;
             const uint4v_t w = *reinterpret_cast<const uint4v_t*>(from + C::XB + row * 64 + (lg ^ (row >> 2 & 3)) * 16);
 #pragma unroll
-            for (int t = 0; t < 4 / FL; ++t) {
-                constexpr int PER = 4 / FL;
+            for (int t = 0; t < PER; ++t) {
                 const int n = r * PER + t, which = n & 1;
                 int8v_t wf = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
@@ -892,8 +904,8 @@ __global__ __launch_bounds__(64 * WX * WR, 2) void k_q4_tile8(Q4Args a, int tile
                 flush(pr, which ^ 1, n == 0 ? carry : sc[pr][pt]);
             }
         }
-        static_assert(NR * (4 / FL) % 2 == 0, "the step's last block lies in the second half of d");
-        carry = sc[NR - 1][4 / FL - 1];
+        static_assert(NR * PER % 2 == 0, "the step's last block lies in the second half of d");
+        carry = sc[NR - 1][PER - 1];
         buf = buf == D - 1 ? 0 : buf + 1;
     }
     flush(NR - 1, 1, carry);
@@ -1388,7 +1400,7 @@ void tile_t(const Q4Plan& p, const Q4Args& a, hipStream_t st) {
 
 template <int WX, int NX, int WR, int FL, int SB>
 void launch_tile8(const Q4Args& a, hipStream_t st) {
-    using C = Tile8Cfg<WX, NX, WR>;
+    using C = Tile8Cfg<WX, NX, WR, FL>;
     const int tm = (int)((a.m + C::BM - 1) / C::BM), tb = (int)((a.b + C::BT - 1) / C::BT);
     KernelTimer t("q4_tile8", st);
     hipLaunchKernelGGL((k_q4_tile8<WX, NX, WR, FL, SB>), dim3(xcd_grid((int64_t)tm * tb * a.splits)), dim3(64 * C::NW), 0, st, a,
