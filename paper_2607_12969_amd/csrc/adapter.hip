@@ -83,22 +83,6 @@ struct AdapterOuter {
     void* G;
 };
 
-// One 16-byte operand a lane: 32 K values of an instruction for 16-bit types, four
-// instructions of 4 K values for binary32.
-template <typename T> __device__ __forceinline__ float4_t mma16(const uint4v_t& a, const uint4v_t& b, float4_t c);
-template <> __device__ __forceinline__ float4_t mma16<half_t>(const uint4v_t& a, const uint4v_t& b, float4_t c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8_t, a), __builtin_bit_cast(half8_t, b), c, 0, 0, 0);
-}
-template <> __device__ __forceinline__ float4_t mma16<bhalf_t>(const uint4v_t& a, const uint4v_t& b, float4_t c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bhalf8_t, a), __builtin_bit_cast(bhalf8_t, b), c, 0, 0, 0);
-}
-template <> __device__ __forceinline__ float4_t mma16<float>(const uint4v_t& a, const uint4v_t& b, float4_t c) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-        c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[e]), __uint_as_float(b[e]), c, 0, 0, 0);
-    return c;
-}
-
 template <typename T> inline constexpr int kParts = sizeof(T) == 4 ? 1 : 2;     // 16-bit values that stand for one of H
 template <typename T> inline constexpr int kStep = 4 * kVec<T>;                 // K values of mma16
 
@@ -117,49 +101,6 @@ template <> __device__ __forceinline__ void split_value<half_t>(float x, unsigne
     p[0] = __builtin_bit_cast(unsigned short, h);
     p[1] = __builtin_bit_cast(unsigned short, (half_t)(__builtin_fabsf(lo) <= 3.4028234663852886e38f ? lo : 0.0f));
 }
-// The power of two that brings a largest magnitude (as bits) to [2^14, 2^15), where
-// binary16 pairs are to hold it; 1 for other types, zeros, infinities and NaN.
-template <typename T> __device__ __forceinline__ float range_scale(unsigned amax) {
-    if constexpr (!__is_same(T, half_t)) return 1.0f;
-    if (amax == 0 || amax >= 0x7F800000u) return 1.0f;
-    const int e = std::max((int)(amax >> 23), 1) - 127;          // floor(log2), subnormals as 2^-126
-    return __uint_as_float((unsigned)(std::min(14 - e, 126) + 127) << 23);
-}
-
-// The vector at column c of a row of L, zeros past the end.
-template <typename T> __device__ __forceinline__ uint4v_t load_zero16(const T* row, int64_t c, int64_t L) {
-    if (c + kVec<T> <= L) return load16(row + c);
-    uint4v_t v = {0, 0, 0, 0};
-#pragma unroll
-    for (int e = 0; e < kVec<T>; ++e)
-        if (c + e < L) {
-            unsigned b;
-            if constexpr (sizeof(T) == 4) b = __builtin_bit_cast(unsigned, row[c + e]);
-            else b = __builtin_bit_cast(unsigned short, row[c + e]);
-            set_bits<T>(v, e, b);
-        }
-    return v;
-}
-
-// The operand of this lane from a tile in LDS whose rows (pitch `pitch`, 8-byte aligned)
-// are the K axis: K values k0 + E (lane / 16) .., column c0 + lane % 16.  The transposing
-// read gives lane i of 16 column i of four rows.
-template <typename T> __device__ __forceinline__ uint4v_t turned(const T* tile, int pitch, int k0, int c0) {
-    const int lr = threadIdx.x & 15, lg = (threadIdx.x & 63) >> 4;
-    if constexpr (sizeof(T) == 4) {
-        uint4v_t x;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = __float_as_uint(tile[(k0 + 4 * lg + e) * pitch + c0 + lr]);
-        return x;
-    } else {
-        typedef short s4_t __attribute__((ext_vector_type(4)));
-        const T* p = tile + (k0 + 8 * lg + (lr >> 2)) * pitch + c0 + 4 * (lr & 3);
-        const s4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4_t*)(p));
-        const s4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4_t*)(p + 4 * pitch));
-        return __builtin_bit_cast(uint4v_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-    }
-}
-
 __device__ __forceinline__ bool named(int64_t id, int64_t count) { return (uint64_t)id < (uint64_t)count; }
 
 }  // namespace

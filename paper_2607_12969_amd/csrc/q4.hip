@@ -173,6 +173,9 @@ struct Q4Args {
     const void* U;
     const float* Tm;      // T' [batch][kp], kp = k rounded up to 16, zero past k; or tsplits
     int tsplits;          // partial sums [tsplits][batch][k] without the factor s
+    const half_t* T16;    // or T' as pairs of binary16 [2][batch][kp16], kp16 = k rounded up to 32, zero past k, ...
+    const float* tinv;    // ... each row times a power of two that tinv undoes
+    int64_t kp16;
     int64_t kp;
     const void* s;
     int64_t k;
@@ -739,6 +742,54 @@ __global__ __launch_bounds__(64 * WX * WR, (TileCfg<T, WX, NX, WR>::EU)) void k_
             }
 }
 
+// acc = T' U^T for binary16 U on the 16-bit matrix cores, T' as pairs (22 bits of the
+// largest of a row): 16 NR rows of W from `i0` on, 16 NX rows of X from `b0` on.  It comes before the
+// main loop, whose registers are free then, so that a step's operands are all loaded at once.
+// 8192 x 8192, 4096 rows, k = 65: 7 us of matrix instructions where binary32 ones take 34.
+template <int NR, int NX>
+__device__ __forceinline__ void ranks16(const Q4Args& a, int64_t i0, int64_t b0, float4_t (&acc)[NR][NX]) {
+    const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
+    const half_t* u[NR];
+#pragma unroll
+    for (int r = 0; r < NR; ++r) u[r] = static_cast<const half_t*>(a.U) + std::min(i0 + 16 * r + lr, a.m - 1) * a.k + 8 * lg;
+    const int64_t first = std::min(b0, a.b - 1);            // b0 may lie past the batch
+    unsigned at[NX];                                         // of a row's pairs, from row `first` on
+#pragma unroll
+    for (int f = 0; f < NX; ++f) at[f] = (unsigned)((std::min(b0 + 16 * f + lr, a.b - 1) - first) * a.kp16) + 8 * lg;
+    const half_t* t = a.T16 + first * a.kp16;
+#pragma unroll 1
+    for (int64_t q = 0; q < a.k; q += 32) {
+        half8_t w[NR], lo[NX], hi[NX];
+        if (q + 32 <= a.k) {
+#pragma unroll
+            for (int r = 0; r < NR; ++r) w[r] = __builtin_bit_cast(half8_t, load16(u[r] + q));
+        } else {
+#pragma unroll
+            for (int r = 0; r < NR; ++r) w[r] = __builtin_bit_cast(half8_t, load_zero16(u[r], q, a.k - 8 * lg));
+        }
+#pragma unroll
+        for (int f = 0; f < NX; ++f) {
+            hi[f] = *reinterpret_cast<const half8_t*>(t + q + at[f]);
+            lo[f] = *reinterpret_cast<const half8_t*>(t + a.b * a.kp16 + q + at[f]);
+        }
+#pragma unroll
+        for (int f = 0; f < NX; ++f)
+#pragma unroll
+            for (int r = 0; r < NR; ++r) {
+                acc[r][f] = mfma(lo[f], w[r], acc[r][f]);
+                acc[r][f] = mfma(hi[f], w[r], acc[r][f]);
+            }
+    }
+#pragma unroll
+    for (int f = 0; f < NX; ++f)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            const float inv = a.tinv[std::min(b0 + 16 * f + 4 * lg + v, a.b - 1)];
+#pragma unroll
+            for (int r = 0; r < NR; ++r) acc[r][f][v] *= inv;
+        }
+}
+
 // ---- many rows of e4m3 activations: tiles on the scaled matrix instructions ------
 // v_mfma_f32_16x16x128_f8f6f4 takes e4m3 and E2M1 operands as they are stored, 128 columns
 // at twice the 16-bit rate, so nothing is widened and a step of 128 columns is one
@@ -764,6 +815,55 @@ template <int WX, int NX, int WR, int FL> struct Tile8Cfg {
 
 typedef int int8v_t __attribute__((ext_vector_type(8)));
 
+// Results of a wave (16 NR rows of W from i0, 16 NX rows of X from b0), scaled and stored, TR rows of X
+// at a time through `out` (LDS of the wave), so that a store covers whole pieces of rows.
+template <int NR, int NX, int TR>
+__device__ __forceinline__ void store_tile8(const Q4Args& a, float* out, int64_t split, int64_t i0, int64_t b0,
+                                            const float4_t (&acc)[NR][NX]) {
+    constexpr int OP = 16 * NR + 4, FB = TR / 16, LANES = 16 * NR / 4, ROWS = 64 / LANES;     // lanes of a row, 4 values each
+    const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4, c4 = lane % LANES * 4, r0 = lane / LANES;
+#pragma unroll
+    for (int f0 = 0; f0 < NX; f0 += FB) {
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int f = 0; f < FB; ++f)
+#pragma unroll
+            for (int r = 0; r < NR; ++r)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) out[(16 * f + 4 * lg + v) * OP + 16 * r + lr] = acc[r][f0 + f][v];
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int t = 0; t < TR; t += ROWS) {
+            const int64_t b = b0 + 16 * f0 + t + r0, i = i0 + c4;
+            float4_t y = *reinterpret_cast<const float4_t*>(out + (t + r0) * OP + c4);
+            if (b >= a.b || i >= a.m) continue;
+            if (a.part) {
+                float* p = a.part + (split * a.b + b) * a.m + i;
+                if (i + 4 <= a.m) __builtin_memcpy(p, &y, 16);
+                else
+                    for (int e = 0; e < 4; ++e)
+                        if (i + e < a.m) p[e] = y[e];
+                continue;
+            }
+            const float s = a.xscale[b];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] *= s;
+            const int64_t at = b * a.ldy + i;
+            if (i + 4 > a.m) {
+                for (int e = 0; e < 4; ++e)
+                    if (i + e < a.m) store_from_f32(a.Y, at + e, a.yprec, y[e]);
+            } else if (a.yprec == P32) {
+                __builtin_memcpy(static_cast<float*>(a.Y) + at, &y, 16);
+            } else {
+                const uint2v_t h = a.yprec == P16 ? uint2v_t{pack2<half_t>(y[0], y[1]), pack2<half_t>(y[2], y[3])}
+                                                  : uint2v_t{pack2<bhalf_t>(y[0], y[1]), pack2<bhalf_t>(y[2], y[3])};
+                __builtin_memcpy(static_cast<unsigned short*>(a.Y) + at, &h, 8);
+            }
+        }
+    }
+}
+
+
 template <int WX, int NX, int WR, int FL, int SB>
 __global__ __launch_bounds__(64 * WX * WR, 2) void k_q4_tile8(Q4Args a, int tiles_m, int tiles_b) {
     using C = Tile8Cfg<WX, NX, WR, FL>;
@@ -784,6 +884,7 @@ __global__ __launch_bounds__(64 * WX * WR, 2) void k_q4_tile8(Q4Args a, int tile
     for (int r = 0; r < NR; ++r)
 #pragma unroll
         for (int f = 0; f < NX; ++f) acc[r][f] = zero_accv<float4_t>();
+    if (split == 0 && a.T16) ranks16<NR, NX>(a, i0 + wr * 16 * NR, b0 + wx * 16 * NX, acc);
     const int64_t blocks = (a.n + 127) / 128;
     const int64_t k0 = blocks * split / a.splits, k1 = blocks * (split + 1) / a.splits;
     // a wave moves 8 rows of X a load and 16 rows of codes; where a step has fewer loads than
@@ -909,7 +1010,7 @@ __global__ __launch_bounds__(64 * WX * WR, 2) void k_q4_tile8(Q4Args a, int tile
         buf = buf == D - 1 ? 0 : buf + 1;
     }
     flush(NR - 1, 1, carry);
-    if (split == 0 && a.k) {
+    if (split == 0 && a.k && !a.T16) {
         int64_t row[NR];
         const float* tm[NX];
 #pragma unroll
@@ -919,48 +1020,160 @@ __global__ __launch_bounds__(64 * WX * WR, 2) void k_q4_tile8(Q4Args a, int tile
         add_ranks(a, tm, row, 0, 16, acc);
     }
     __syncthreads();
-    float* out = reinterpret_cast<float*>(S) + wave * C::TR * C::OP;
-    constexpr int FB = C::TR / 16, LANES = 16 * NR / 4, ROWS = 64 / LANES;        // lanes of a row, 4 values each
-    const int c4 = lane % LANES * 4, r0 = lane / LANES;
+    store_tile8<NR, NX, C::TR>(a, reinterpret_cast<float*>(S) + wave * C::TR * C::OP, split, i0 + wr * 16 * NR,
+                               b0 + wx * 16 * NX, acc);
+}
+
+// The same for large products in groups of 128 columns and more: 256 x 256 results on 2 x 4
+// waves of 128 rows of X and 64 of W, which read 20 KB of LDS a step for 32 matrix
+// instructions (the smaller tile 12 KB for 16).  Three buffers: a step begins when it and the next
+// one have landed, so that operands are read two blocks ahead across the steps, and a block's
+// products join acc three instructions later.
+struct Wide8 {
+    static constexpr int NR = 4, NX = 8, BM = 256, BT = 256, XB = BT * 128, SB0 = XB + BM * 64, BUF = SB0 + BM * 4;
+    static constexpr int XL = 4, WL = 2, TR = 32;
+};
+template <int SB>
+__global__ __launch_bounds__(512, 2) void k_q4_wide8(Q4Args a, int tiles_m, int tiles_b) {
+    using C = Wide8;
+    constexpr int NR = C::NR, NX = C::NX;
+    __shared__ alignas(16) char S[3 * C::BUF];
+    const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wx = wave & 1, wr = wave >> 1;
+    const int64_t lt = xcd_tile((int64_t)tiles_m * tiles_b);
+    if (lt >= (int64_t)tiles_m * tiles_b) return;
+    const int64_t g = lt / (8 * tiles_b), gs = std::min<int64_t>(8, tiles_m - 8 * g), in = lt - g * 8 * tiles_b;
+    const int64_t i0 = (8 * g + in % gs) * C::BM, b0 = in / gs * C::BT;
+    float4_t acc[NR][NX];
 #pragma unroll
-    for (int f0 = 0; f0 < NX; f0 += FB) {
-        __builtin_amdgcn_wave_barrier();
+    for (int r = 0; r < NR; ++r)
 #pragma unroll
-        for (int f = 0; f < FB; ++f)
+        for (int f = 0; f < NX; ++f) acc[r][f] = zero_accv<float4_t>();
+    // the compensation first, while the loop's registers are free
+    if (a.T16) {
+        ranks16<NR, NX>(a, i0 + wr * 16 * NR, b0 + wx * 16 * NX, acc);
+    } else if (a.k) {
+        int64_t row[NR];
+        const float* tm[NX];
 #pragma unroll
-            for (int r = 0; r < NR; ++r)
+        for (int r = 0; r < NR; ++r) row[r] = std::min(i0 + wr * 16 * NR + 16 * r + lr, a.m - 1);
 #pragma unroll
-                for (int v = 0; v < 4; ++v) out[(16 * f + 4 * lg + v) * C::OP + 16 * r + lr] = acc[r][f0 + f][v];
-        __builtin_amdgcn_wave_barrier();
+        for (int f = 0; f < NX; ++f) tm[f] = a.Tm + std::min(b0 + wx * 16 * NX + 16 * f + lr, a.b - 1) * a.kp;
+        add_ranks(a, tm, row, 0, 16, acc);
+    }
+    const int64_t steps = (a.n + 127) / 128;
+    const char* xs[C::XL];
 #pragma unroll
-        for (int t = 0; t < C::TR; t += ROWS) {
-            const int64_t b = b0 + wx * 16 * NX + 16 * f0 + t + r0, i = i0 + wr * 16 * NR + c4;
-            float4_t y = *reinterpret_cast<const float4_t*>(out + (t + r0) * C::OP + c4);
-            if (b >= a.b || i >= a.m) continue;
-            if (a.part) {
-                float* p = a.part + (split * a.b + b) * a.m + i;
-                if (i + 4 <= a.m) __builtin_memcpy(p, &y, 16);
-                else
-                    for (int e = 0; e < 4; ++e)
-                        if (i + e < a.m) p[e] = y[e];
-                continue;
-            }
-            const float s = a.xscale[b];
+    for (int h = 0; h < C::XL; ++h) {
+        const int r = (wave * C::XL + h) * 8 + (lane >> 3);
+        xs[h] = static_cast<const char*>(a.X) + std::min(b0 + r, a.b - 1) * a.ldx + ((lane & 7) ^ (r >> 1 & 7)) * 16;
+    }
+    const unsigned char* cs[C::WL];
+    int cc[C::WL];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] *= s;
-            const int64_t at = b * a.ldy + i;
-            if (i + 4 > a.m) {
-                for (int e = 0; e < 4; ++e)
-                    if (i + e < a.m) store_from_f32(a.Y, at + e, a.yprec, y[e]);
-            } else if (a.yprec == P32) {
-                __builtin_memcpy(static_cast<float*>(a.Y) + at, &y, 16);
-            } else {
-                const uint2v_t h = a.yprec == P16 ? uint2v_t{pack2<half_t>(y[0], y[1]), pack2<half_t>(y[2], y[3])}
-                                                  : uint2v_t{pack2<bhalf_t>(y[0], y[1]), pack2<bhalf_t>(y[2], y[3])};
-                __builtin_memcpy(static_cast<unsigned short*>(a.Y) + at, &h, 8);
+    for (int h = 0; h < C::WL; ++h) {
+        const int r = (wave * C::WL + h) * 16 + (lane >> 2);
+        cs[h] = a.codes + std::min(i0 + r, a.m - 1) * a.rb;
+        cc[h] = ((lane & 3) ^ (r >> 2 & 3)) * 16;
+    }
+    const int sl = wave & 3;                                 // waves 4 .. 7 repeat the loads of 0 .. 3
+    const char* ss = static_cast<const char*>(a.scales) + std::min(i0 + sl * 64 + lane, a.m - 1) * a.G * SB;
+    auto move = [&](int64_t kb, int buf) {
+        char* to = S + buf * C::BUF;
+#pragma unroll
+        for (int h = 0; h < C::XL; ++h)
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(xs[h] + kb * 128),
+                                             (__attribute__((address_space(3))) void*)(to + (wave * C::XL + h) * 1024), 16, 0, 0);
+#pragma unroll
+        for (int h = 0; h < C::WL; ++h)
+            __builtin_amdgcn_global_load_lds(
+                (const __attribute__((address_space(1))) void*)(cs[h] + std::min(kb * 64 + cc[h], a.rb - 16)),
+                (__attribute__((address_space(3))) void*)(to + C::XB + (wave * C::WL + h) * 1024), 16, 0, 0);
+        const int64_t at = kb * 128 >> a.gshift;
+        __builtin_amdgcn_global_load_lds(
+            (const __attribute__((address_space(1))) void*)(reinterpret_cast<uintptr_t>(ss + at * SB) & ~(uintptr_t)3),
+            (__attribute__((address_space(3))) void*)(to + C::SB0 + sl * 256), 4, 0, 0);
+    };
+    unsigned odd[NR];
+#pragma unroll
+    for (int r = 0; r < NR; ++r)
+        odd[r] = (unsigned)(std::min(i0 + wr * 16 * NR + 16 * r + lr, a.m - 1) * a.G) +
+                 (unsigned)(reinterpret_cast<uintptr_t>(a.scales) >> 1);
+    const unsigned bf16_mask = a.sprec == PB16 ? ~0u : 0u;
+    uint4v_t xr[4][2], w[NR], wn[NR];
+    unsigned sw[NR], swn[NR];
+    // where this lane's operands lie in a buffer: 16 rows on, the swizzle is the same
+    const int xrow = (wx * 16 * NX + lr) * 128, xc0 = (lg ^ (lr >> 1 & 7)) * 16, xc1 = ((lg + 4) ^ (lr >> 1 & 7)) * 16;
+    const int wrow = C::XB + (wr * 16 * NR + lr) * 64 + (lg ^ (lr >> 2 & 3)) * 16, srow = C::SB0 + (wr * 16 * NR + lr) * 4;
+    auto read_x = [&](const char* from, int f, uint4v_t (&x)[2]) {
+        x[0] = *reinterpret_cast<const uint4v_t*>(from + xrow + f * 2048 + xc0);
+        x[1] = *reinterpret_cast<const uint4v_t*>(from + xrow + f * 2048 + xc1);
+    };
+    auto read_w = [&](const char* from, uint4v_t (&to)[NR], unsigned (&sc)[NR]) {
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+            to[r] = *reinterpret_cast<const uint4v_t*>(from + wrow + r * 1024);
+            sc[r] = *reinterpret_cast<const unsigned*>(from + srow + r * 64);
+        }
+    };
+    auto landed = [] {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    move(0, 0);
+    if (steps > 1) move(1, 1);
+    landed();
+    read_w(S, w, sw);
+    read_x(S, 0, xr[0]);
+    read_x(S, 1, xr[1]);
+    int buf = 0;
+    for (int64_t kb = 0; kb < steps; ++kb) {
+        const int next = buf == 2 ? 0 : buf + 1, last = next == 2 ? 0 : next + 1;
+        if (kb) landed();                                   // this step and the next one are there
+        if (kb + 2 < steps) move(kb + 2, last);
+        const char* from = S + buf * C::BUF;
+        const char* then = S + next * C::BUF;               // past the end: read, not used
+        const unsigned at = (unsigned)(kb * 128 >> a.gshift);
+        float sc[NR];
+#pragma unroll
+        for (int r = 0; r < NR; ++r)
+            sc[r] = scale_of_bits<SB>(SB == 4 ? sw[r] : (odd[r] + at) & 1 ? sw[r] >> 16 : sw[r] & 0xFFFFu, bf16_mask);
+        float4_t d[4];
+        auto join = [&](int i) {                            // block i = 4 f + r
+#pragma unroll
+            for (int v = 0; v < 4; ++v) acc[i & 3][i >> 2][v] += sc[i & 3] * d[i & 3][v];
+        };
+#pragma unroll
+        for (int f = 0; f < NX; ++f) {
+            if (f + 2 < NX) read_x(from, f + 2, xr[(f + 2) & 3]);
+            else read_x(then, f + 2 - NX, xr[(f + 2) & 3]);
+            if (f == NX - 3) read_w(then, wn, swn);
+            int8v_t x;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = (int)xr[f & 3][e >> 2][e & 3];
+#pragma unroll
+            for (int r = 0; r < NR; ++r) {
+                const int i = 4 * f + r;
+                if (i >= 3) join(i - 3);
+                int8v_t wf = {(int)w[r][0], (int)w[r][1], (int)w[r][2], (int)w[r][3], 0, 0, 0, 0};
+                d[r] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, wf, zero_accv<float4_t>(), 0, 4, 0, 0x7F7F7F7F, 0,
+                                                                        0x7F7F7F7F);
             }
         }
+#pragma unroll
+        for (int i = 4 * NX - 3; i < 4 * NX; ++i) join(i);
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+            w[r] = wn[r];
+            sw[r] = swn[r];
+        }
+        buf = next;
     }
+    __syncthreads();
+    store_tile8<NR, NX, C::TR>(a, reinterpret_cast<float*>(S) + wave * C::TR * (16 * NR + 4), 0, i0 + wr * 16 * NR,
+                               b0 + wx * 16 * NX, acc);
 }
 
 // Y = the sum of the splits, in their order.
@@ -1261,6 +1474,145 @@ __global__ __launch_bounds__(256) void k_q4_mid16(const T* __restrict__ X, int64
     }
 }
 
+// The same for batches of 64 rows and more of e4m3 activations and binary16 factors: 64 rows
+// and 16 F ranks a workgroup, steps of 128 columns through registers to one of two LDS
+// buffers, two ahead.  V lies in LDS as it does in memory, its operands come by the transposing
+// read; activations are widened as operands.  k >= 8.
+template <int F>
+__global__ __launch_bounds__(256, 2) void k_q4_mid8(const unsigned char* __restrict__ X, int64_t ldx, const half_t* __restrict__ V,
+                                                    int64_t n, int64_t k, int64_t b, int64_t chunk, float* __restrict__ part) {
+    constexpr int VP = 16 * F + 8, RC = 2 * F, ST = 2;                            // pitch and vectors of a row of V
+    __shared__ alignas(16) unsigned char sx[2][64 * 128];
+    __shared__ alignas(16) half_t sv[2][128 * VP];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, lr = lane & 15, lg = lane >> 4;
+    const int64_t r0 = (int64_t)blockIdx.x * 16 * F, s = blockIdx.y, b0 = (int64_t)blockIdx.z * 64;
+    const int64_t j0 = s * chunk, j1 = std::min(n, j0 + chunk);
+    // vector h of this thread: row r of the step, ranks r0 + 8 c on, or the last 8 ranks where
+    // these pass k (k >= 8): they overlap the vector before and are written one by one
+    const half_t* vp[F];
+    int to[F];                                               // place in LDS
+    unsigned whole = 0, tail = 0;
+    const int last = (int)(k - 8 - r0);                      // of the last 8 ranks, in the row
+#pragma unroll
+    for (int h = 0; h < F; ++h) {
+        const int at = tid + 256 * h, r = at / RC, c = at % RC;
+        const bool fits = r0 + 8 * c <= k - 8;
+        vp[h] = V + (j0 + r) * k + (fits ? r0 + 8 * c : k - 8);
+        to[h] = r * VP + (fits ? 8 * c : 0);
+        whole |= (unsigned)fits << h;
+        tail |= (unsigned)(!fits && r0 + 8 * c < k) << h;
+    }
+    const unsigned char* xp[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) xp[h] = X + std::min(b0 + (tid >> 3) + 32 * h, b - 1) * ldx + (tid & 7) * 16;
+    uint4v_t xv[ST][2], vv[ST][F];
+    auto load = [&](int64_t j, uint4v_t (&x)[2], uint4v_t (&v)[F]) {
+        if (j + 128 <= j1) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) x[h] = load16(xp[h] + j);
+#pragma unroll
+            for (int h = 0; h < F; ++h) v[h] = load16(vp[h] + (j - j0) * k);
+            return;
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            x[h] = uint4v_t{0, 0, 0, 0};
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                if (j + (tid & 7) * 16 + e < j1) x[h][e >> 2] |= (unsigned)xp[h][j + e] << (8 * (e & 3));
+        }
+#pragma unroll
+        for (int h = 0; h < F; ++h) {
+            v[h] = uint4v_t{0, 0, 0, 0};
+            if (j + (tid + 256 * h) / RC < j1) v[h] = load16(vp[h] + (j - j0) * k);
+        }
+    };
+    auto put = [&](int buf, const uint4v_t (&x)[2], const uint4v_t (&v)[F]) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int r = (tid >> 3) + 32 * h;
+            *reinterpret_cast<uint4v_t*>(&sx[buf][r * 128 + ((tid & 7) ^ (r >> 1 & 7)) * 16]) = x[h];
+        }
+#pragma unroll
+        for (int h = 0; h < F; ++h) {
+            if (whole >> h & 1) {
+                *reinterpret_cast<uint4v_t*>(&sv[buf][to[h]]) = v[h];
+            } else if (tail >> h & 1) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (last + e >= 0)
+                        sv[buf][to[h] + last + e] = __builtin_bit_cast(half_t, (unsigned short)(v[h][e >> 1] >> (16 * (e & 1))));
+            }
+        }
+    };
+    float4_t acc[F];
+#pragma unroll
+    for (int f = 0; f < F; ++f) acc[f] = zero_accv<float4_t>();
+    auto step = [&](int64_t j, int buf, uint4v_t (&x)[2], uint4v_t (&v)[F], const uint4v_t (&xn)[2], const uint4v_t (&vn)[F]) {
+        if (j + 128 * ST < j1) load(j + 128 * ST, x, v);
+        const int row = 16 * wave + lr;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            // 8 of a row's bytes: half of chunk 2 q + lg / 2
+            const uint2v_t raw = *reinterpret_cast<const uint2v_t*>(
+                &sx[buf][row * 128 + ((2 * q + (lg >> 1)) ^ (row >> 1 & 7)) * 16 + (lg & 1) * 8]);
+            const half8_t xa = widen_e4m3(raw);
+#pragma unroll
+            for (int f = 0; f < F; ++f)
+                acc[f] = mfma(xa, __builtin_bit_cast(half8_t, turned<half_t>(sv[buf], VP, 32 * q, 16 * f)), acc[f]);
+        }
+        if (j + 128 < j1) put(buf ^ 1, xn, vn);
+        __syncthreads();
+    };
+    if (j0 < j1) {
+        load(j0, xv[0], vv[0]);
+        if (j0 + 128 < j1) load(j0 + 128, xv[1], vv[1]);
+        put(0, xv[0], vv[0]);
+    }
+    __syncthreads();
+    for (int64_t j = j0; j < j1; j += 256) {
+        step(j, 0, xv[0], vv[0], xv[1], vv[1]);
+        if (j + 128 < j1) step(j + 128, 1, xv[1], vv[1], xv[0], vv[0]);
+    }
+#pragma unroll
+    for (int f = 0; f < F; ++f)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            const int64_t bb = b0 + 16 * wave + 4 * lg + v, r = r0 + 16 * f + lr;
+            if (bb < b && r < k) part[(s * b + bb) * k + r] = acc[f][v];
+        }
+}
+
+// T' as pairs of binary16 (Q4Args): a wave for each row, whose largest value sets the range.
+__global__ __launch_bounds__(256) void k_q4_mid_pairs(const float* __restrict__ part, int splits, const half_t* __restrict__ s,
+                                                      int64_t k, int64_t kp, int64_t b, half_t* __restrict__ T16,
+                                                      float* __restrict__ tinv) {
+    const int lane = threadIdx.x & 63;
+    const int64_t step = (int64_t)gridDim.x * 4;
+    for (int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); t < b; t += step) {
+        auto value = [&](int64_t r) { return sum_splits(part + t * k + r, splits, b * k) * (float)s[r]; };
+        float held[2];                                       // of up to 128 ranks; more are summed twice
+        unsigned amax = 0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            held[h] = lane + 64 * h < k ? value(lane + 64 * h) : 0.0f;
+            amax = std::max(amax, __float_as_uint(held[h]) & 0x7FFFFFFFu);
+        }
+        for (int64_t r = lane + 128; r < k; r += 64) amax = std::max(amax, __float_as_uint(value(r)) & 0x7FFFFFFFu);
+#pragma unroll
+        for (int off = 32; off >= 1; off >>= 1) amax = std::max(amax, (unsigned)__shfl_xor((int)amax, off, 64));
+        const float sc = range_scale<half_t>(amax);
+        if (lane == 0) tinv[t] = 1.0f / sc;
+        for (int64_t r = lane; r < kp; r += 64) {
+            const float x = (r < 64 ? held[0] : r < 128 ? held[1] : r < k ? value(r) : 0.0f) * sc;
+            const half_t hi = (half_t)x;
+            const float lo = x - (float)hi;
+            T16[t * kp + r] = hi;
+            T16[(b + t) * kp + r] = (half_t)(__builtin_fabsf(lo) <= 3.4028234663852886e38f ? lo : 0.0f);
+        }
+    }
+}
+
 // T'[b][r] = s_r times the sum of the partials, in split order; rows of kp, zero
 // past k.
 __global__ __launch_bounds__(256) void k_q4_mid_finish(const float* __restrict__ part, int splits,
@@ -1291,7 +1643,8 @@ struct Q4Plan {
     size_t lds;
     int mid_splits, mid_tw;
     int64_t mid_chunk;
-    bool mid_finish;      // T' finished by a kernel of its own
+    bool mid_finish;      // T' finished by a kernel of its own ...
+    bool pairs;           // ... as pairs of binary16
     size_t tm, mid_part, planes, part;
 };
 
@@ -1346,7 +1699,9 @@ Q4Plan plan_q4(const Q4Weights& w, const void* X, int64_t ldx, int64_t b, int pr
         p.mid_splits = (int)((w.n + p.mid_chunk - 1) / p.mid_chunk);
         p.mid_finish = p.tile || b * p.mid_splits > 64 || b * kp > kRowsTm;
         p.mid_part = (size_t)p.mid_splits * b * w.k * 4;
-        if (p.mid_finish) p.tm = (size_t)b * kp * 4;
+        p.pairs = prec == PE4M3 && p.tile && w.fprec == P16;
+        if (p.pairs) p.tm = (size_t)round_up(b * 4, 256) + (size_t)2 * b * round_up(w.k, 32) * 2;
+        else if (p.mid_finish) p.tm = (size_t)b * kp * 4;
     }
     return p;
 }
@@ -1414,8 +1769,18 @@ void tile8_sb(const Q4Plan& p, const Q4Args& a, hipStream_t st) {
     if (p.nx == 2) return launch_tile8<1, 2, 4, FL, SB>(a, st);
     launch_tile8<1, 4, 4, FL, SB>(a, st);
 }
+// Large products: at least a workgroup of the wide tile for every compute unit.
+bool wide8_takes(const Q4Args& a) { return a.gshift >= 7 && a.b > 128 && ((a.m + 255) / 256) * ((a.b + 255) / 256) >= 256; }
 template <int FL>
 void tile8_t(const Q4Plan& p, const Q4Args& a, hipStream_t st) {
+    if constexpr (FL == 4)
+        if (p.splits == 1 && wide8_takes(a)) {
+            const int tm = (int)((a.m + 255) / 256), tb = (int)((a.b + 255) / 256);
+            KernelTimer t("q4_wide8", st);
+            hipLaunchKernelGGL(a.sprec == P32 ? k_q4_wide8<4> : k_q4_wide8<2>, dim3(xcd_grid((int64_t)tm * tb)), dim3(512), 0, st,
+                               a, tm, tb);
+            return;
+        }
     if (a.sprec == P32) tile8_sb<FL, 4>(p, a, st);
     else tile8_sb<FL, 2>(p, a, st);
 }
@@ -1444,6 +1809,15 @@ void mid_f(const Q4Plan& p, const Q4Weights& w, const Q4Args& a, float* part, hi
     hipLaunchKernelGGL(kern, grid, dim3(256), lds, st, x, a.ldx, w.V, w.fprec, w.n, w.k, a.b, p.mid_chunk, part);
 }
 
+void mid8(const Q4Plan& p, const Q4Weights& w, const Q4Args& a, float* part, hipStream_t st) {
+    KernelTimer t("q4_mid", st);
+    const int f = w.k <= 32 ? 2 : w.k <= 80 ? 5 : 8;
+    auto* kern = f == 2 ? k_q4_mid8<2> : f == 5 ? k_q4_mid8<5> : k_q4_mid8<8>;
+    hipLaunchKernelGGL(kern, dim3((unsigned)((w.k + 16 * f - 1) / (16 * f)), p.mid_splits, (unsigned)((a.b + 63) / 64)), dim3(256), 0,
+                       st, static_cast<const unsigned char*>(a.X), a.ldx, static_cast<const half_t*>(w.V), w.n, w.k, a.b, p.mid_chunk,
+                       part);
+}
+
 template <typename T>
 hipError_t apply_t(const Q4Weights& w, Q4Args& a, int prec, Workspace& ws, hipStream_t st) {
     const Q4Plan p = plan_q4(w, a.X, a.ldx, a.b, prec);
@@ -1453,10 +1827,21 @@ hipError_t apply_t(const Q4Weights& w, Q4Args& a, int prec, Workspace& ws, hipSt
     a.part = static_cast<float*>(ws.take(p.part));
     if (ws.overrun) return hipErrorOutOfMemory;
     if (w.k) {
-        if (w.k <= 32) mid_f<T, 2>(p, w, a, mid, st);
+        if (p.pairs && p.mid_tw == 4 && w.k >= 8) mid8(p, w, a, mid, st);
+        else if (w.k <= 32) mid_f<T, 2>(p, w, a, mid, st);
         else if (w.k <= 80) mid_f<T, 5>(p, w, a, mid, st);
         else mid_f<T, 8>(p, w, a, mid, st);
-        if (p.mid_finish) {
+        if (p.pairs) {
+            KernelTimer t("q4_mid_finish", st);
+            float* inv = Tm;
+            half_t* pairs = reinterpret_cast<half_t*>(reinterpret_cast<char*>(Tm) + round_up(a.b * 4, 256));
+            const int64_t kp = round_up(w.k, 32);
+            hipLaunchKernelGGL(k_q4_mid_pairs, dim3((unsigned)std::min<int64_t>((a.b + 3) / 4, 65536)), dim3(256), 0, st, mid,
+                               p.mid_splits, static_cast<const half_t*>(w.s), w.k, kp, a.b, pairs, inv);
+            a.T16 = pairs;
+            a.tinv = inv;
+            a.kp16 = kp;
+        } else if (p.mid_finish) {
             KernelTimer t("q4_mid_finish", st);
             hipLaunchKernelGGL(k_q4_mid_finish, dim3(strided_grid(a.b * a.kp)), dim3(256), 0, st, mid,
                                p.mid_splits, w.s, w.fprec, w.k, a.kp, a.b, Tm);

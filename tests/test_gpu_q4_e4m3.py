@@ -114,3 +114,30 @@ def test_every_code_and_what_is_not_finite(lrc, b):
     t[-1] = float("nan")
     got = lrc.q4_apply(codes, scales, X.view(torch.float8_e4m3fn), 128, x_scales=t)
     assert got.dtype == torch.bfloat16 and torch.isnan(got[-1]).all()
+
+
+@pytest.mark.parametrize("m,n,k,group,b", [(4100, 640, 65, 128, 4097), (8192, 130, 0, 256, 2000), (4352, 1000, 9, 512, 3850)])
+@pytest.mark.parametrize("sdt", ["fp32", "fp16", "bf16"])
+def test_large_tiles(lrc, m, n, k, group, b, sdt):
+    """Products of a tile for every compute unit: sampled rows and columns, and the rest against them twice."""
+    rng = np.random.default_rng([m, n, b])
+    codes = torch.randint(0, 256, (m, (n + 31) // 32 * 16), dtype=torch.uint8, device="cuda", generator=torch.Generator("cuda").manual_seed(n))
+    nib = torch.stack((codes & 15, codes >> 4), 2).view(m, -1)
+    nib[:, n:] = 0
+    codes = nib[:, 0::2] | (nib[:, 1::2] << 4)
+    scales = (torch.rand(m, -(-n // group), device="cuda") * 0.04 + 0.01).to(DT[sdt])
+    X = (torch.randn(b, n, device="cuda") * 50).clamp(-440, 440).to(torch.float8_e4m3fn)
+    t = torch.rand(b, device="cuda") * 0.01
+    F = tuple((torch.randn(*s, device="cuda") * n ** -0.5).half() for s in ((m, k), (k,), (n, k))) if k else None
+    got = lrc.q4_apply(codes, scales, X, group, F, out_dtype=torch.float32, x_scales=t)
+    rows = np.unique(np.concatenate([rng.integers(0, b, 60), [0, 255, 256, b - 1]]))
+    cols = np.unique(np.concatenate([rng.integers(0, m, 60), [0, 63, 64, 255, 256, m - 1]]))
+    W = H.weights(nib[:, :n].cpu().numpy()[cols].astype(int), scales.double().cpu().numpy()[cols], group)
+    Fs = None if F is None else (F[0][torch.from_numpy(cols).cuda()], F[1], F[2])
+    ri = torch.from_numpy(rows).cuda()
+    check(got[ri][:, torch.from_numpy(cols).cuda()], W, X.view(torch.uint8)[ri].view(torch.float8_e4m3fn), t[ri], Fs, "fp32")
+    # every other value: halves of the batch, which take other tiles
+    for part in (slice(0, b // 8), slice(b // 8, b // 3)):
+        small = lrc.q4_apply(codes, scales, X[part], group, F, out_dtype=torch.float32, x_scales=t[part])
+        size = got[part].abs().mean()
+        assert (small - got[part]).abs().max() <= 1e-4 * size * 10
