@@ -214,13 +214,15 @@ __global__ __launch_bounds__(NT) void k_rms_norm(NormArgs a, int64_t row0) {
 }
 
 // A workgroup takes the rows g, g + G, .. and adds up their part of dw, each thread
-// for the columns that are its own: part[g][n].  NV = 0: rows of any length, read
-// twice, and dw through the partial sums in memory.
+// for the columns that are its own: part[g][n].  NV <= 2: the next row is on its way
+// while this one is reduced, and the weights stay in registers.  NV = 0: rows of any
+// length, read twice, and dw through the partial sums in memory.
 template <typename T, int NV, int NT>
-__global__ __launch_bounds__(NT) void k_rms_norm_backward(NormGradArgs a, float* __restrict__ part) {
+__global__ __launch_bounds__(NT, 4) void k_rms_norm_backward(NormGradArgs a, float* __restrict__ part) {
     constexpr int E = kVec<T>, H = NV > 0 ? NV : 1;
+    constexpr bool kAhead = NV == 1 || NV == 2;
     __shared__ float red[2][NT / 64];
-    const int t = threadIdx.x;
+    const int t = threadIdx.x, nt = blockDim.x;             // whole waves, at most NT
     const int64_t full = a.n / E, tail = full * E + t;
     const bool has_tail = tail < a.n;
     float dw[H][E], dwlast = 0.0f;
@@ -230,18 +232,78 @@ __global__ __launch_bounds__(NT) void k_rms_norm_backward(NormGradArgs a, float*
         for (int e = 0; e < E; ++e) dw[i][e] = 0.0f;
     float* mine = part ? part + (int64_t)blockIdx.x * a.n : nullptr;
     const float wlast = has_tail ? load_weight(a.weight, a.wprec, tail) : 0.0f;
+    float wv[H][E];
+    if constexpr (kAhead) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) wv[i][e] = 0.0f;
+            const int64_t q = t + (int64_t)i * nt;
+            if (q < full) load_weights<E>(a.weight, a.wprec, q * E, wv[i]);
+        }
+    }
+    uint4v_t vd[H], vh[H], vs[H], nd[H], nh[H];
+    float rstd = 0.0f, nrstd = 0.0f;
+    T td{}, th{}, ts{}, ntd{}, nth{};                       // the tail's element
+    auto fetch = [&](int64_t r, uint4v_t (&d)[H], uint4v_t (&x)[H], float& rs, T& dl, T& xl) {
+        const T* dy = static_cast<const T*>(a.dy) + r * a.lddy;
+        const T* h = static_cast<const T*>(a.h) + r * a.ldh;
+        rs = a.rstd[r];
+        if (has_tail) {
+            dl = dy[tail];
+            xl = h[tail];
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int64_t q = t + (int64_t)i * nt;
+            d[i] = x[i] = uint4v_t{0, 0, 0, 0};
+            if (q < full) {
+                d[i] = load16_once(dy + q * E);
+                x[i] = load16_once(h + q * E);
+            }
+        }
+    };
     int parity = 0;
+    if constexpr (kAhead)
+        if ((int64_t)blockIdx.x < a.rows) fetch(blockIdx.x, nd, nh, nrstd, ntd, nth);
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x, parity ^= 1) {
         const T* dy = static_cast<const T*>(a.dy) + r * a.lddy;
         const T* h = static_cast<const T*>(a.h) + r * a.ldh;
         const T* ds = a.dsum ? static_cast<const T*>(a.dsum) + r * a.ldd : nullptr;
         T* dx = static_cast<T*>(a.dx) + r * a.ldx;
-        const float rstd = a.rstd[r];
-        uint4v_t vd[H], vh[H], vs[H];
+        // asked for before the next row, and needed after the sum
+        if (ds && has_tail) ts = ds[tail];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int64_t q = t + (int64_t)i * nt;
+            vs[i] = uint4v_t{0, 0, 0, 0};
+            if (ds && q < full) vs[i] = load16_once(ds + q * E);
+        }
+        if constexpr (kAhead) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                vd[i] = nd[i];
+                vh[i] = nh[i];
+            }
+            rstd = nrstd;
+            td = ntd;
+            th = nth;
+            if (r + gridDim.x < a.rows) fetch(r + gridDim.x, nd, nh, nrstd, ntd, nth);
+        } else {
+            fetch(r, vd, vh, rstd, td, th);
+        }
         float s = 0.0f;
+        auto weights = [&](int i, int64_t q, float (&w)[E]) {
+            if constexpr (kAhead) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) w[e] = wv[i][e];
+            } else {
+                load_weights<E>(a.weight, a.wprec, q * E, w);
+            }
+        };
         auto along = [&](int i, int64_t q, const uint4v_t& d, const uint4v_t& x) {
             float w[E];
-            load_weights<E>(a.weight, a.wprec, q * E, w);
+            weights(i, q, w);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 const float g = elem<T>(d, e), xh = elem<T>(x, e) * rstd;
@@ -251,32 +313,30 @@ __global__ __launch_bounds__(NT) void k_rms_norm_backward(NormGradArgs a, float*
         };
         float gl = 0.0f, xl = 0.0f;
         if (has_tail) {
-            gl = (float)dy[tail];
-            xl = (float)h[tail] * rstd;
+            gl = (float)td;
+            xl = (float)th * rstd;
             s += gl * wlast * xl;
             dwlast += gl * xl;
         }
         if constexpr (NV > 0) {
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int64_t q = t + (int64_t)i * NT;
-                vd[i] = vh[i] = vs[i] = uint4v_t{0, 0, 0, 0};
-                if (q < full) {
-                    vd[i] = load16_once(dy + q * E);
-                    vh[i] = load16_once(h + q * E);
-                    if (ds) vs[i] = load16_once(ds + q * E);
-                }
-            }
-#pragma unroll
             for (int i = 0; i < NV; ++i)
-                if (t + (int64_t)i * NT < full) along(i, t + (int64_t)i * NT, vd[i], vh[i]);
+                if (t + (int64_t)i * nt < full) along(i, t + (int64_t)i * nt, vd[i], vh[i]);
         } else {
-            for (int64_t q = t; q < full; q += NT) along(0, q, load16(dy + q * E), load16(h + q * E));
+            for (int64_t q = t; q < full; q += nt) along(0, q, load16(dy + q * E), load16(h + q * E));
         }
-        const float mean = block_total<NT>(s, red[parity]) / (float)a.n;
-        auto store = [&](int64_t q, const uint4v_t& d, const uint4v_t& x, const uint4v_t& o) {
+        // the sum of the row; two sets of places, so that one barrier a row is enough
+        float total = wave_sum(s);
+        if (NT > 64 && nt > 64) {
+            if ((t & 63) == 0) red[parity][t >> 6] = total;
+            __syncthreads();
+            total = 0.0f;
+            for (int w = 0; w < nt / 64; ++w) total += red[parity][w];
+        }
+        const float mean = total / (float)a.n;
+        auto store = [&](int i, int64_t q, const uint4v_t& d, const uint4v_t& x, const uint4v_t& o) {
             float w[E], g[E];
-            load_weights<E>(a.weight, a.wprec, q * E, w);
+            weights(i, q, w);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 const float y = rstd * (elem<T>(d, e) * w[e] - elem<T>(x, e) * rstd * mean);
@@ -287,9 +347,9 @@ __global__ __launch_bounds__(NT) void k_rms_norm_backward(NormGradArgs a, float*
         if constexpr (NV > 0) {
 #pragma unroll
             for (int i = 0; i < NV; ++i)
-                if (t + (int64_t)i * NT < full) store(t + (int64_t)i * NT, vd[i], vh[i], vs[i]);
+                if (t + (int64_t)i * nt < full) store(i, t + (int64_t)i * nt, vd[i], vh[i], vs[i]);
         } else {
-            for (int64_t q = t; q < full; q += NT) {
+            for (int64_t q = t; q < full; q += nt) {
                 const uint4v_t d = load16(dy + q * E), x = load16(h + q * E);
                 if (mine) {
                     const bool first = r == blockIdx.x;
@@ -299,19 +359,19 @@ __global__ __launch_bounds__(NT) void k_rms_norm_backward(NormGradArgs a, float*
                         mine[q * E + e] = first ? g : mine[q * E + e] + g;
                     }
                 }
-                store(q, d, x, ds ? load16(ds + q * E) : uint4v_t{0, 0, 0, 0});
+                store(0, q, d, x, ds ? load16(ds + q * E) : uint4v_t{0, 0, 0, 0});
             }
         }
         if (has_tail) {
             const float y = rstd * (gl * wlast - xl * mean);
-            dx[tail] = from_f32<T>(ds ? y + (float)ds[tail] : y);
+            dx[tail] = from_f32<T>(ds ? y + (float)ts : y);
         }
     }
     if (!mine) return;
     if constexpr (NV > 0) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int64_t q = t + (int64_t)i * NT;
+            const int64_t q = t + (int64_t)i * nt;
             if (q < full)
 #pragma unroll
                 for (int h = 0; h < E / 4; ++h) {
@@ -391,18 +451,19 @@ struct NormGradPlan {
 NormGradPlan plan_norm_grad(int64_t rows, int64_t n, int prec) {
     const int64_t vecs = n / (prec == P32 ? 4 : 8);
     NormGradPlan p;
-    p.nt = vecs <= 128 ? 64 : vecs <= 512 ? 256 : vecs <= 1024 ? 512 : 1024;
-    const int64_t nv = (vecs + p.nt - 1) / p.nt;
-    p.nv = nv <= 1 ? 1 : nv <= 2 ? 2 : nv <= 4 ? 4 : 0;
-    // workgroups that a compute unit holds at once
-    p.groups = std::min<int64_t>(rows, 256 * std::max(1, 1024 / p.nt));
+    // waves that hold the row in two vectors a thread, four past 2 x 1024
+    p.nv = vecs <= 64 ? 1 : vecs <= 2048 ? 2 : vecs <= 4096 ? 4 : 0;
+    p.nt = p.nv == 0 ? 1024 : (int)std::max<int64_t>(1, (vecs + 64 * p.nv - 1) / (64 * p.nv)) * 64;
+    // as many workgroups as the compute units hold at once, with the same number of rows each
+    const int64_t most = 256 * std::max(1, 1024 / p.nt), rounds = std::max<int64_t>(1, (rows + most - 1) / most);
+    p.groups = (rows + rounds - 1) / rounds;
     return p;
 }
 
 template <typename T, int NV, int NT>
-hipError_t grad_launch(const NormGradArgs& a, float* part, int64_t groups, hipStream_t st) {
+hipError_t grad_launch(const NormGradArgs& a, float* part, const NormGradPlan& p, hipStream_t st) {
     KernelTimer t("rms_norm_backward", st);
-    hipLaunchKernelGGL((k_rms_norm_backward<T, NV, NT>), dim3((unsigned)groups), dim3(NT), 0, st, a, part);
+    hipLaunchKernelGGL((k_rms_norm_backward<T, NV, NT>), dim3((unsigned)p.groups), dim3(p.nt), 0, st, a, part);
     return hipGetLastError();
 }
 template <typename T> hipError_t grad_t(const NormGradArgs& a, Workspace& ws, hipStream_t st) {
@@ -414,12 +475,11 @@ template <typename T> hipError_t grad_t(const NormGradArgs& a, Workspace& ws, hi
     }
     hipError_t e = hipSuccess;
     if (a.rows) {
-        if (p.nt == 64) e = p.nv == 1 ? grad_launch<T, 1, 64>(a, part, p.groups, st) : grad_launch<T, 2, 64>(a, part, p.groups, st);
-        else if (p.nt == 256) e = p.nv == 1 ? grad_launch<T, 1, 256>(a, part, p.groups, st) : grad_launch<T, 2, 256>(a, part, p.groups, st);
-        else if (p.nt == 512) e = grad_launch<T, 2, 512>(a, part, p.groups, st);
-        else if (p.nv == 2) e = grad_launch<T, 2, 1024>(a, part, p.groups, st);
-        else if (p.nv == 4) e = grad_launch<T, 4, 1024>(a, part, p.groups, st);
-        else e = grad_launch<T, 0, 1024>(a, part, p.groups, st);
+        if (p.nv == 1) e = grad_launch<T, 1, 64>(a, part, p, st);
+        else if (p.nv == 2 && p.nt <= 512) e = grad_launch<T, 2, 512>(a, part, p, st);
+        else if (p.nv == 2) e = grad_launch<T, 2, 1024>(a, part, p, st);
+        else if (p.nv == 4) e = grad_launch<T, 4, 1024>(a, part, p, st);
+        else e = grad_launch<T, 0, 1024>(a, part, p, st);
     }
     if (e != hipSuccess || !a.dw) return e;
     KernelTimer t("rms_norm_dw", st);
