@@ -839,16 +839,17 @@ def _norm_args(x, weight, residual, eps, sum_out):
     prec = _head_prec(x.dtype)
     ldx = _rows(x, "x")
     dev = x.device
-    _on(dev, weight=weight, residual=residual)
     wprec = 0
     if weight is not None:
         wprec = _head_prec(weight.dtype)
         _need(weight.shape == (n,) and weight.is_contiguous(), f"weight must hold {n} contiguous values")
     if residual is None:
         _need(sum_out is None, "sum belongs to a residual")
+        _on(dev, weight=weight)
         return (x.data_ptr(), ldx, None, 0, rows, n, prec, weight.data_ptr() if weight is not None else None, wprec,
                 float(eps), None, 0), x, dev
     _need(residual.shape == x.shape and residual.dtype == x.dtype, "residual must have x's shape and dtype")
+    _on(dev, weight=weight, residual=residual)
     h, ldh = _like(sum_out, "sum", (rows, n), x.dtype, dev)
     return (x.data_ptr(), ldx, residual.data_ptr(), _rows(residual, "residual"), rows, n, prec,
             weight.data_ptr() if weight is not None else None, wprec, float(eps), h.data_ptr(), ldh), h, dev
@@ -894,7 +895,6 @@ def rms_norm_backward(dy, h, weight, rstd, dsum=None, dx=None):
     lddy, ldh = _rows(dy, "dy"), _rows(h, "h")
     pr = _row_values(rstd, "rstd", rows, _whole_dtypes()[2])
     _need(pr is not None, "rstd must be given")
-    _on(dev, h=h, weight=weight, rstd=rstd, dsum=dsum)
     pd, ldd = None, 0
     if dsum is not None:
         _need(dsum.shape == dy.shape and dsum.dtype == dy.dtype, "dsum must have dy's shape and dtype")
@@ -903,7 +903,10 @@ def rms_norm_backward(dy, h, weight, rstd, dsum=None, dx=None):
     if weight is not None:
         wprec = _head_prec(weight.dtype)
         _need(weight.shape == (n,) and weight.is_contiguous(), f"weight must hold {n} contiguous values")
-        pw, dw = weight.data_ptr(), _empty((n,), weight.dtype, dev)
+        pw = weight.data_ptr()
+    _on(dev, h=h, weight=weight, rstd=rstd, dsum=dsum)
+    if weight is not None:
+        dw = _empty((n,), weight.dtype, dev)
     dx, ldx = _like(dx, "dx", (rows, n), dy.dtype, dev)
     _launch(dev, "lrc_rms_norm_backward", dy.data_ptr(), lddy, h.data_ptr(), ldh, pr, rows, n, prec, pw, wprec, pd, ldd,
             dx.data_ptr(), ldx, dw.data_ptr() if dw is not None else None)
@@ -912,6 +915,7 @@ def rms_norm_backward(dy, h, weight, rstd, dsum=None, dx=None):
 
 def _adapter_args(A, B, ids, scale, rows, dtype, dev):
     """(m, n, k, count, prec, pointers of A, B, ids and scale)"""
+    prec = _head_prec(dtype)
     _need(A.dim() == 3 and B.dim() == 3, "A and B must be count x k x n and count x m x k")
     count, k, n = A.shape
     m = B.shape[1]
@@ -928,7 +932,7 @@ def _adapter_args(A, B, ids, scale, rows, dtype, dev):
         _need(scale.shape == (count,) and scale.is_contiguous(), f"scale must hold {count} contiguous values")
     _on(dev, A=A, B=B, ids=ids, scale=scale)
     _need(A.is_contiguous() and B.is_contiguous(), "tensors must be contiguous (row-major)")
-    return m, n, k, count, _head_prec(dtype), A.data_ptr(), B.data_ptr(), pi, scale.data_ptr() if scale is not None else None
+    return m, n, k, count, prec, A.data_ptr(), B.data_ptr(), pi, scale.data_ptr() if scale is not None else None
 
 
 def adapter_apply(X, A, B, ids, scale=None, base=None, hidden: bool = False, Y=None):
