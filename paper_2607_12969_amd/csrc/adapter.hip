@@ -280,13 +280,14 @@ __global__ __launch_bounds__(kSortThreads) void k_adapter_sort(AdapterSort s, in
     const int b = wave * per * 64, e = b + per * 64;        // positions of this wave; those past the rows stay last
     const u64 below = (1ull << lane) - 1, upto = below | 1ull << lane;
     for (int64_t q = t; q < s.count; q += kSortThreads) s.runs_of[q] = int2{0, 0};
-    for (int p = t; p < kSortThreads * per; p += kSortThreads) {
-        int k = INT32_MAX;
-        if (p < rows) {
-            const int64_t id = s.ids[p];
-            k = named(id, s.count) ? (int)id : (int)s.count;
-        }
-        skey[0][p] = k;
+    int64_t id[kLdsRows / kSortThreads];                    // all loads at once: one latency, not `per` of them
+#pragma unroll
+    for (int i = 0; i < kLdsRows / kSortThreads; ++i) id[i] = s.ids[std::min(t + i * kSortThreads, rows - 1)];
+#pragma unroll
+    for (int i = 0; i < kLdsRows / kSortThreads; ++i) {
+        const int p = t + i * kSortThreads;
+        if (i >= per) break;
+        skey[0][p] = p >= rows ? INT32_MAX : named(id[i], s.count) ? (int)id[i] : (int)s.count;
         sorder[0][p] = (unsigned short)p;
     }
     __syncthreads();
@@ -400,17 +401,21 @@ __global__ __launch_bounds__(kSortThreads) void k_adapter_sort(AdapterSort s, in
         if (walk) break;
         if (lane < 3) sums[wave][lane] = lane == 0 ? n[0] : lane == 1 ? n[1] : n[2];
         __syncthreads();
-        unsigned all[3] = {0, 0, 0};
-#pragma unroll 1
-        for (int w = 0; w < kSortWaves; ++w)
+        unsigned run[3];                                    // lane w: the waves up to w
+#pragma unroll
+        for (int q = 0; q < 3; ++q) run[q] = sums[lane & 15][q];
+#pragma unroll
+        for (int off = 1; off < 16; off <<= 1)
 #pragma unroll
             for (int q = 0; q < 3; ++q) {
-                at[q] += w < wave ? sums[w][q] : 0u;
-                all[q] += sums[w][q];
+                const unsigned v = __shfl_up(run[q], off, 16);
+                if ((lane & 15) >= off) run[q] += v;
             }
-        if (t == 0) {
-            s.counts[0] = (int)all[0];
-            s.counts[1] = (int)all[1];
+#pragma unroll
+        for (int q = 0; q < 3; ++q) at[q] = wave ? __shfl(run[q], wave - 1, 64) : 0u;
+        if (t == 15) {
+            s.counts[0] = (int)run[0];
+            s.counts[1] = (int)run[1];
         }
     }
 }
@@ -677,7 +682,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && (KS == 1 || KS == 2) ? 3 : 2
     __shared__ alignas(16) T qt[TURN ? 4 : 1][TURN ? KV * TP : 1];
     extern __shared__ uint4v_t dyn[];
     __shared__ float factor[kTile];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, lr = lane & 15, lg = lane >> 4;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 15, lg = lane >> 4;
     const int64_t lt = xcd_tile((int64_t)a.max_tiles * a.chunks);
     if (lt >= (int64_t)a.max_tiles * a.chunks) return;
     const int tile = (int)(lt / a.chunks), chunk = (int)(lt % a.chunks);
@@ -724,7 +729,11 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && (KS == 1 || KS == 2) ? 3 : 2
     }
     const T* Q = static_cast<const T*>(a.Q) + (int64_t)td.z * a.L * a.k;
     uint4v_t bn[NI], qn[KN][2];
-    // `edge`: the columns may pass L
+    // `edge`: the columns may pass L.  What lies past k (another rank's values, from a clamped
+    // place) becomes 0 where it is used: here it would make the fetch wait for itself.
+    auto past = [&](int s, int f) {
+        return TURN ? s * KV + f * (KV / 2) + lane / CH >= (int)a.k : VEC && s * KV + lg * E >= (int)a.k;
+    };
     auto fetch_q = [&](int64_t c, int s, uint4v_t (&q)[2], auto edge) {
 #pragma unroll
         for (int f = 0; f < 2; ++f) {
@@ -733,13 +742,11 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && (KS == 1 || KS == 2) ? 3 : 2
                 const T* row = Q + std::min(j, a.k - 1) * a.L;
                 if constexpr (edge) q[f] = load_zero16(row, c + ch * E, a.L);
                 else q[f] = load16(row + c + ch * E);
-                if (j >= a.k) q[f] = uint4v_t{0, 0, 0, 0};
             } else {
                 const int64_t j = (int64_t)s * KV + lg * E;
                 const T* row = Q + std::min(c + 16 * f + lr, a.L - 1) * a.k;
                 if constexpr (VEC) {
                     q[f] = load16(row + std::min<int64_t>(j, a.k - E));
-                    if (j >= a.k) q[f] = uint4v_t{0, 0, 0, 0};
                 } else {
                     q[f] = load_zero16(row, j, a.k);
                 }
@@ -769,23 +776,28 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && (KS == 1 || KS == 2) ? 3 : 2
         const int64_t step = a.rows * a.kp;
         const float inner = a.inner ? a.inner[td.z] : 1.0f;
         // E values of vector q, zeros past kp (and, as the parts hold them, rounded from garbage past k)
+        // (eight parts of all of it at once: the sum waits for memory once or twice)
         auto values = [&](int q, float (&x)[E]) {
+            constexpr int N4 = E / 4;
+            float4_t v[N4];
 #pragma unroll
-            for (int e = 0; e < E; e += 4) {
-                const int64_t j = (int64_t)q * E + e;
-                const float* f = from + std::min<int64_t>(j, a.kp - 4);
-                float4_t v = zero_accv<float4_t>();
-                for (int p = 0; p < a.splits; p += 4) {
-                    float4_t w[4];
+            for (int e = 0; e < N4; ++e) v[e] = zero_accv<float4_t>();
+            for (int p = 0; p < a.splits; p += 8) {
+                float4_t w[8][N4];
 #pragma unroll
-                    for (int h = 0; h < 4; ++h) w[h] = *reinterpret_cast<const float4_t*>(f + std::min(p + h, a.splits - 1) * step);
+                for (int h = 0; h < 8; ++h)
 #pragma unroll
-                    for (int h = 0; h < 4; ++h)
-                        if (p + h < a.splits) v += w[h];
-                }
+                    for (int e = 0; e < N4; ++e)
+                        w[h][e] = *reinterpret_cast<const float4_t*>(from + std::min<int64_t>((int64_t)q * E + 4 * e, a.kp - 4) +
+                                                                     std::min(p + h, a.splits - 1) * step);
 #pragma unroll
-                for (int h = 0; h < 4; ++h) x[e + h] = j + h < a.k ? v[h] * inner : 0.0f;
+                for (int h = 0; h < 8; ++h)
+                    if (p + h < a.splits)
+#pragma unroll
+                        for (int e = 0; e < N4; ++e) v[e] += w[h][e];
             }
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[e] = (int64_t)q * E + e < a.k ? v[e >> 2][e & 3] * inner : 0.0f;
         };
         unsigned amax = 0;
         for (int q = sub; q < 4 * steps; q += 4) {
@@ -853,12 +865,14 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && (KS == 1 || KS == 2) ? 3 : 2
     for (int i = 0; i < NI; ++i) fac[i] = factor[r0 + RS * i];
     uint4v_t b[NI], q[KN][2];
     auto product = [&](float4_t (&acc)[2][4], int s, const uint4v_t (&w)[2]) {
-        uint4v_t x[2] = {w[0], w[1]};
+        uint4v_t x[2];
+#pragma unroll
+        for (int f = 0; f < 2; ++f) x[f] = past(s, f) ? uint4v_t{0, 0, 0, 0} : w[f];
         if constexpr (TURN) {
             __builtin_amdgcn_wave_barrier();
 #pragma unroll
             for (int f = 0; f < 2; ++f)
-                *reinterpret_cast<uint4v_t*>(&qt[wave][(f * (KV / 2) + lane / CH) * TP + ch * E]) = w[f];
+                *reinterpret_cast<uint4v_t*>(&qt[wave][(f * (KV / 2) + lane / CH) * TP + ch * E]) = x[f];
             __builtin_amdgcn_wave_barrier();
 #pragma unroll
             for (int f = 0; f < 2; ++f) x[f] = turned<T>(qt[wave], TP, 0, 16 * f);
@@ -909,14 +923,14 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && (KS == 1 || KS == 2) ? 3 : 2
 #pragma unroll
                     for (int h = 0; h < 4; ++h) y[e + h] = elem<T>(b[i], e + h) + fac[i] * v[h];
                 }
-                if (live[i]) {
-                    if constexpr (edge) {
+                // rows past the tile's are its last row once more, bit for bit: stored without a
+                // branch, so that the next step's loads can be waited for without these stores
+                if constexpr (edge) {
 #pragma unroll
-                        for (int e = 0; e < E; ++e)
-                            if (cc + e < a.L) out[i][cc + e] = from_f32<T>(y[e]);
-                    } else {
-                        store16(out[i] + cc, pack16<T>(y));
-                    }
+                    for (int e = 0; e < E; ++e)
+                        if (live[i] && cc + e < a.L) out[i][cc + e] = from_f32<T>(y[e]);
+                } else {
+                    store16(out[i] + cc, pack16<T>(y));
                 }
             }
         }

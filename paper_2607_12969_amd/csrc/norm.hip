@@ -215,7 +215,9 @@ __global__ __launch_bounds__(NT) void k_rms_norm(NormArgs a, int64_t row0) {
 
 // A workgroup takes the rows g, g + G, .. and adds up their part of dw, each thread
 // for the columns that are its own: part[g][n].  NV <= 2: the next row is on its way
-// while this one is reduced, and the weights stay in registers.  NV = 0: rows of any
+// while this one is reduced, and the weights stay in registers; threads past the row's
+// vectors load and store the last one again, the same bits, without a branch (a branch around
+// stores would make the next row's loads wait for them).  NV = 0: rows of any
 // length, read twice, and dw through the partial sums in memory.
 template <typename T, int NV, int NT>
 __global__ __launch_bounds__(NT, 4) void k_rms_norm_backward(NormGradArgs a, float* __restrict__ part) {
@@ -238,8 +240,7 @@ __global__ __launch_bounds__(NT, 4) void k_rms_norm_backward(NormGradArgs a, flo
         for (int i = 0; i < NV; ++i) {
 #pragma unroll
             for (int e = 0; e < E; ++e) wv[i][e] = 0.0f;
-            const int64_t q = t + (int64_t)i * nt;
-            if (q < full) load_weights<E>(a.weight, a.wprec, q * E, wv[i]);
+            load_weights<E>(a.weight, a.wprec, std::min(t + (int64_t)i * nt, full - 1) * E, wv[i]);
         }
     }
     uint4v_t vd[H], vh[H], vs[H], nd[H], nh[H];
@@ -255,12 +256,9 @@ __global__ __launch_bounds__(NT, 4) void k_rms_norm_backward(NormGradArgs a, flo
         }
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int64_t q = t + (int64_t)i * nt;
-            d[i] = x[i] = uint4v_t{0, 0, 0, 0};
-            if (q < full) {
-                d[i] = load16_once(dy + q * E);
-                x[i] = load16_once(h + q * E);
-            }
+            const int64_t q = std::min(t + (int64_t)i * nt, full - 1);
+            d[i] = load16_once(dy + q * E);
+            x[i] = load16_once(h + q * E);
         }
     };
     int parity = 0;
@@ -275,9 +273,9 @@ __global__ __launch_bounds__(NT, 4) void k_rms_norm_backward(NormGradArgs a, flo
         if (ds && has_tail) ts = ds[tail];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int64_t q = t + (int64_t)i * nt;
+            const int64_t q = std::min(t + (int64_t)i * nt, full - 1);
             vs[i] = uint4v_t{0, 0, 0, 0};
-            if (ds && q < full) vs[i] = load16_once(ds + q * E);
+            if (ds) vs[i] = load16_once(ds + q * E);
         }
         if constexpr (kAhead) {
 #pragma unroll
@@ -347,7 +345,7 @@ __global__ __launch_bounds__(NT, 4) void k_rms_norm_backward(NormGradArgs a, flo
         if constexpr (NV > 0) {
 #pragma unroll
             for (int i = 0; i < NV; ++i)
-                if (t + (int64_t)i * nt < full) store(i, t + (int64_t)i * nt, vd[i], vh[i], vs[i]);
+                store(i, std::min(t + (int64_t)i * nt, full - 1), vd[i], vh[i], vs[i]);
         } else {
             for (int64_t q = t; q < full; q += nt) {
                 const uint4v_t d = load16(dy + q * E), x = load16(h + q * E);
@@ -452,7 +450,7 @@ NormGradPlan plan_norm_grad(int64_t rows, int64_t n, int prec) {
     const int64_t vecs = n / (prec == P32 ? 4 : 8);
     NormGradPlan p;
     // waves that hold the row in two vectors a thread, four past 2 x 1024
-    p.nv = vecs <= 64 ? 1 : vecs <= 2048 ? 2 : vecs <= 4096 ? 4 : 0;
+    p.nv = vecs < 1 ? 0 : vecs <= 64 ? 1 : vecs <= 2048 ? 2 : vecs <= 4096 ? 4 : 0;
     p.nt = p.nv == 0 ? 1024 : (int)std::max<int64_t>(1, (vecs + 64 * p.nv - 1) / (64 * p.nv)) * 64;
     // as many workgroups as the compute units hold at once, with the same number of rows each
     const int64_t most = 256 * std::max(1, 1024 / p.nt), rounds = std::max<int64_t>(1, (rows + most - 1) / most);
