@@ -647,8 +647,9 @@ int lrc_rms_norm_backward(const void* dy, int64_t lddy, const void* h, int64_t l
  * Errors: LRC_EINVAL for NULL pointers, rows < 0, m, n or count < 1, k outside
  * [1, LRC_ADAPTER_MAX_RANK], pitches below the rows, unknown precisions or an output
  * that overlaps an input (other than base = Y) or another output; LRC_EOVERFLOW as
- * elsewhere and for rows above 2^28 or count, m or n above 2^30; LRC_ENOMEM, LRC_EHIP,
- * LRC_ENODEV as elsewhere.
+ * elsewhere and for rows above 2^23, count above 2^22, m or n above 2^30 (in
+ * lrc_adapter_backward also where the gradients of A or B take more than 2^23 blocks of 512
+ * rows and 128 columns); LRC_ENOMEM, LRC_EHIP, LRC_ENODEV as elsewhere.
  */
 #define LRC_ADAPTER_MAX_RANK 256
 int lrc_adapter_apply(const void* X, int64_t ldx, const void* A, const void* B, const int64_t* ids, const float* scale,

@@ -538,12 +538,13 @@ __global__ __launch_bounds__(256, F <= 4 ? 2 : 1) void k_adapter_down(AdapterDow
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, lr = lane & 15, lg = lane >> 4;
     const int64_t lt = xcd_tile((int64_t)a.max_tiles * a.splits);
     if (lt >= (int64_t)a.max_tiles * a.splits) return;
-    const int split = (int)(lt / a.max_tiles), tile = (int)(lt % a.max_tiles);
+    const int split = (int)((unsigned)lt / (unsigned)a.max_tiles), tile = (int)lt - split * a.max_tiles;
+    const int4 td = a.tiles[tile];                             // on its way together with the count
     if (tile >= a.counts[0]) return;
-    const int4 td = a.tiles[tile];
     if (td.z >= a.count) return;
     const int64_t j0 = (int64_t)blockIdx.y * 128;              // ranks j0 .. j0 + 16 F
-    const int64_t steps = (a.L + S - 1) / S, s0 = steps * split / a.splits, s1 = steps * (split + 1) / a.splits;
+    const unsigned steps = (unsigned)((a.L + S - 1) / S), each = steps / (unsigned)a.splits, more = steps - each * a.splits;
+    const int64_t s0 = each * split + std::min<unsigned>(split, more), s1 = s0 + each + ((unsigned)split < more);
     const int ch = tid & 15, rr = tid >> 4;
     const T *px[4], *qx[F];
 #pragma unroll
@@ -600,15 +601,26 @@ __global__ __launch_bounds__(256, F <= 4 ? 2 : 1) void k_adapter_down(AdapterDow
         for (int i = 0; i < ST; ++i) load(std::min(s0 + i, whole - 1), vp[i], vq[i]);
         put(0, vp[0], vq[0]);
         __syncthreads();
-        for (int64_t s = s0; s < whole; s += ST) {
+        auto step = [&](int i) {
+            product(buf);
+            put(buf ^ 1, vp[(i + 1) % ST], vq[(i + 1) % ST]);
+            __syncthreads();
+            buf ^= 1;
+        };
+        int64_t s = s0;
+        // no branch between the loads: each wait is for its own (more than 64 ranks would spill)
+        for (; F <= 4 && s + 2 * ST <= whole; s += ST)
+#pragma unroll
+            for (int i = 0; i < ST; ++i) {
+                load(s + i + ST, vp[i], vq[i]);
+                step(i);
+            }
+        for (; s < whole; s += ST) {
 #pragma unroll
             for (int i = 0; i < ST; ++i) {
                 if (s + i >= whole) break;
                 if (s + i + ST < whole) load(s + i + ST, vp[i], vq[i]);
-                product(buf);
-                put(buf ^ 1, vp[(i + 1) % ST], vq[(i + 1) % ST]);
-                __syncthreads();
-                buf ^= 1;
+                step(i);
             }
         }
     }
@@ -685,9 +697,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && (KS == 1 || KS == 2) ? 3 : 2
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 15, lg = lane >> 4;
     const int64_t lt = xcd_tile((int64_t)a.max_tiles * a.chunks);
     if (lt >= (int64_t)a.max_tiles * a.chunks) return;
-    const int tile = (int)(lt / a.chunks), chunk = (int)(lt % a.chunks);
+    const int tile = (int)((unsigned)lt / (unsigned)a.chunks), chunk = (int)lt - tile * a.chunks;
+    const int4 td = a.tiles[tile];                                  // on its way together with the count
     if (tile >= a.counts[0]) return;
-    const int4 td = a.tiles[tile];
     const int64_t stride = (int64_t)a.chunks * 128;
     const bool has = td.z < a.count;
     const int steps = KS ? KS : ks, pitch = 4 * steps + 1;          // chunks of a row of H
@@ -1002,10 +1014,10 @@ __device__ __forceinline__ void outer_product(const AdapterOuter& a, OuterLds<T,
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, lr = lane & 15, lg = lane >> 4;
     const int64_t total = (int64_t)a.max_runs * a.tiles_l, lt = xcd_tile(total);
     if (blockIdx.x >= (total + 7) / 8 * 8 || lt >= total) return;       // the grid is the larger gradient's
-    const int run = (int)(lt / a.tiles_l);
+    const int run = total <= UINT32_MAX ? (int)((unsigned)lt / (unsigned)a.tiles_l) : (int)(lt / a.tiles_l);
+    const int4 rd = a.runs[run];                                        // on its way together with the count
     if (run >= a.counts[1]) return;
-    const int4 rd = a.runs[run];
-    const int64_t c0 = lt % a.tiles_l * 128, j0 = (int64_t)blockIdx.y * kOuterRanks<T>;
+    const int64_t c0 = (lt - (int64_t)run * a.tiles_l) * 128, j0 = (int64_t)blockIdx.y * kOuterRanks<T>;
     const int ch = tid % CH, r0 = tid / CH, n = rd.y;
     for (int p = tid; p < n; p += 256) order[p] = a.order[rd.x + p];
     __syncthreads();

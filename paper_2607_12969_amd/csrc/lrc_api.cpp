@@ -1230,9 +1230,11 @@ static int check_adapter(int64_t rows, int64_t m, int64_t n, int64_t k, int64_t 
     if (k < 1 || k > LRC_ADAPTER_MAX_RANK)
         return fail(LRC_EINVAL, "k = %lld outside [1, %d]", (long long)k, LRC_ADAPTER_MAX_RANK);
     if (!head_prec(prec)) return fail(LRC_EINVAL, "unknown precision code %d", prec);
+    // (grids of at most 2^24 workgroups)
     const int64_t most = (int64_t)1 << 30;
-    if (rows > (int64_t)1 << 28 || m > most || n > most || count > most)
-        return fail(LRC_EOVERFLOW, "rows = %lld above 2^28, or m, n or count above 2^30", (long long)rows);
+    if (rows > (int64_t)1 << 23 || count > (int64_t)1 << 22 || m > most || n > most)
+        return fail(LRC_EOVERFLOW, "rows = %lld above 2^23, count = %lld above 2^22, or m or n above 2^30", (long long)rows,
+                    (long long)count);
     int64_t t;
     if (!mul_ok(count * k, std::max(m, n), &t) || !mul_ok(t, 8, &t) || !mul_ok(rows + 1, std::max(m, n), &t) || !mul_ok(t, 2048, &t))
         return fail(LRC_EOVERFLOW, "array sizes overflow int64");
@@ -1276,6 +1278,8 @@ int lrc_adapter_backward(const void* dY, int64_t lddy, const void* X, int64_t ld
         return fail(LRC_EINVAL, "NULL array argument");
     if (!dX) base = nullptr;
     if (!dA) X = nullptr;
+    if ((dA || dB) && (rows / 512 + std::min(rows, count + 1)) * ((std::max(m, n) + 127) / 128) > (int64_t)1 << 23)
+        return fail(LRC_EOVERFLOW, "gradients of %lld adapters from %lld rows", (long long)count, (long long)rows);
     const int e = elem_bytes(prec);
     if ((rc = check_pitch(dY, "dY", rows, lddy, m, e, &yb)) || (rc = check_pitch(X, "X", rows, ldx, n, e, &xb)) ||
         (rc = check_pitch(base, "base", rows, ldb, n, e, &sb)) || (rc = check_pitch(dX, "dX", rows, lddx, n, e, &db)))

@@ -70,7 +70,7 @@ def test_adapter_refusals():
                dict(Y=A[0]), dict(Y=A[1]), dict(Y=A[2]), dict(Y=A[3]), dict(Y=A[4]), dict(Y=A[5], ldy=51), dict(Y=A[5] + 2),
                dict(hidden=A[0]), dict(hidden=A[5]), dict(hidden=A[6])):
         assert adapter(**kw) == INVALID, kw
-    assert adapter(rows=2 ** 28 + 1) == OVERFLOW and adapter(count=2 ** 31) == OVERFLOW and adapter(m=2 ** 31, ldb=2 ** 31, ldy=2 ** 31) == OVERFLOW
+    assert adapter(rows=2 ** 23 + 1) == OVERFLOW and adapter(count=2 ** 22 + 1) == OVERFLOW and adapter(m=2 ** 31, ldb=2 ** 31, ldy=2 ** 31) == OVERFLOW
     assert adapter(ldx=2 ** 62) == OVERFLOW
     assert adapter(count=2 ** 30, n=2 ** 30, ldx=2 ** 30, k=256) == OVERFLOW
     assert adapter(rows=0, X=None, Am=None, B=None, ids=None, Y=None) == 0
@@ -91,7 +91,9 @@ def test_adapter_gradient_refusals():
                dict(dX=A[7] + 2), dict(dX=A[7], lddx=101), dict(dX=A[6]), dict(dA=A[2]), dict(dA=A[8]), dict(dB=A[3]), dict(dB=A[9]),
                dict(dA=A[4]), dict(dB=A[7])):
         assert adapter_back(**kw) == INVALID, kw
-    assert adapter_back(rows=2 ** 28 + 1) == OVERFLOW
+    assert adapter_back(rows=2 ** 23 + 1) == OVERFLOW
+    assert adapter_back(rows=70000, count=70000, n=2 ** 16, ldx=2 ** 16, ldb=2 ** 16, lddx=2 ** 16) == OVERFLOW
+    assert b"gradients of 70000" in L().lrc_last_error()
     assert adapter_back(dX=None, dA=None, dB=None) == 0
     assert adapter_back(rows=0, dA=None, dB=None) == 0
     if nodev():
