@@ -264,9 +264,9 @@ __device__ __forceinline__ int block_min_behind(int x, int* red) {
 //
 // Up to 8192 rows, in LDS: a wave takes consecutive positions, 64 at a time.  A position's
 // rank among those of its digit is counted by ballots, lane d keeping the running number of
-// digit d; only the waves' totals meet.  The kernel runs once, so that its instructions come
-// from memory: the loops stay rolled (4096 rows: 14 us with the loops unrolled over registers,
-// 15 us with a counter of each thread and digit in LDS, 24 us through memory).
+// digit d; only the waves' totals meet.  4096 rows of 8 adapters take 15 us, bound by the
+// issue and the latency of one compute unit (counters of each thread and digit in LDS: 15 us
+// too, through memory: 24 us; the loops unrolled over registers: 14 us, for four times the code).
 __global__ __launch_bounds__(kSortThreads) void k_adapter_sort(AdapterSort s, int passes) {
     typedef unsigned long long u64;
     __shared__ int skey[2][kLdsRows];
@@ -433,6 +433,23 @@ __global__ __launch_bounds__(kSortThreads) void k_adapter_sort_memory(AdapterSor
     int which = 0;
     auto key = [&](int p) -> int& { return s.key[which][p]; };
     auto order = [&](int p) -> int& { return s.order[which][p]; };
+    // f(position, key, order) of this thread's positions in turn, those of 8 loaded at once: 65536
+    // rows of 8 adapters 312 us (one after the other, each waiting for memory, 413 us)
+    auto each = [&](auto with_order, auto&& f) {
+        for (int p = b; p < e; p += 8) {
+            int k[8], o[8] = {};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) k[j] = key(std::min(p + j, e - 1));
+            if constexpr (with_order)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) o[j] = order(std::min(p + j, e - 1));
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (p + j < e) f(p + j, k[j], o[j]);
+        }
+    };
+    const std::true_type yes;
+    const std::false_type no;
     for (int p = t; p < rows; p += kSortThreads) {
         const int64_t id = s.ids[p];
         key(p) = named(id, s.count) ? (int)id : (int)s.count;
@@ -443,7 +460,7 @@ __global__ __launch_bounds__(kSortThreads) void k_adapter_sort_memory(AdapterSor
         const int shift = 4 * pass;
 #pragma unroll
         for (int d = 0; d < 16; ++d) cnt[d * kSortThreads + t] = 0;
-        for (int p = b; p < e; ++p) ++cnt[(key(p) >> shift & 15) * kSortThreads + t];
+        each(no, [&](int, int k, int) { ++cnt[(k >> shift & 15) * kSortThreads + t]; });
         __syncthreads();
         // running count over (digit, thread): thread t's 16 entries are consecutive
         unsigned c[16], sum = 0, total;
@@ -459,43 +476,50 @@ __global__ __launch_bounds__(kSortThreads) void k_adapter_sort_memory(AdapterSor
             at += c[d];
         }
         __syncthreads();
-        for (int p = b; p < e; ++p) {
-            const int k = key(p), o = order(p);
+        each(yes, [&](int, int k, int o) {
             const unsigned to = cnt[(k >> shift & 15) * kSortThreads + t]++;
-            which ^= 1;
-            key(to) = k;
-            order(to) = o;
-            which ^= 1;
-        }
+            s.key[which ^ 1][to] = k;
+            s.order[which ^ 1][to] = o;
+        });
         which ^= 1;
         __syncthreads();
     }
     // segments of equal keys
-    int first = -1, head = INT32_MAX;        // this thread's last and first segment start
-    for (int p = b; p < e; ++p)
-        if (p == 0 || key(p) != key(p - 1)) {
+    const int left = b > 0 && b < e ? key(b - 1) : -1;              // keys are not negative
+    int first = -1, head = INT32_MAX, prev = left;                  // this thread's last and first segment start
+    each(no, [&](int p, int k, int) {
+        if (k != prev) {
             first = p;
             head = std::min(head, p);
         }
+        prev = k;
+    });
     const int before = block_max_before(first, redi);
     const int behind = block_min_behind(head, redi);
     // two walks over this thread's positions: count, then write
     unsigned tiles = 0, runs = 0, slots = 0, tile0 = 0, run0 = 0, slot0 = 0;
+#pragma unroll 1
     for (int walk = 0; walk < 2; ++walk) {
-        int start = before;
-        for (int p = b; p < e; ++p) {
-            const int k = key(p);
-            if (p == 0 || k != key(p - 1)) start = p;
+        int start = before, end = -1;                               // end: of the segment, once it is known
+        prev = left;
+        each(no, [&](int p, int k, int) {
+            if (k != prev) {
+                start = p;
+                end = -1;
+            }
+            prev = k;
             const int in = p - start;
-            if (in % kTile) continue;
+            if (in % kTile) return;
             // the segment's end: the next start, here or behind this thread's part
             const bool run = in % kRun == 0 && k < s.count;
-            int end = std::min(behind, rows);
-            for (int q = p + 1; q < e; ++q)
-                if (key(q) != key(q - 1)) {
-                    end = q;
-                    break;
-                }
+            if (end < 0) {
+                end = std::min(behind, rows);
+                for (int q = p + 1; q < e; ++q)
+                    if (key(q) != k) {
+                        end = q;
+                        break;
+                    }
+            }
             const int n_runs = (end - start + kRun - 1) / kRun;
             if (walk) s.tiles[tile0 + tiles] = int4{p, std::min(kTile, end - p), k, 0};
             ++tiles;
@@ -507,7 +531,7 @@ __global__ __launch_bounds__(kSortThreads) void k_adapter_sort_memory(AdapterSor
                 ++runs;
                 slots += n_runs > 1;
             }
-        }
+        });
         if (!walk) {
             unsigned nt, nr, ns;
             tile0 = block_scan(tiles, red, nt);

@@ -1010,7 +1010,7 @@ static int q4_apply(const void* codes, const void* scales, int sprec, int64_t gr
     const Q4Weights w{codes, scales, m, n, group, sprec, U, s, V, k, fprec};
     Workspace& ws = workspace_for(dev, st);
     ws.reset();
-    const size_t bytes = q4_apply_workspace_bytes(w, X, ldx, batch, prec);
+    const size_t bytes = q4_apply_workspace_bytes(w, X, ldx, batch, prec, yprec);
     hipError_t e = bytes ? ws.reserve(bytes, st) : hipSuccess;
     if (e != hipSuccess) return fail_hip(e, "workspace");
     e = launch_q4_apply(w, X, ldx, xscale, Y, ldy, batch, prec, yprec, ws, st);

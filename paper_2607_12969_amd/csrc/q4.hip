@@ -1221,6 +1221,18 @@ __global__ __launch_bounds__(256) void k_q4_pack8(const unsigned char* __restric
     }
 }
 
+// e4m3 activations as binary16, which holds every one of them, in padded rows (pitch ldp,
+// zero from n on).
+__global__ __launch_bounds__(256) void k_q4_widen8(const unsigned char* __restrict__ X, int64_t ldx, int64_t n, int64_t b,
+                                                   half_t* __restrict__ out, int64_t ldp) {
+    const int64_t per = ldp / 8, step = (int64_t)gridDim.x * 256;
+    for (int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x; c < b * per; c += step) {
+        half8_t v[1];
+        load_act<e4m3_t>(reinterpret_cast<const e4m3_t*>(X + c / per * ldx), c % per * 8, n, v);
+        *reinterpret_cast<half8_t*>(out + c * 8) = v[0];
+    }
+}
+
 // ---- T' = diag(s) V^T x -----------------------------------------------------
 // Partial sums of V^T x over a range of columns: part[split][batch][k].  A
 // workgroup of 4 waves takes 16 TW batch rows and up to 16 F ranks; steps of 128
@@ -1645,6 +1657,7 @@ struct Q4Plan {
     int64_t mid_chunk;
     bool mid_finish;      // T' finished by a kernel of its own ...
     bool pairs;           // ... as pairs of binary16
+    bool widen;           // e4m3 activations through binary16
     size_t tm, mid_part, planes, part;
 };
 
@@ -1670,7 +1683,12 @@ bool plan_rows(Q4Plan& p, const Q4Weights& w, int64_t b, int prec) {
     return true;
 }
 
-Q4Plan plan_q4(const Q4Weights& w, const void* X, int64_t ldx, int64_t b, int prec) {
+// e4m3 activations and a result in FP32 go by way of binary16: the 8-bit instruction adds its
+// 128 products with fewer bits than binary32 has.  Relative to 64 bits and the results'
+// size (n = 4096): 4.4e-6 by it, 7e-8 by the 16-bit ones; results of 16 bits (2.4e-4 and
+// 2e-3 by their own rounding) do not see the difference, and 4096 rows of 8192 take 315 us in
+// place of 650.
+Q4Plan plan_q4(const Q4Weights& w, const void* X, int64_t ldx, int64_t b, int prec, int yprec) {
     Q4Plan p{};
     const int64_t blocks = (w.n + 127) / 128;
     p.tile = !plan_rows(p, w, b, prec);
@@ -1684,7 +1702,9 @@ Q4Plan plan_q4(const Q4Weights& w, const void* X, int64_t ldx, int64_t b, int pr
         const int e = elem_bytes(prec);
         p.ldp = blocks * 128;
         p.pack = prec == P32 || w.n % 128 || reinterpret_cast<uintptr_t>(X) % 16 || ldx * e % 16;
-        if (p.pack) p.planes = (size_t)(prec == P32 ? 3 : 1) * b * p.ldp * std::min(e, 2);
+        p.widen = prec == PE4M3 && yprec == P32;
+        if (p.widen) p.planes = (size_t)b * p.ldp * 2;
+        else if (p.pack) p.planes = (size_t)(prec == P32 ? 3 : 1) * b * p.ldp * std::min(e, 2);
         if (p.splits > 1) p.part = (size_t)p.splits * b * w.m * 4;
     }
     if (w.k) {
@@ -1699,7 +1719,7 @@ Q4Plan plan_q4(const Q4Weights& w, const void* X, int64_t ldx, int64_t b, int pr
         p.mid_splits = (int)((w.n + p.mid_chunk - 1) / p.mid_chunk);
         p.mid_finish = p.tile || b * p.mid_splits > 64 || b * kp > kRowsTm;
         p.mid_part = (size_t)p.mid_splits * b * w.k * 4;
-        p.pairs = prec == PE4M3 && p.tile && w.fprec == P16;
+        p.pairs = prec == PE4M3 && p.tile && !p.widen && w.fprec == P16;
         if (p.pairs) p.tm = (size_t)round_up(b * 4, 256) + (size_t)2 * b * round_up(w.k, 32) * 2;
         else if (p.mid_finish) p.tm = (size_t)b * kp * 4;
     }
@@ -1820,14 +1840,14 @@ void mid8(const Q4Plan& p, const Q4Weights& w, const Q4Args& a, float* part, hip
 
 template <typename T>
 hipError_t apply_t(const Q4Weights& w, Q4Args& a, int prec, Workspace& ws, hipStream_t st) {
-    const Q4Plan p = plan_q4(w, a.X, a.ldx, a.b, prec);
+    const Q4Plan p = plan_q4(w, a.X, a.ldx, a.b, prec, a.yprec);
     float* Tm = static_cast<float*>(ws.take(p.tm));
     float* mid = static_cast<float*>(ws.take(p.mid_part));
     unsigned short* planes = static_cast<unsigned short*>(ws.take(p.planes));
     a.part = static_cast<float*>(ws.take(p.part));
     if (ws.overrun) return hipErrorOutOfMemory;
     if (w.k) {
-        if (p.pairs && p.mid_tw == 4 && w.k >= 8) mid8(p, w, a, mid, st);
+        if (prec == PE4M3 && w.fprec == P16 && p.mid_tw == 4 && w.k >= 8) mid8(p, w, a, mid, st);
         else if (w.k <= 32) mid_f<T, 2>(p, w, a, mid, st);
         else if (w.k <= 80) mid_f<T, 5>(p, w, a, mid, st);
         else mid_f<T, 8>(p, w, a, mid, st);
@@ -1857,8 +1877,20 @@ hipError_t apply_t(const Q4Weights& w, Q4Args& a, int prec, Workspace& ws, hipSt
         return rows_t<T, 4>(p, a, st);
     }
     a.splits = p.splits;
+    auto tiles = [&](auto x) {
+        using X = decltype(x);
+        if (a.gshift == 5) tile_t<X, 1>(p, a, st);
+        else if (a.gshift == 6) tile_t<X, 2>(p, a, st);
+        else tile_t<X, 4>(p, a, st);
+    };
     if constexpr (std::is_same_v<T, e4m3_t>) {
-        if (p.pack) {
+        if (p.widen) {
+            KernelTimer t("q4_pack", st);
+            hipLaunchKernelGGL(k_q4_widen8, dim3(strided_grid(a.b * (p.ldp / 8))), dim3(256), 0, st,
+                               static_cast<const unsigned char*>(a.X), a.ldx, w.n, a.b, reinterpret_cast<half_t*>(planes), p.ldp);
+            a.X = planes;
+            a.ldx = p.ldp;
+        } else if (p.pack) {
             KernelTimer t("q4_pack", st);
             hipLaunchKernelGGL(k_q4_pack8, dim3(strided_grid(a.b * (p.ldp / 16))), dim3(256), 0, st,
                                static_cast<const unsigned char*>(a.X), a.ldx, w.n, a.b, reinterpret_cast<unsigned char*>(planes),
@@ -1866,7 +1898,8 @@ hipError_t apply_t(const Q4Weights& w, Q4Args& a, int prec, Workspace& ws, hipSt
             a.X = planes;
             a.ldx = p.ldp;
         }
-        if (a.gshift == 5) tile8_t<1>(p, a, st);
+        if (p.widen) tiles(half_t());
+        else if (a.gshift == 5) tile8_t<1>(p, a, st);
         else if (a.gshift == 6) tile8_t<2>(p, a, st);
         else tile8_t<4>(p, a, st);
     } else {
@@ -1878,9 +1911,7 @@ hipError_t apply_t(const Q4Weights& w, Q4Args& a, int prec, Workspace& ws, hipSt
             a.ldx = p.ldp;
             a.plane = a.b * p.ldp;
         }
-        if (a.gshift == 5) tile_t<T, 1>(p, a, st);
-        else if (a.gshift == 6) tile_t<T, 2>(p, a, st);
-        else tile_t<T, 4>(p, a, st);
+        tiles(T());
     }
     if (p.splits > 1) {
         KernelTimer t("q4_join", st);
@@ -1898,12 +1929,12 @@ hipError_t apply_t(const Q4Weights& w, Q4Args& a, int prec, Workspace& ws, hipSt
 constexpr int64_t kQ4Panel = 1 << 20;
 int64_t weight_panel(int64_t batch) { return std::min<int64_t>(1 << 28, ((int64_t)1 << 36) / batch); }
 
-size_t q4_apply_workspace_bytes(const Q4Weights& w, const void* X, int64_t ldx, int64_t batch, int prec) {
+size_t q4_apply_workspace_bytes(const Q4Weights& w, const void* X, int64_t ldx, int64_t batch, int prec, int yprec) {
     size_t bytes = 0;
     auto panel = [&](int64_t m, int64_t b) {
         Q4Weights part = w;
         part.m = m;
-        if (m && b) bytes = std::max(bytes, plan_bytes(plan_q4(part, X, ldx, b, prec)));
+        if (m && b) bytes = std::max(bytes, plan_bytes(plan_q4(part, X, ldx, b, prec, yprec)));
     };
     const int64_t b = std::min(batch, kQ4Panel), m = std::min(w.m, weight_panel(b));
     for (int64_t rows : {b, batch % b}) {

@@ -141,3 +141,19 @@ def test_large_tiles(lrc, m, n, k, group, b, sdt):
         small = lrc.q4_apply(codes, scales, X[part], group, F, out_dtype=torch.float32, x_scales=t[part])
         size = got[part].abs().mean()
         assert (small - got[part]).abs().max() <= 1e-4 * size * 10
+
+
+@pytest.mark.parametrize("b", [1, 8, 9, 17, 48, 64, 65, 130, 300])
+@pytest.mark.parametrize("m,n,group", [(300, 1024, 128), (2100, 1000, 32), (530, 777, 64), (260, 1024, 512)])
+def test_sums_hold_32_bits(lrc, b, m, n, group):
+    """Whole activations and weights whose sums stay below 2^24 (1024 * 448 * 12 = 5.5e6): every partial sum is a whole number
+    that binary32 holds, so a result in FP32 is exact, whatever the order of its sums."""
+    rng = np.random.default_rng([5, b, m, n])
+    codes, scales = rng.integers(0, 16, (m, n)), torch.full((m, -(-n // group)), 2.0).half()
+    W = H.weights(codes, scales.double().numpy(), group)
+    whole = O.E4M3[(O.E4M3 == np.floor(O.E4M3))]
+    X = torch.from_numpy(rng.choice(whole, (b, n)) * rng.choice([-1.0, 1.0], (b, n))).float().to(torch.float8_e4m3fn).cuda()
+    t = torch.from_numpy(2.0 ** rng.integers(-3, 4, b)).float().cuda()
+    want = host(t)[:, None] * (host(X.float()) @ W.T)
+    got = lrc.q4_apply(torch.from_numpy(H.pack(codes)).cuda(), scales.cuda(), X, group, out_dtype=torch.float32, x_scales=t)
+    assert np.array_equal(host(got), want)
