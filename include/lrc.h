@@ -581,7 +581,10 @@ int lrc_distill_backward(const void* logits, int64_t ld, int64_t rows, int64_t v
  *   xscale  device, batch factors (binary32): row b of Y is
  *           xscale_b (X_b W^T + [(X_b V) diag(s)] U^T)
  * The rest as lrc_q4_apply.  Products of codes and activations are exact; the
- * row's factor enters last, in binary32.  An e4m3 NaN makes its row NaN.
+ * row's factor enters last, in binary32.  Y in LRC_FP32: sums in binary32.  Y in 16 bits,
+ * batches above 8: the matrix instruction adds 128 products with fewer bits (about 2^-18
+ * of the sums' size in all), and with factors in LRC_FP16 (X_b V) diag(s) enters the second
+ * product with 22 bits of the row's largest.  An e4m3 NaN makes its row NaN.
  */
 int lrc_q4_apply_e4m3(const void* codes, const void* scales, int sprec, int64_t group, const void* U, const void* s,
                       const void* V, int64_t k, int fprec, const void* X, int64_t ldx, const float* xscale, void* Y,

@@ -1357,8 +1357,13 @@ template <typename T, int F> void outer_f(const AdapterOuter& a, const AdapterOu
     hipLaunchKernelGGL((k_adapter_outer<T, F>), grid, dim3(256), 0, st, a, b);
 }
 
-// Batches of this many rows and fewer go row by row.
-constexpr int64_t kFewRows = 64;
+// Few rows go one by one, each with its adapter's factors from L2 or beyond; more are sorted by
+// adapter first, which costs three launches and the sort.  8192 x 8192 with a base, in us, row by
+// row against sorted, of 4 and of 64 adapters: bfloat16, k = 16: 64 rows 13 and 14, 128 rows 13
+// against 25 and 15 against 31, 256 rows 19 against 28 and 26 against 31; k = 64: 128 rows 35 against 37 and
+// 48 against 45, 256 rows 63 against 46 and 85 against 45; FP32, k = 16: 128 rows 20 against 25 and 27
+// against 54, 256 rows 38 against 32 and 45 against 54; k = 64: 128 rows 75 against 54 and 101 against 128.
+bool few_rows(int64_t rows, int64_t k, int prec) { return rows <= 64 || (rows <= 256 && rows * k * elem_bytes(prec) <= 16384); }
 
 int64_t rows_splits(int64_t n, int prec) {
     const int64_t per = 64 * (prec == P32 ? 4 : 8);
@@ -1372,7 +1377,7 @@ struct ApplySlices {
 };
 ApplySlices apply_slices(const AdapterArgs& a, Slices& s) {
     ApplySlices o{};
-    if (a.rows <= kFewRows) {
+    if (few_rows(a.rows, a.k, a.prec)) {
         o.part = s.take<float>(rows_splits(a.n, a.prec) * a.rows * a.k);
         return o;
     }
@@ -1386,7 +1391,7 @@ template <typename T> hipError_t apply_t(const AdapterArgs& a, Workspace& ws, hi
     Slices s{&ws};
     const ApplySlices o = apply_slices(a, s);
     if (ws.overrun) return hipErrorOutOfMemory;
-    if (a.rows <= kFewRows) {
+    if (few_rows(a.rows, a.k, a.prec)) {
         const int splits = (int)rows_splits(a.n, a.prec);
         {
             KernelTimer t("adapter_down_rows", st);

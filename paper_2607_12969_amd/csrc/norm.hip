@@ -9,6 +9,9 @@
 // registers of its workgroup between its sum, its maximum and its output (up to NV
 // vectors of 16 bytes a thread); longer rows are read again.  Thread t of NT takes
 // the row's whole vectors t, t + NT, .. and the n % kVec last elements one a thread.
+// 4096 rows of 8192 in bfloat16 with a residual, to e4m3: 50 us, 4.7 TB/s (a large copy
+// 4.7); 2047 rows of 5003 (odd rows begin off 16 bytes) 21 us, their gradient 25 us and 5 for
+// the sum of dw: 3.9 and 3.3 TB/s.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -410,13 +413,15 @@ __global__ __launch_bounds__(1024) void k_rms_norm_dw(const float* __restrict__ 
 
 namespace {
 
-// Threads of a row: with many rows as few as hold it in four vectors each, with few
-// rows one vector each.  nv = 0: the row is read again.
+// Threads of a row: with many rows as few as hold it in four vectors each, so that a compute
+// unit holds several rows, with few rows one vector each.  bfloat16, rows of 5003, four vectors against
+// one: 512 rows 11.6 and 9.2 us, 1024 rows 14.2 and 15.5, 4096 rows 40 and 48 (rows of 8192, which
+// fill 1024 threads: 12.6 and 9.3, 16.7 and 16.4, 52 and 49).  nv = 0: the row is read again.
 struct NormPlan {
     int nt, nv;
 };
 NormPlan plan_norm(int64_t rows, int64_t n, int prec) {
-    const int64_t vecs = n / (prec == P32 ? 4 : 8), want = rows >= 512 ? 4 : 1;
+    const int64_t vecs = n / (prec == P32 ? 4 : 8), want = rows >= 1024 ? 4 : 1;
     NormPlan p{vecs <= 64 * want ? 64 : vecs <= 256 * want ? 256 : 1024, 0};
     const int64_t nv = (vecs + p.nt - 1) / p.nt;
     p.nv = nv <= 1 ? 1 : nv <= 2 ? 2 : nv <= 4 ? 4 : 0;
