@@ -295,3 +295,60 @@ def test_offsets_past_32_bits(lrc):
     L = x.unflatten(0, (R, D + 1))
     one, two = lrc.verify(L, d, u, draft_logits=L[:, :D]), lrc.verify(small.view(R, D + 1, n), d, u, draft_logits=small.view(R, D + 1, n)[:, :D])
     assert torch.equal(one[0], two[0]) and torch.equal(one[1], two[1])
+
+
+# ---------------------------------------------------------------- many of them --
+
+@pytest.mark.parametrize("R,D,V", [(70000, 1, 5), (1, 3000, 3), (2, 65536, 2), (5000, 7, 2)])
+def test_many_requests_and_drafts(lrc, R, D, V):
+    """Greedy: drafts hold up to the first that is not its row's largest logit."""
+    g = torch.Generator(device="cuda").manual_seed(R)
+    L = torch.randn(R, D + 1, V, generator=g, device="cuda")
+    best = L.argmax(2)
+    stop = torch.randint(0, D + 1, (R,), generator=g, device="cuda")
+    drafts = best[:, :D].clone()
+    at = torch.arange(D, device="cuda")[None] == stop[:, None]
+    drafts[at] = (drafts[at] + 1) % V
+    tokens, accepted = lrc.verify(L, drafts, torch.rand(R, D + 1, generator=g, device="cuda"), temperature=torch.zeros(R, device="cuda"))
+    behind = torch.arange(D + 1, device="cuda")[None] > stop[:, None]
+    assert torch.equal(accepted, stop) and torch.equal(tokens, best.masked_fill(behind, -1))
+
+
+@pytest.mark.parametrize("rows,n", [(300000, 4), (70000, 1), (2100000, 3), (3, 300001)])
+def test_norm_of_many_rows_and_of_long_ones(lrc, rows, n):
+    """Against 64 bits: n + 8 roundings of the sum (halved by the root), four of the product."""
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    x, dy = torch.randn(rows, n, generator=g, device="cuda"), torch.randn(rows, n, generator=g, device="cuda")
+    w = torch.randn(n, generator=g, device="cuda")
+    y, h, rstd = lrc.rms_norm(x, w, stats=True, eps=1e-3)
+    X, W, DY = x.double(), w.double(), dy.double()
+    r = (X * X).mean(1, keepdim=True).add(1e-3).rsqrt()
+    bound = (n + 16) * U
+    assert ((y.double() - X * r * W).abs() <= bound * (X * r * W).abs() + 1e-38).all()
+    dx, dw = lrc.rms_norm_backward(dy, h, w, rstd)
+    s = (DY * W * X * r).mean(1, keepdim=True)
+    size = (DY * W * X * r).abs().mean(1, keepdim=True)
+    want, scale = r * (DY * W - X * r * s), r * ((DY * W).abs() + (X * r).abs() * size)
+    assert ((dx.double() - want).abs() <= 2 * bound * scale + 1e-38).all()
+    want, scale = (DY * X * r).sum(0), (DY * X * r).abs().sum(0)
+    assert ((dw.double() - want).abs() <= (bound + (rows + 16) * U) * scale).all()
+
+
+def test_adapters_of_a_great_many_rows(lrc):
+    """More rows than two bytes name; whole values, so that every sum is exact."""
+    rows, n, m, k, count = 300000, 4, 5, 2, 7
+    g = torch.Generator(device="cuda").manual_seed(11)
+    whole = lambda *s: torch.randint(-2, 3, s, generator=g, device="cuda").float()  # noqa: E731
+    X, A, B, base, dY = whole(rows, n), whole(count, k, n), whole(count, m, k), whole(rows, m), whole(rows, m)
+    ids = torch.randint(-1, count + 1, (rows,), generator=g, device="cuda")
+    Y, Hd = lrc.adapter_apply(X, A, B, ids, base=base, hidden=True)
+    dX, dA, dB = lrc.adapter_backward(dY, X, A, B, ids, Hd)
+    wH, wY, wX = torch.zeros(rows, k, device="cuda"), base.clone(), torch.zeros(rows, n, device="cuda")
+    for a in range(count):
+        i = ids == a
+        wH[i] = X[i] @ A[a].T
+        wY[i] += wH[i] @ B[a].T
+        dh = dY[i] @ B[a]
+        wX[i] = dh @ A[a]
+        assert torch.equal(dA[a], dh.T @ X[i]) and torch.equal(dB[a], dY[i].T @ wH[i])
+    assert torch.equal(Hd, wH) and torch.equal(Y, wY) and torch.equal(dX, wX)
