@@ -280,9 +280,10 @@ __global__ __launch_bounds__(kSortThreads) void k_adapter_sort(AdapterSort s, in
     const int b = wave * per * 64, e = b + per * 64;        // positions of this wave; those past the rows stay last
     const u64 below = (1ull << lane) - 1, upto = below | 1ull << lane;
     for (int64_t q = t; q < s.count; q += kSortThreads) s.runs_of[q] = int2{0, 0};
-    int64_t id[kLdsRows / kSortThreads];                    // all loads at once: one latency, not `per` of them
+    int64_t id[kLdsRows / kSortThreads] = {};               // all loads at once: one latency, not `per` of them
+    if (rows > 0)
 #pragma unroll
-    for (int i = 0; i < kLdsRows / kSortThreads; ++i) id[i] = s.ids[std::min(t + i * kSortThreads, rows - 1)];
+        for (int i = 0; i < kLdsRows / kSortThreads; ++i) id[i] = s.ids[std::min(t + i * kSortThreads, rows - 1)];
 #pragma unroll
     for (int i = 0; i < kLdsRows / kSortThreads; ++i) {
         const int p = t + i * kSortThreads;

@@ -352,3 +352,30 @@ def test_adapters_of_a_great_many_rows(lrc):
         wX[i] = dh @ A[a]
         assert torch.equal(dA[a], dh.T @ X[i]) and torch.equal(dB[a], dY[i].T @ wH[i])
     assert torch.equal(Hd, wH) and torch.equal(Y, wY) and torch.equal(dX, wX)
+
+
+@pytest.mark.parametrize("prec", ["fp32", "fp16", "bf16"])
+def test_gradients_without_rows(lrc, prec):
+    """Empty tensors, without memory of their own, and weights whose gradients are 0."""
+    new = lambda *s: torch.empty(*s, dtype=DT[prec], device="cuda")  # noqa: E731
+    A, B, w = new(3, 5, 20).fill_(1), new(3, 30, 5).fill_(1), new(20).fill_(1)
+    ids = torch.empty(0, dtype=torch.int64, device="cuda")
+    dX, dA, dB = lrc.adapter_backward(new(0, 30), new(0, 20), A, B, ids, torch.empty(0, 5, device="cuda"))
+    assert dX.shape == (0, 20) and not dA.any() and not dB.any()
+    assert lrc.adapter_apply(new(0, 20), A, B, ids).shape == (0, 30)
+    dx, dw = lrc.rms_norm_backward(new(0, 20), new(0, 20), w, torch.empty(0, device="cuda"))
+    assert dx.shape == (0, 20) and not dw.any()
+
+
+@pytest.mark.parametrize("prec", ["fp32", "fp16", "bf16"])
+@pytest.mark.parametrize("rows,n", [(3000, 515), (2047, 5003), (700, 9000), (300, 17000), (40, 8)])
+def test_norm_gradient_in_place(lrc, prec, rows, n):
+    g = torch.Generator(device="cuda").manual_seed(n)
+    rand = lambda *s: torch.randn(*s, generator=g, device="cuda").to(DT[prec])  # noqa: E731
+    dy, h, ds, w = rand(rows, n), rand(rows, n), rand(rows, n), rand(n)
+    rstd = lrc.rms_norm(h, w, stats=True)[2]
+    want, dw = lrc.rms_norm_backward(dy, h, w, rstd, dsum=ds)
+    for mine in (0, 1):
+        a, b = dy.clone(), ds.clone()
+        got, dw2 = lrc.rms_norm_backward(a, h, w, rstd, dsum=b, dx=(a, b)[mine])
+        assert torch.equal(got, want) and torch.equal(dw, dw2)
