@@ -554,7 +554,8 @@ __global__ __launch_bounds__(kSortThreads) void k_adapter_sort_memory(AdapterSor
 // ranks: more would spill).  Q is N x k x L, or (TURN)
 // N x L x k: then its part lies in LDS as it does in memory and the operands come by the
 // transposing read.  16-byte chunks are XOR-swizzled by the row.  VEC: k in whole vectors
-// (TURN).  part[split][position][kp].
+// (TURN).  part[split][position][kp].  4096 rows of 8192 (67 MB): k = 16 and 64 20 us, 3.3 TB/s;
+// a workgroup has nine steps, and three dependent reads before the first.
 template <typename T, int F, bool TURN, bool VEC>
 __global__ __launch_bounds__(256, F <= 4 ? 2 : 1) void k_adapter_down(AdapterDown a) {
     constexpr int E = kVec<T>, S = 16 * E, QP = 16 * F + E;          // QP: pitch of turned rows
@@ -706,8 +707,9 @@ __global__ __launch_bounds__(256) void k_adapter_join(AdapterDown a, const int* 
 // comes straight from L2 as operands, or (TURN: N x k x L) through LDS of the wave and
 // the transposing read, the base straight from memory, all of it one step ahead.  A wave
 // works alone, without a barrier: its results cross LDS, 32 rows at a time, so that
-// neighbouring lanes load and store neighbouring 16 bytes of a row (with the operands' own
-// layout, 16 rows apart from lane to lane, 4096 rows of 8192 at k = 64 took 51 us).
+// neighbouring lanes load and store neighbouring 16 bytes of a row.  4096 rows of 8192 with a
+// base (134 MB): k = 16 34 us, k = 64 45 (51 with the operands' own layout, 16 rows apart from
+// lane to lane).
 // KS: steps of the K axis (k rounded up), 0: any number.  VEC: k in whole vectors, so
 // that operands are loaded without a branch.
 template <typename T, int KS, bool VEC, bool TURN>
@@ -1018,8 +1020,9 @@ __global__ __launch_bounds__(256) void k_adapter_range(AdapterRange a) {
 }
 
 // G = sum over a run's rows of P_row x H_row.  One workgroup of 4 waves: 128 columns of P,
-// of them 32 a wave, and up to 16 F ranks; steps of 64 rows go through registers to one of two LDS buffers, H as kParts values, turned ([rank][row]).  COLS: G is k x L (else
-// L x k).
+// of them 32 a wave's, and up to 16 F ranks; steps of 64 rows go through registers to one of
+// two LDS buffers, H as kParts values, turned ([rank][row]).  COLS: G is k x L (else L x k).
+// 4096 rows of 8192, k = 16, both gradients: 34 to 40 us for 134 MB.
 // Ranks of a workgroup of `outer` (more would spill).
 template <typename T> inline constexpr int kOuterRanks = sizeof(T) == 4 ? 32 : 64;
 
@@ -1364,7 +1367,9 @@ template <typename T, int F> void outer_f(const AdapterOuter& a, const AdapterOu
 // against 25 and 15 against 31, 256 rows 19 against 28 and 26 against 31; k = 64: 128 rows 35 against 37 and
 // 48 against 45, 256 rows 63 against 46 and 85 against 45; FP32, k = 16: 128 rows 20 against 25 and 27
 // against 54, 256 rows 38 against 32 and 45 against 54; k = 64: 128 rows 75 against 54 and 101 against 128.
-bool few_rows(int64_t rows, int64_t k, int prec) { return rows <= 64 || (rows <= 256 && rows * k * elem_bytes(prec) <= 16384); }
+bool few_rows(int64_t rows, int64_t k, int prec) {
+    return rows <= 64 || (rows <= 256 && rows * k * elem_bytes(prec) <= 16384);
+}
 
 int64_t rows_splits(int64_t n, int prec) {
     const int64_t per = 64 * (prec == P32 ? 4 : 8);
