@@ -600,7 +600,8 @@ int lrc_q4_apply_e4m3(const void* codes, const void* scales, int sprec, int64_t 
  *           `x` itself (equal pitch).  Not written without residual
  *   y       device, rows x n (pitch ldy) in `yprec`: prec, or LRC_E4M3
  *   scales  device, rows, for LRC_E4M3: t = max |y| / 448 of the row, and y holds the
- *           e4m3 values nearest to y / t (ties to even; 0 where t is 0).  A row with a
+ *           e4m3 values nearest to y / t, rounded to binary32 first (ties to even; 0 where
+ *           t is 0).  A row with a
  *           NaN or an infinity among its y gets the scale NaN and codes NaN
  *   rstd    device, rows, or NULL: (mean h^2 + eps)^(-1/2), for the gradient
  * Sums are in binary32: squares pass its range for |h| above 1.8e19, and such rows give 0.

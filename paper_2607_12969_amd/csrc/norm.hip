@@ -2,7 +2,7 @@
 // asked for, an 8-bit output behind; and its gradient.
 //
 //   h = x + r (rounded once to the storage type), rstd = (mean h^2 + eps)^(-1/2),
-//   y = h rstd w;   in 8 bits: t = max |y| / 448, y8 = the e4m3 value nearest to y / t.
+//   y = h rstd w;   in 8 bits: t = max |y| / 448, y8 = the e4m3 value nearest to the binary32 y / t.
 //   dh = rstd (w dy - h rstd mean(w dy h rstd)) + dsum,   dw = sum_rows dy h rstd.
 //
 // Bound by memory: every array is read or written once.  A row stays in the
@@ -75,20 +75,29 @@ template <int NT> __device__ __forceinline__ float block_total(float x, float* r
     else return block_add<NT>(x, red);
 }
 
-// The 8-bit codes of a row: y / t, t its scale.  The factor 1 / t is rounded once
-// more than a division is; where it would pass binary32's range, y is divided.
+// The 8-bit codes of a row: the values nearest to the binary32 quotients y / t, t its scale, ties to
+// even.  A quotient is y (1 / t) corrected by its remainder twice: the first time leaves it less than
+// a step from y / t, the second the nearest binary32 value.  (y (1 / t) alone is off by a step or two, which
+// takes the other neighbour where y / t lies there beside the middle of two codes; products of bfloat16 values
+// and weights meet such middles in one place of ten thousand.)  4096 rows of 8192: 50 us with
+// and without the corrections.
 struct ToE4m3 {
-    float t, inv;
+    float t, up, d, inv;         // d = t up, a power of two that keeps the remainders of tiny scales in range
     bool nan;
     __device__ __forceinline__ explicit ToE4m3(unsigned amax_bits) {
         nan = amax_bits >= 0x7F800000u;                     // a NaN or an infinity among the y
         t = nan ? __builtin_nanf("") : __uint_as_float(amax_bits) / kE4m3Max;
-        inv = 1.0f / t;
+        up = t < 0x1p-60f ? 0x1p80f : 1.0f;
+        d = t * up;
+        inv = d > 0.0f ? 1.0f / d : 0.0f;                   // a scale of 0: codes 0
     }
-    // nearest, ties to even; the clamp meets scales that rounding made too small
+    // the clamp meets scales that rounding made too small
     __device__ __forceinline__ float scaled(float y) const {
-        const float q = inv <= 3.4028234663852886e38f ? y * inv : t > 0.0f ? y / t : 0.0f;
-        return __builtin_fminf(__builtin_fmaxf(q, -kE4m3Max), kE4m3Max);
+        const float a = y * up;
+        float q = a * inv;
+        q = __builtin_fmaf(__builtin_fmaf(-q, d, a), inv, q);
+        q = __builtin_fmaf(__builtin_fmaf(-q, d, a), inv, q);
+        return __builtin_copysignf(__builtin_fminf(__builtin_fabsf(q), kE4m3Max), y);     // the corrections lose the sign of 0
     }
     __device__ __forceinline__ unsigned pack4(const float* y) const {
         if (nan) return kE4m3NaN;

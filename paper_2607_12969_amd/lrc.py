@@ -873,8 +873,8 @@ def rms_norm(x, weight=None, residual=None, eps: float = 1e-6, stats: bool = Fal
 
 def rms_norm_e4m3(x, weight=None, residual=None, eps: float = 1e-6, out=None, sum=None):
     """rms_norm with y in 8 bits: returns (codes, scales, h), codes (rows x n,
-    float8_e4m3fn) the values nearest to y / scale and scales (rows, float32)
-    max |y| / 448 of each row, as q4_apply takes them."""
+    float8_e4m3fn) the values nearest to the float32 quotients y / scale and
+    scales (rows, float32) max |y| / 448 of each row, as q4_apply takes them."""
     args, h, dev = _norm_args(x, weight, residual, eps, sum)
     rows, n = args[4], args[5]
     y, ldy = _like(out, "out", (rows, n), _e4m3_dtype(), dev)
