@@ -335,13 +335,12 @@ __global__ __launch_bounds__(NT, 4) void k_rms_norm_backward(NormGradArgs a, flo
         } else {
             for (int64_t q = t; q < full; q += nt) along(0, q, load16(dy + q * E), load16(h + q * E));
         }
-        // Where dx is dy or dsum, what a thread past the row's vectors has loaded has to be here
-        // before the wave that owns it stores: the barrier alone does not wait for loads.
-        if constexpr (NV > 0)
-            if (t + (int64_t)(NV - 1) * nt >= full) {
-                stay(vd);
-                stay(vs);
-            }
+        // Where dx is dy or dsum, several threads load a row's last vector and several store it: it has
+        // to be here in each of them before the barrier, behind which the first may store.
+        if constexpr (NV > 0) {
+            stay(vd);
+            stay(vs);
+        }
         // the sum of the row; two sets of places, so that one barrier a row is enough
         float total = wave_sum(s);
         if (NT > 64 && nt > 64) {
