@@ -79,8 +79,8 @@ template <int NT> __device__ __forceinline__ float block_total(float x, float* r
 // even.  A quotient is y (1 / t) corrected by its remainder twice: the first time leaves it less than
 // a step from y / t, the second the nearest binary32 value.  (y (1 / t) alone is off by a step or two, which
 // takes the other neighbour where y / t lies there beside the middle of two codes; products of bfloat16 values
-// and weights meet such middles in one place of ten thousand.)  4096 rows of 8192: 50 us with
-// and without the corrections.
+// and weights meet such middles in one place of ten thousand.)  4096 rows of 8192: 51 us with
+// the corrections, 50.5 without (shortest calls).
 struct ToE4m3 {
     float t, up, d, inv;         // d = t up, a power of two that keeps the remainders of tiny scales in range
     bool nan;
