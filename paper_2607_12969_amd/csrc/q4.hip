@@ -1789,10 +1789,15 @@ void tile8_sb(const Q4Plan& p, const Q4Args& a, hipStream_t st) {
     if (p.nx == 2) return launch_tile8<1, 2, 4, FL, SB>(a, st);
     launch_tile8<1, 4, 4, FL, SB>(a, st);
 }
-// Large products: at least a workgroup of the wide tile for every compute unit.  8192 x 8192,
-// k = 65: 1792 rows (224 wide tiles) 180 us on the smaller tile, 2048 rows (256) 145 on the wide one;
-// 4096 rows 429 and 310 to 336.
-bool wide8_takes(const Q4Args& a) { return a.gshift >= 7 && a.b > 128 && ((a.m + 255) / 256) * ((a.b + 255) / 256) >= 256; }
+// Whether the wide tile takes a product: where its rounds of a tile for every compute unit, which
+// last one and a half times as long, are fewer by as much.  8192 x 8192, k = 65, wide and 256 x 128 tiles in us:
+// 1024 rows (one round of each) 144 and 109, 1152 rows (one and two) 145 and 190, 2048 rows 158 and 199, 2049
+// rows (two and three) 279 and 280, 4096 rows (two and four) 304 and 385; 33024 x 2048, 300 rows (two and two) 108 and 84;
+// 66048 x 2048, 300 rows (three and four) 150 and 147.
+bool wide8_takes(const Q4Args& a) {
+    auto rounds = [&](int64_t bt) { return ((a.m + 255) / 256 * ((a.b + bt - 1) / bt) + 255) / 256; };
+    return a.gshift >= 7 && 3 * rounds(256) <= 2 * rounds(128);
+}
 template <int FL>
 void tile8_t(const Q4Plan& p, const Q4Args& a, hipStream_t st) {
     if constexpr (FL == 4)

@@ -94,9 +94,11 @@ def weights(nib, scales, n, group, cols):
     return H.weights(nib[:, :n].cpu().numpy()[cols].astype(int), scales.double().cpu().numpy()[cols], group)
 
 
-# m, n, k, group, batch: tiles of 256 x 256 (groups of 128 and more; one and odd numbers of groups a row), of 256 x 128, of
-# 128 x 128, of 64, 32 and 16 rows of X, and split over columns; last tiles of a few rows and columns
+# m, n, k, group, batch: tiles of 256 x 256 (groups of 128 and more; one and odd numbers of groups a row), of 256 x 128 (groups of
+# 128 in one round of them, and in two where 256 x 256 tiles take two as well; groups of 32 and 64), of 128 x 128, of 64, 32 and
+# 16 rows of X, and split over columns; last tiles of a few rows and columns
 SIZES = [(4100, 640, 65, 128, 4097), (8192, 130, 9, 256, 2000), (4352, 1000, 12, 512, 3850), (8200, 300, 21, 128, 1030),
+         (8150, 300, 21, 128, 1010), (33000, 130, 8, 128, 300),
          (8192, 200, 33, 32, 1100), (8200, 330, 8, 64, 1030), (300, 515, 65, 128, 130), (200, 1030, 7, 32, 257), (530, 777, 20, 64, 140),
          (500, 2048, 65, 128, 64), (257, 1000, 16, 32, 50), (135, 640, 130, 64, 33), (300, 1100, 5, 256, 17), (260, 2100, 40, 32, 9)]
 TYPES = [("fp16", "fp16"), ("fp32", "fp32"), ("bf16", "bf16"), ("fp32", "fp16"), ("bf16", "fp32")]
