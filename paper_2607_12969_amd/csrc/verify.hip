@@ -11,11 +11,13 @@
 // of sample.hip.  All sums are of whole numbers: the result does not depend on how
 // the work is split.
 //
-// Three launches.  The first, one workgroup a row, passes each row as often as its
-// filters need (maximum; bins, cut; sum) and leaves which tokens it keeps, their sum
-// and the draft's weight.  The others decide and draw: sums over parts of the row (or two)
-// that a request draws from, then the part that holds the token (by one workgroup a
-// request in one launch 48 requests of 65536 took 60 us, 14 + 10 in two).
+// The rows come in rounds, a launch each: as many places of every request at first as fill the compute
+// units, then twice as many each time; rows behind a rejected draft are left out (48 requests of 5
+// drafts: two rounds, 140 of 8: four).  A workgroup passes its row as often as the filters need (maximum;
+// bins, cut; sum) and leaves which tokens it keeps, their sum and the draft's weight.  Two more launches
+// decide and draw: sums over parts of the row (or two) that a request draws from, then the part that
+// holds the token (by one workgroup a request in one launch 48 requests of 65536 took 60 us, 14 + 10 in
+// two).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -193,7 +195,6 @@ __device__ __forceinline__ void law_of_row(Shared& s, const R& row, const Kept<W
     });
 }
 
-// Rows whose cut the fast paths do not hold: every pass over the row.
 // A cut with ties that are not all kept.
 template <typename T>
 __device__ __noinline__ void law_ties(Shared& s, Row<T> row, Kept<Weigh> kept, RowLaw* law) {
@@ -202,6 +203,7 @@ __device__ __noinline__ void law_ties(Shared& s, Row<T> row, Kept<Weigh> kept, R
     *law = o;
 }
 
+// Rows whose cut the fast paths do not hold: every pass over the row.
 template <typename T, typename W>
 __device__ __noinline__ void law_any(Shared& s, Row<T> row, W wt, int64_t k, float p, float floor_w, RowLaw* law) {
     RowLaw o = *law;
