@@ -1219,7 +1219,8 @@ struct AdapterPlan {
         const int64_t segments = std::min(rows, count + 1);
         max_tiles = std::max<int64_t>(1, rows / kTile + segments);
         max_runs = std::max<int64_t>(1, rows / kRun + segments);
-        max_slots = 2 * (rows / kRun) + 1;
+        // an adapter of r > kRun rows has at most (r + kRun - 1) / kRun runs
+        max_slots = std::max<int64_t>(1, (rows + (kRun - 1) * std::min(count, rows / (kRun + 1))) / kRun);
     }
     // columns of `down` are split until about 512 workgroups share them
     int down_splits(int64_t L, int e) const {
