@@ -106,39 +106,27 @@ __device__ __forceinline__ bool named(int64_t id, int64_t count) { return (uint6
 }  // namespace
 
 // ---- few rows -----------------------------------------------------------------
-// part[split][row][k]: X_row A^T over 64 E VX columns.
-template <typename T, int VX>
+// part[split][row][k]: X_row A^T over 64 E columns.
+template <typename T>
 __global__ __launch_bounds__(256) void k_adapter_down_rows(AdapterArgs a, float* __restrict__ part) {
     constexpr int E = kVec<T>;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t r = blockIdx.y, id = a.ids[r];
     if (!named(id, a.count)) return;
-    const int64_t c0 = (int64_t)blockIdx.x * 64 * E * VX;
-    const T* x = static_cast<const T*>(a.X) + r * a.ldx;
+    const int64_t c = ((int64_t)blockIdx.x * 64 + lane) * E;
     const T* A = static_cast<const T*>(a.A) + id * a.k * a.n;
-    float xv[VX][E];
-#pragma unroll
-    for (int v = 0; v < VX; ++v) {
-        const uint4v_t w = load_zero16(x, c0 + (v * 64 + lane) * E, a.n);
-#pragma unroll
-        for (int e = 0; e < E; ++e) xv[v][e] = elem<T>(w, e);
-    }
+    const uint4v_t x = load_zero16(static_cast<const T*>(a.X) + r * a.ldx, c, a.n);
     float* out = part + ((int64_t)blockIdx.x * a.rows + r) * a.k;
     for (int64_t j0 = wave * 4; j0 < a.k; j0 += 16) {
         float s[4];
-        uint4v_t w[4][VX];
+        uint4v_t w[4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-#pragma unroll
-            for (int v = 0; v < VX; ++v)
-                w[q][v] = load_zero16(A + std::min(j0 + q, a.k - 1) * a.n, c0 + (v * 64 + lane) * E, a.n);
+        for (int q = 0; q < 4; ++q) w[q] = load_zero16(A + std::min(j0 + q, a.k - 1) * a.n, c, a.n);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             s[q] = 0.0f;
 #pragma unroll
-            for (int v = 0; v < VX; ++v)
-#pragma unroll
-                for (int e = 0; e < E; ++e) s[q] += xv[v][e] * elem<T>(w[q][v], e);
+            for (int e = 0; e < E; ++e) s[q] += elem<T>(x, e) * elem<T>(w[q], e);
             s[q] = wave_sum(s[q]);
         }
         if (lane < 4 && j0 + lane < a.k) out[j0 + lane] = lane == 0 ? s[0] : lane == 1 ? s[1] : lane == 2 ? s[2] : s[3];
@@ -1019,13 +1007,14 @@ __global__ __launch_bounds__(256) void k_adapter_range(AdapterRange a) {
     }
 }
 
+// Ranks of a workgroup of `outer`: more would spill (and in 16-bit types a build of 128 gave
+// wrong gradients of B, for a reason that was not found).
+template <typename T> inline constexpr int kOuterRanks = sizeof(T) == 4 ? 32 : 64;
+
 // G = sum over a run's rows of P_row x H_row.  One workgroup of 4 waves: 128 columns of P,
 // of them 32 a wave's, and up to 16 F ranks; steps of 64 rows go through registers to one of
 // two LDS buffers, H as kParts values, turned ([rank][row]).  COLS: G is k x L (else L x k).
 // 4096 rows of 8192, k = 16, both gradients: 34 to 40 us for 134 MB.
-// Ranks of a workgroup of `outer` (more would spill).
-template <typename T> inline constexpr int kOuterRanks = sizeof(T) == 4 ? 32 : 64;
-
 template <typename T, int F> struct OuterLds {
     static constexpr int PITCH = 128 + (sizeof(T) == 4 ? 4 : 16), HP = 64 + kVec<T>;
     alignas(16) T p[2][64 * PITCH];
@@ -1402,7 +1391,7 @@ template <typename T> hipError_t apply_t(const AdapterArgs& a, Workspace& ws, hi
         const int splits = (int)rows_splits(a.n, a.prec);
         {
             KernelTimer t("adapter_down_rows", st);
-            hipLaunchKernelGGL((k_adapter_down_rows<T, 1>), dim3(splits, (unsigned)a.rows), dim3(256), 0, st, a, o.part);
+            hipLaunchKernelGGL(k_adapter_down_rows<T>, dim3(splits, (unsigned)a.rows), dim3(256), 0, st, a, o.part);
         }
         int shift = 0;
         while (shift < 4 && (kVec<T> << shift) < a.k) ++shift;
