@@ -18,7 +18,9 @@
 // gradients of A and B, long runs of rows split and joined in order).  H and dH stay in
 // binary32; as an operand of the 16-bit matrix cores a value is the sum of two 16-bit ones
 // (16 bits of a bfloat16 pair, 22 of a binary16 pair), which is well below the rounding
-// of the 16-bit result.  Binary16 pairs are scaled by a power of two, of the row or, where rows
+// of the 16-bit result.  (Three bfloat16 values, 24 bits, leave the results' errors against 64 bits
+// as they are to four digits, 1.66e-3 by their own rounding, and cost, 4096 rows of 8192: k = 16 2 of 166 us,
+// k = 64 2 of 67 in the product and 45 of 154 in the gradient, k = 96 18 of 82 and 63 of 274.)  Binary16 pairs are scaled by a power of two, of the row or, where rows
 // are summed, of the column of the tile, so that their range does not matter.
 #include <hip/hip_runtime.h>
 
