@@ -1683,9 +1683,9 @@ bool plan_rows(Q4Plan& p, const Q4Weights& w, int64_t b, int prec) {
 
 // e4m3 activations and a result in FP32 or FP16 go by way of binary16: the 8-bit instruction cuts
 // products (k_q4_tile8) by up to 7 2^-13 of the largest of eight columns, which is below half of what
-// rounding the sum of magnitudes to bfloat16 may take, but four times as much for binary16.  The largest
-// activation's own rounding to e4m3 may have taken 2^-4.  Sums of random values, relative to 64
-// bits and the results' size (n = 4096): 4.4e-6 by it, 7e-8 by the 16-bit instructions.  8192 x 8192, k = 65,
+// rounding the sum of magnitudes to bfloat16 may take, but four times as much for binary16.  Relative to 64 bits
+// and the results' size (n = 4096): 4.4e-6 by it for random values, up to 4e-5 with a few columns 20 to 1000
+// times larger (their rounding to e4m3 costs 2e-2), 7e-8 by the 16-bit instructions.  8192 x 8192, k = 65,
 // bfloat16 and FP32 results: 48 rows 41 and 41 us, 512 rows 100 and 117, 4096 rows 306 and 667; 65536 x 4096, 48
 // rows 60 and 71.
 Q4Plan plan_q4(const Q4Weights& w, const void* X, int64_t ldx, int64_t b, int prec, int yprec) {
